@@ -1,0 +1,296 @@
+"""Timed cases of what follows the gradients in a training step: the global
+norm over all gradient tensors, clipping by it, and the AdamW update.
+
+A case is a dict of plain values. ``op`` says which operator it goes through:
+
+  norm   the L2 norm of all gradients of a network
+  clip   the gradients scaled to a norm of at most ``max_norm``, written to
+         buffers of their own
+  adamw  one AdamW step of every tensor; with a finite ``max_norm`` its
+         gradients are clipped on the way
+
+``net`` names a list of tensor shapes, or is "" for ``tensors`` tensors of
+uneven sizes with ``elems`` elements together. ``g``, ``o`` and ``w`` are the
+types of the gradients, the clipped gradients and the weights; ``master`` says
+that bf16 weights have a 32-bit copy that the update works on. ``shift`` moves
+every tensor that many elements off its aligned place.
+
+The tensors of one kind lie in one arena, each in a slot of its own that starts
+at a multiple of 64 elements (plus ``shift``), the gaps filled with zeros. So
+the plain form may work on whole arenas (a zero gradient of a zero weight
+changes nothing), and the gaps show whether a kernel wrote outside a tensor.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+INF = math.inf
+BETA1, BETA2, EPS, DECAY, LR = 0.9, 0.999, 1e-8, 0.01, 1e-3
+DONE = 1000  # steps done before the timed one
+
+NETS = {
+    # the 784 -> 100 layer
+    "dense1": [100 * 784],
+    # the 784-1000-1000-10 MLP
+    "mlp3": [784 * 1000, 1000 * 1000, 1000 * 10],
+    # the 9-layer conv net on 32x32x3
+    "conv9": [9 * a * b for a, b in ((3, 64), (64, 64), (64, 128), (128, 128), (128, 256),
+                                     (256, 256), (256, 256), (256, 256))] + [256 * 16 * 10],
+    # the 20-layer conv net on 28x28x1
+    "conv20": [9 * 32] + 9 * [9 * 32 * 32] + [9 * 32 * 64] + 8 * [9 * 64 * 64] + [64 * 10],
+    # stacks of the wide 4096 -> 4096 layer
+    "wide1": [4096 * 4096],
+    "wide4": 4 * [4096 * 4096],
+    "wide12": 12 * [4096 * 4096],
+}
+
+
+def _case(name, op, net, tensors=0, elems=0, g="f32", o="f32", w="f32", master=False, max_norm=1.0,
+          shift=0):
+    return dict(name=name, op=op, net=net, tensors=tensors, elems=elems, g=g, o=o, w=w,
+                master=master, max_norm=max_norm, shift=shift)
+
+
+def listed():
+    return [
+        # one small layer: launches and latency
+        _case("norm-dense1", "norm", "dense1"),
+        # the diagnostics of a deep conv net: a few hundred thousand weights in 20 tensors
+        _case("norm-conv20", "norm", "conv20"),
+        # a wide network's gradients as the backward writes them, and as they are exchanged
+        _case("norm-wide12", "norm", "wide12"),
+        _case("norm-wide4-bf16", "norm", "wide4", g="bf16"),
+        # clipped gradients for an optimiser of the user's own
+        _case("clip-mlp3", "clip", "mlp3", max_norm=0.5),
+        # a wide network's exchanged gradients, clipped and widened again
+        _case("clip-wide4-bf16", "clip", "wide4", g="bf16"),
+        # many small tensors off their aligned places, clipped and narrowed for the exchange
+        _case("clip-many-ragged-bf16", "clip", "", 700, 5_000_011, o="bf16", max_norm=2.0, shift=1),
+        # a clipped training step of the nets that this repository trains
+        _case("adamw-dense1", "adamw", "dense1"),
+        _case("adamw-conv9", "adamw", "conv9"),
+        # very many very small tensors: gains, biases, thresholds
+        _case("adamw-many-small", "adamw", "", 1500, 400_003, max_norm=5.0),
+        # the wide layer with bf16 weights and their 32-bit copy, without clipping
+        _case("adamw-wide1-master", "adamw", "wide1", w="bf16", master=True, max_norm=INF),
+        # the largest: a wide network's clipped step
+        _case("adamw-wide12", "adamw", "wide12"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["norm", "clip", "adamw", "adamw"])
+    elems = _log(rng, 1_000, 150_000_000)
+    tensors = min(_log(rng, 1, 1500), elems)
+    w = rng.choice(["f32", "f32", "bf16"])
+    c = _case("", op, "", tensors, elems, rng.choice(["f32", "f32", "bf16"]),
+              rng.choice(["f32", "bf16"]), w, w == "bf16" and rng.random() < 0.6,
+              rng.choice([0.3, 1.0, 50.0, INF if op == "adamw" else 10.0]),
+              rng.choice([0, 0, 0, 1, 2, 3]))
+    c.pop("name")
+    return c
+
+
+# ------------------------------------------------------------------ inputs --
+def _dev():
+    return torch.device("cuda" if torch.cuda.is_available() else "cpu")
+
+
+def _dtype(name):
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _sizes(c):
+    """Elements of each tensor. The uneven sizes are shares of the whole that
+    spread over a factor of 400, every tensor with an element at least."""
+    if c["net"]:
+        return NETS[c["net"]]
+    n, left = c["tensors"], c["elems"] - c["tensors"]
+    rng = random.Random(n * 1_000_003 + c["elems"])
+    share = [math.exp(rng.uniform(0.0, 6.0)) for _ in range(n)]
+    k = left / sum(share)
+    sizes = [1 + int(k * s) for s in share]
+    sizes[rng.randrange(n)] += c["elems"] - sum(sizes)
+    return sizes
+
+
+def _slots(c):
+    """(start, elements) of each tensor in its arena, and the arena's length."""
+    at, slots = 0, []
+    for n in _sizes(c):
+        slots.append((at + c["shift"], n))
+        at += -(-(n + c["shift"]) // 64) * 64
+    return slots, at
+
+
+def _inputs(c, seed):
+    """The arenas of gradients, weights, moments. Gradients of a spiking layer:
+    a quarter exactly zero (silent neurons), the others over a few decades."""
+    gen = torch.Generator(device=_dev()).manual_seed(int(seed))
+    slots, total = _slots(c)
+    inside = torch.zeros(total + 1, dtype=torch.int32, device=_dev())
+    edges = torch.tensor(slots, device=_dev())
+    inside.index_add_(0, edges[:, 0], torch.ones(len(slots), dtype=torch.int32, device=_dev()))
+    inside.index_add_(0, edges.sum(1), -torch.ones(len(slots), dtype=torch.int32, device=_dev()))
+    inside = inside[:total].cumsum(0) > 0
+
+    def normal():
+        return torch.randn(total, generator=gen, device=_dev())
+
+    scale = 10.0 / math.sqrt(sum(_sizes(c)))
+    g = normal() * (0.8 * normal()).exp_() * scale
+    g = g * (torch.rand(total, generator=gen, device=_dev()) > 0.25) * inside
+    a = dict(g=g.to(_dtype(c["g"])))
+    if c["op"] == "adamw":
+        w = normal() * 0.05 * inside
+        a["w"] = w.to(_dtype(c["w"]))
+        if c["master"]:
+            a["w32"] = w
+        a["m"] = normal() * (0.3 * scale) * inside
+        a["v"] = (normal() * scale).square_() * inside
+    elif c["op"] == "clip":
+        a["out"] = torch.zeros(total, dtype=_dtype(c["o"]), device=_dev())
+    return a
+
+
+def prepare(case, seed):
+    s = dict(case, **_inputs(case, seed))
+    s["norm"] = torch.zeros(1, device=_dev())
+    if case["op"] == "adamw":
+        s["step"] = torch.full((1,), DONE, dtype=torch.int64, device=_dev())
+        s["lr"] = torch.full((1,), LR, device=_dev())  # on the device: a schedule writes it there
+    if own:
+        from paper_2607_14672_amd import dstd
+
+        slots, _ = _slots(case)
+
+        def tensors(key):
+            return [s[key][a:a + n] for a, n in slots] if key in s else None
+
+        s["list"] = dstd.make_tensor_list(tensors("g"), weights=tensors("w"), m=tensors("m"),
+                                          v=tensors("v"), master=tensors("w32"), out=tensors("out"))
+        s["ws"] = dstd.workspace(dstd.dstd_tensor_list_workspace_size(s["list"].c), _dev())
+        if case["op"] == "adamw":
+            s["hp"] = dstd.make_adamw(LR, BETA1, BETA2, EPS, DECAY, case["max_norm"])
+    return s
+
+
+# --------------------------------------------------------------------- run --
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+def _run_own(s):
+    from paper_2607_14672_amd import dstd
+
+    if s["op"] == "norm":
+        return dstd.grad_norm(s["list"], norm=s["norm"], ws=s["ws"])
+    if s["op"] == "clip":
+        return dstd.grad_clip(s["list"], s["max_norm"], norm=s["norm"], ws=s["ws"]), s["out"]
+    norm = s["norm"] if math.isfinite(s["max_norm"]) else None
+    dstd.adamw_step(s["list"], s["hp"], s["step"], lr=s["lr"], norm=norm, ws=s["ws"])
+    return _state(s)
+
+
+def _state(s):
+    out = {k: s[k] for k in ("w", "w32", "m", "v", "step") if k in s}
+    if math.isfinite(s["max_norm"]):
+        out["norm"] = s["norm"]
+    return out
+
+
+def _norm(g):
+    """The norm, its sum over many elements in 64 bits."""
+    return g.square().sum(dtype=torch.float64).sqrt()
+
+
+def _factor(norm, max_norm):
+    return torch.where(torch.isfinite(norm.float()) & (norm > max_norm), max_norm / norm,
+                       torch.ones_like(norm)).float()
+
+
+def _run_plain(s):
+    g = s["g"].float()
+    if s["op"] == "norm":
+        return _norm(g).float().reshape(1)
+    if s["op"] == "clip":
+        norm = _norm(g)
+        return norm.float().reshape(1), (g * _factor(norm, s["max_norm"])).to(s["out"].dtype)
+    ok = None
+    if math.isfinite(s["max_norm"]):
+        norm = _norm(g)
+        g = g * _factor(norm, s["max_norm"])
+        s["norm"] = norm.float().reshape(1)
+        ok = torch.isfinite(s["norm"])
+    t = s["step"] + 1
+    # 1 - beta^t in 64 bits: it is small in the first steps
+    c1 = 1.0 - torch.pow(torch.full_like(t, BETA1, dtype=torch.float64), t)
+    c2 = 1.0 - torch.pow(torch.full_like(t, BETA2, dtype=torch.float64), t)
+    w = s["w32"] if s["master"] else s["w"].float()
+    m = BETA1 * s["m"] + (1.0 - BETA1) * g
+    v = BETA2 * s["v"] + (1.0 - BETA2) * (g * g)
+    step = (m / c1.float()) / ((v / c2.float()).sqrt() + EPS)
+    new = w - s["lr"] * (step + DECAY * w)
+    if ok is not None:  # a step whose norm is not finite changes nothing
+        m, v, new = (torch.where(ok, a, b) for a, b in ((m, s["m"]), (v, s["v"]), (new, w)))
+        t = torch.where(ok, t, s["step"])
+    s["m"], s["v"], s["step"] = m, v, t
+    if s["master"]:
+        s["w32"] = new
+    s["w"] = new.to(s["w"].dtype)
+    return _state(s)
+
+
+# ------------------------------------------------------------------ floors --
+def work(case):
+    n = float(sum(_sizes(case)))
+    b = {"f32": 4, "bf16": 2}
+    if case["op"] == "norm":
+        return {"bytes": b[case["g"]] * n, "flops": 2 * n}
+    if case["op"] == "clip":
+        return {"bytes": (b[case["g"]] + b[case["o"]]) * n, "flops": 3 * n}
+    weight = 4 + 4 + 2 if case["master"] else 2 * b[case["w"]]
+    return {"bytes": (b[case["g"]] + 16 + weight) * n,
+            "flops": (14 if math.isfinite(case["max_norm"]) else 12) * n}
+
+
+# ------------------------------------------------- the same in 64 bits ----
+def exact(case, seed):
+    """Tensor by tensor, from the definitions, every value in 64 bits."""
+    a = _inputs(case, seed)
+    slots, total = _slots(case)
+    squares = [torch.dot(x, x) for x in (a["g"][p:p + n].double() for p, n in slots)]
+    norm = math.sqrt(math.fsum(torch.stack(squares).tolist()))
+    shown = torch.full((1,), norm, dtype=torch.float64, device=_dev())
+    if case["op"] == "norm":
+        return shown
+    c = min(1.0, case["max_norm"] / norm) if norm > 0.0 else 1.0
+    if case["op"] == "clip":
+        out = torch.zeros(total, dtype=torch.float64, device=_dev())
+        for p, n in slots:
+            out[p:p + n] = a["g"][p:p + n].double().mul_(c)
+        return shown, out
+    t = DONE + 1
+    res = {k: torch.zeros(total, dtype=torch.float64, device=_dev()) for k in ("w", "m", "v")}
+    for p, n in slots:
+        g, m, v = (a[k][p:p + n].double() for k in ("g", "m", "v"))
+        w = a["w32" if case["master"] else "w"][p:p + n].double()
+        g = g * c
+        m = m + (1.0 - BETA1) * (g - m)
+        v = v + (1.0 - BETA2) * (g * g - v)
+        m_hat, v_hat = m / -math.expm1(t * math.log(BETA1)), v / -math.expm1(t * math.log(BETA2))
+        w = w * (1.0 - LR * DECAY) - LR * m_hat / (v_hat.sqrt() + EPS)
+        res["w"][p:p + n], res["m"][p:p + n], res["v"][p:p + n] = w, m, v
+    if case["master"]:
+        res["w32"] = res["w"]
+    res["step"] = torch.full((1,), t, dtype=torch.int64, device=_dev())
+    if math.isfinite(case["max_norm"]):
+        res["norm"] = shown
+    return res
