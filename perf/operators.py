@@ -172,7 +172,7 @@ def prepare(case, seed):
         slots, _ = _slots(case)
 
         def tensors(key):
-            return [s[key][a:a + n] for a, n in slots] if key in s else None
+            return [s[key][a:a + n] for a, n in slots] if torch.is_tensor(s.get(key)) else None
 
         s["list"] = dstd.make_tensor_list(tensors("g"), weights=tensors("w"), m=tensors("m"),
                                           v=tensors("v"), master=tensors("w32"), out=tensors("out"))
