@@ -509,6 +509,116 @@ dstd_status dstd_exact_backward(const dstd_lif_params *p, int64_t B, int64_t N_i
                                 const float *grad_t_out, float *grad_W, float *grad_t_in,
                                 void *ws, size_t ws_bytes, void *stream);
 
+/* ----------------------------------------------------------- optimising -- */
+
+/*
+ * What follows the gradients in a training step: the global norm over all
+ * gradient tensors, clipping by it, and the AdamW update (App. C.1 trains with
+ * AdamW). The calls work on a list of tensors, one launch for all of them.
+ *
+ * One tensor of a list; its arrays hold n elements each, dense, in the same
+ * order, and need no more alignment than their type has.
+ *  g           gradient, fp32 or bf16 (g_dtype).
+ *  out         where dstd_grad_clip writes the clipped gradient, fp32 or bf16
+ *              (out_dtype); NULL or g (of the same type) = in place.
+ *  w           weights, fp32 or bf16 (w_dtype), or NULL in a list of gradients
+ *              alone, which dstd_adamw_step does not take.
+ *  w32         fp32 copy of bf16 weights, or NULL. With it an AdamW step
+ *              updates w32 and writes w as its rounding; without it the step
+ *              is added to the widened w and rounded (to nearest even), so
+ *              changes below half a bf16 step are lost.
+ *  m, v        first and second moments; required with w, NULL without.
+ *  lr_scale, decay_scale  factors of the learning rate and the weight decay
+ *              for this tensor, finite and >= 0 (1 = the step's own).
+ */
+typedef struct {
+    void *g, *out, *w;
+    float *w32, *m, *v;
+    int64_t n;
+    int32_t g_dtype, out_dtype, w_dtype;
+    float lr_scale, decay_scale;
+} dstd_tensor;
+
+/*
+ * A list as the calls take it: filled by dstd_tensor_list_build, not changed
+ * by the caller. `mem` is the caller's device memory that holds the table.
+ */
+typedef struct {
+    const void *mem;
+    int64_t n_tensors, n_chunks, n_elems;
+    uint32_t magic, has_weights;
+} dstd_tensor_list;
+
+/* Bytes of device memory that a list of these tensors needs (only their n
+   counts); 0 for invalid arguments (the build then reports the error). */
+size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
+
+/*
+ * Writes the table of `tensors` (host array) to mem (256-byte aligned) on
+ * `stream` and fills *list. The host array may go once the call returns; mem
+ * and the tensors have to stay while the list is used, and a call on another
+ * stream has to be ordered behind the build. A tensor that moves needs a new
+ * build. n_tensors and any n may be 0; n < 2^40 and fewer than 2^31 chunks
+ * of 4096 elements in all. Arrays of one list must not overlap (out = g
+ * apart): DSTD_ERR_PARAM.
+ */
+dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
+                                   size_t mem_bytes, dstd_tensor_list *list, void *stream);
+
+/* Workspace bytes of dstd_grad_norm, dstd_grad_clip and dstd_adamw_step;
+   0 for a list that no build has filled. */
+size_t dstd_tensor_list_workspace_size(const dstd_tensor_list *list);
+
+/*
+ * norm [1] out: the L2 norm of all gradients of the list together, the sum of
+ * squares in 64 bits (no overflow or underflow for any fp32 gradients), the
+ * norm rounded to fp32. 0 for an empty list; NaN or inf as the gradients have
+ * them.
+ */
+dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, size_t ws_bytes,
+                           void *stream);
+
+/*
+ * Clips the gradients to a norm of at most max_norm (> 0 or +INFINITY):
+ * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c rounded
+ * to fp32 once, each product once to its type). A norm that is not finite
+ * clips nothing (c = 1).
+ *  norm [1]   norm_given = 0: out, the norm before clipping, or NULL;
+ *             norm_given = 1: in, the norm to clip by, for gradients that are
+ *             spread over several lists or ranks (their squared norms added);
+ *             the call then sums nothing.
+ */
+dstd_status dstd_grad_clip(const dstd_tensor_list *list, double max_norm, float *norm,
+                           int32_t norm_given, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * AdamW's constants: 0 <= beta < 1, eps > 0 (not 0 in fp32), lr and
+ * weight_decay finite and >= 0, max_norm > 0 or +INFINITY
+ * (DSTD_ERR_PARAM otherwise).
+ */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, max_norm;
+} dstd_adamw_params;
+
+/*
+ * One AdamW step of every tensor of the list, with t = step + 1:
+ *   g' = c g                    (c as in dstd_grad_clip; g itself is only read)
+ *   m  = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *   w  = w - lr lr_scale (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ *                         + weight_decay decay_scale w)
+ * in fp32 (the powers in 64 bits).
+ *  lr [1]     learning rate on the device, for schedules under a captured
+ *             graph, or NULL: p->lr.
+ *  step [1]   in/out, on the device: steps done (>= 0).
+ *  norm [1]   as in dstd_grad_clip. The norm is summed if norm is not NULL or
+ *             max_norm is finite; a step whose norm is then not finite leaves
+ *             w, w32, m, v and step as they were. With norm = NULL and
+ *             max_norm = +INFINITY no norm is formed and every step is made.
+ */
+dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_params *p,
+                            const float *lr, int64_t *step, float *norm, int32_t norm_given,
+                            void *ws, size_t ws_bytes, void *stream);
+
 /* ----------------------------------------------------------------- misc -- */
 
 const char *dstd_status_string(dstd_status s);

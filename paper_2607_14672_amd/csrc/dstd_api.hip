@@ -8,7 +8,9 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <mutex>
+#include <vector>
 
 #include "../../include/dstd_lif.h"
 #include "dstd_internal.h"
@@ -396,7 +398,7 @@ const char *dstd_status_string(dstd_status s) {
 
 const char *dstd_last_error(void) { return g_err; }
 
-int32_t dstd_version(void) { return 100; }
+int32_t dstd_version(void) { return 101; }
 
 size_t dstd_lif_forward_workspace_size(const dstd_lif_params *p, int64_t B, int64_t N_in,
                                        int64_t N_out) {
@@ -1032,6 +1034,259 @@ dstd_status dstd_lif_multispike_backward(const dstd_lif_params *p, int64_t B, in
                                             bw, t_in, t_out, slope, q_idx, cur, grad_t_out, grad_W,
                                             grad_t_in, static_cast<hipStream_t>(stream));
     return hip_status(e, "multi-spike backward launch");
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------- optimising --
+namespace {
+
+constexpr uint32_t kListMagic = 0x4c545344;
+
+dstd_status check_dtype(int32_t t, const char *what) {
+    if (t != DSTD_F32 && t != DSTD_BF16) return fail(DSTD_ERR_PARAM, "unknown %s dtype %d", what, (int)t);
+    return DSTD_OK;
+}
+
+int64_t dtype_bytes(int32_t t) { return t == DSTD_BF16 ? 2 : 4; }
+
+// chunks of the whole list, in *n_chunks
+dstd_status check_counts(int64_t n, const dstd_tensor *t, int64_t *n_chunks, int64_t *n_elems) {
+    if (n < 0) return fail(DSTD_ERR_SHAPE, "n_tensors must be >= 0");
+    if (n > 0 && !t) return fail(DSTD_ERR_NULL, "tensors is NULL");
+    const int64_t lim = (int64_t)1 << 31;
+    if (n >= lim) return fail(DSTD_ERR_SHAPE, "too many tensors");
+    int64_t c = 0, e = 0;
+    for (int64_t k = 0; k < n; ++k) {
+        if (t[k].n < 0 || t[k].n >= (int64_t)1 << 40)
+            return fail(DSTD_ERR_SHAPE, "tensor %lld: n = %lld must be in [0, 2^40)", (long long)k,
+                        (long long)t[k].n);
+        c += (t[k].n + dstd::kOptChunk - 1) / dstd::kOptChunk;
+        e += t[k].n;
+        if (c >= lim) return fail(DSTD_ERR_SHAPE, "the list's tensors are too large together");
+    }
+    *n_chunks = c;
+    *n_elems = e;
+    return DSTD_OK;
+}
+
+size_t list_tensors_bytes(int64_t n) { return align_up((size_t)n * sizeof(dstd::OptTensor)); }
+size_t list_bytes(int64_t n, int64_t n_chunks) {
+    return std::max(kAlign, list_tensors_bytes(n) + align_up((size_t)n_chunks * sizeof(dstd::OptChunk)));
+}
+
+struct Range { uintptr_t lo, hi; int64_t k; };
+
+dstd_status add_range(std::vector<Range> &r, const void *p, int64_t n, int64_t bytes, int64_t k,
+                      const char *what) {
+    const uintptr_t a = (uintptr_t)p;
+    if (a % (uintptr_t)bytes != 0)
+        return fail(DSTD_ERR_PARAM, "tensor %lld: %s is not aligned to its type", (long long)k, what);
+    if (n > 0) r.push_back(Range{a, a + (uintptr_t)(n * bytes), k});
+    return DSTD_OK;
+}
+
+dstd_status check_tensor(const dstd_tensor &t, int64_t k, std::vector<Range> &r) {
+    dstd_status s;
+    if (t.n == 0) return DSTD_OK;
+    if (!t.g) return fail(DSTD_ERR_NULL, "tensor %lld: g is NULL", (long long)k);
+    if ((s = check_dtype(t.g_dtype, "gradient")) != DSTD_OK) return s;
+    if ((s = add_range(r, t.g, t.n, dtype_bytes(t.g_dtype), k, "g")) != DSTD_OK) return s;
+    if (t.out) {
+        if ((s = check_dtype(t.out_dtype, "out")) != DSTD_OK) return s;
+        if (t.out == t.g && t.out_dtype != t.g_dtype)
+            return fail(DSTD_ERR_PARAM, "tensor %lld: in place, out has the type of g", (long long)k);
+        if (t.out != t.g &&
+            (s = add_range(r, t.out, t.n, dtype_bytes(t.out_dtype), k, "out")) != DSTD_OK)
+            return s;
+    }
+    if (!t.w) {
+        if (t.w32 || t.m || t.v)
+            return fail(DSTD_ERR_NULL, "tensor %lld: w32, m and v go with w", (long long)k);
+        return DSTD_OK;
+    }
+    if (!t.m || !t.v) return fail(DSTD_ERR_NULL, "tensor %lld: m and v are required with w", (long long)k);
+    if ((s = check_dtype(t.w_dtype, "weight")) != DSTD_OK) return s;
+    if (t.w32 && t.w_dtype != DSTD_BF16)
+        return fail(DSTD_ERR_PARAM, "tensor %lld: w32 goes with bf16 weights", (long long)k);
+    if (!(isfinite(t.lr_scale) && t.lr_scale >= 0.f && isfinite(t.decay_scale) && t.decay_scale >= 0.f))
+        return fail(DSTD_ERR_PARAM, "tensor %lld: lr_scale and decay_scale must be finite and >= 0",
+                    (long long)k);
+    if ((s = add_range(r, t.w, t.n, dtype_bytes(t.w_dtype), k, "w")) != DSTD_OK) return s;
+    if (t.w32 && (s = add_range(r, t.w32, t.n, 4, k, "w32")) != DSTD_OK) return s;
+    if ((s = add_range(r, t.m, t.n, 4, k, "m")) != DSTD_OK) return s;
+    return add_range(r, t.v, t.n, 4, k, "v");
+}
+
+dstd_status check_list(const dstd_tensor_list *l) {
+    if (!l) return fail(DSTD_ERR_NULL, "list is NULL");
+    if (l->magic != kListMagic || !l->mem || l->n_tensors < 0 || l->n_chunks < 0 ||
+        l->n_chunks >= (int64_t)1 << 31)
+        return fail(DSTD_ERR_PARAM, "not a list that dstd_tensor_list_build has filled");
+    return DSTD_OK;
+}
+
+struct OptWs {
+    size_t part, at, total;
+};
+OptWs opt_ws_layout() {
+    OptWs w{};
+    w.part = 0;
+    w.at = align_up(dstd::kOptMaxPart * sizeof(double));
+    w.total = w.at + align_up(sizeof(dstd::OptStep));
+    return w;
+}
+
+dstd::OptList opt_list(const dstd_tensor_list *l) {
+    const char *mem = static_cast<const char *>(l->mem);
+    return dstd::OptList{reinterpret_cast<const dstd::OptTensor *>(mem),
+                         reinterpret_cast<const dstd::OptChunk *>(mem + list_tensors_bytes(l->n_tensors)),
+                         (int)l->n_chunks};
+}
+
+dstd_status check_max_norm(double max_norm) {
+    if (!(max_norm > 0.0)) return fail(DSTD_ERR_PARAM, "max_norm must be > 0 or +inf (got %g)", max_norm);
+    return DSTD_OK;
+}
+
+dstd_status check_norm(const float *norm, int32_t norm_given) {
+    if (norm_given != 0 && norm_given != 1) return fail(DSTD_ERR_PARAM, "norm_given must be 0 or 1");
+    if (norm_given && !norm) return fail(DSTD_ERR_NULL, "norm is NULL but said to be given");
+    return DSTD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors) {
+    int64_t nc, ne;
+    if (check_counts(n_tensors, tensors, &nc, &ne) != DSTD_OK) return 0;
+    return list_bytes(n_tensors, nc);
+}
+
+dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
+                                   size_t mem_bytes, dstd_tensor_list *list, void *stream) try {
+    int64_t nc, ne;
+    dstd_status s = check_counts(n_tensors, tensors, &nc, &ne);
+    if (s != DSTD_OK) return s;
+    if (!list) return fail(DSTD_ERR_NULL, "list is NULL");
+    const size_t need = list_bytes(n_tensors, nc);
+    std::vector<Range> ranges;
+    ranges.reserve((size_t)n_tensors * 6 + 1);
+    uint32_t has_weights = 1;
+    for (int64_t k = 0; k < n_tensors; ++k) {
+        if ((s = check_tensor(tensors[k], k, ranges)) != DSTD_OK) return s;
+        if (tensors[k].n > 0 && !tensors[k].w) has_weights = 0;
+    }
+    if ((s = check_ws(mem, mem_bytes, need)) != DSTD_OK) return s;
+    ranges.push_back(Range{(uintptr_t)mem, (uintptr_t)mem + need, -1});
+    std::sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
+    for (size_t i = 1; i < ranges.size(); ++i)
+        if (ranges[i].lo < ranges[i - 1].hi)
+            return fail(DSTD_ERR_PARAM, "arrays of tensors %lld and %lld overlap (-1: the list's own memory)",
+                        (long long)ranges[i - 1].k, (long long)ranges[i].k);
+    auto *ten = static_cast<dstd::OptTensor *>(mem);
+    auto *chunks = at<dstd::OptChunk>(mem, list_tensors_bytes(n_tensors));
+    int64_t c = 0;
+    for (int64_t k0 = 0; k0 < n_tensors; k0 += dstd::kOptBatch) {
+        const int count = (int)std::min<int64_t>(dstd::kOptBatch, n_tensors - k0);
+        dstd::OptBatch b{};
+        b.first = (int32_t)k0;
+        for (int i = 0; i < count; ++i) {
+            const dstd_tensor &t = tensors[k0 + i];
+            dstd::OptTensor &o = b.ten[i];
+            o.g = t.g;
+            o.out = t.out ? t.out : t.g;
+            o.w = t.w;
+            o.w32 = t.w32;
+            o.m = t.m;
+            o.v = t.v;
+            o.lr_scale = t.lr_scale;
+            o.decay_scale = t.decay_scale;
+            o.types = (t.g_dtype == DSTD_BF16 ? dstd::kOptGradBf16 : 0) |
+                      ((t.out ? t.out_dtype : t.g_dtype) == DSTD_BF16 ? dstd::kOptOutBf16 : 0) |
+                      (t.w_dtype == DSTD_BF16 ? dstd::kOptWeightBf16 : 0);
+            b.n[i] = t.n;
+            b.chunk0[i] = c;
+            c += (t.n + dstd::kOptChunk - 1) / dstd::kOptChunk;
+        }
+        hipError_t e = dstd::launch_tensor_list(b, count, ten, chunks, static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return hip_status(e, "tensor list launch");
+    }
+    *list = dstd_tensor_list{mem, n_tensors, nc, ne, kListMagic, has_weights};
+    return DSTD_OK;
+} catch (const std::exception &e) {
+    return fail(DSTD_ERR_UNSUPPORTED, "tensor list: %s", e.what());
+}
+
+size_t dstd_tensor_list_workspace_size(const dstd_tensor_list *list) {
+    if (check_list(list) != DSTD_OK) return 0;
+    return opt_ws_layout().total;
+}
+
+dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, size_t ws_bytes,
+                           void *stream) {
+    dstd_status s = check_list(list);
+    if (s != DSTD_OK) return s;
+    if (!norm) return fail(DSTD_ERR_NULL, "norm is NULL");
+    const OptWs w = opt_ws_layout();
+    if ((s = check_ws(ws, ws_bytes, w.total)) != DSTD_OK) return s;
+    const dstd::OptList L = opt_list(list);
+    const dstd::OptNorm nm{at<double>(ws, w.part), dstd::opt_norm_blocks(L.n_chunks), norm, INFINITY};
+    return hip_status(dstd::launch_grad_norm(L, nm, static_cast<hipStream_t>(stream)), "grad_norm launch");
+}
+
+dstd_status dstd_grad_clip(const dstd_tensor_list *list, double max_norm, float *norm,
+                           int32_t norm_given, void *ws, size_t ws_bytes, void *stream) {
+    dstd_status s = check_list(list);
+    if (s != DSTD_OK) return s;
+    if ((s = check_max_norm(max_norm)) != DSTD_OK) return s;
+    if ((s = check_norm(norm, norm_given)) != DSTD_OK) return s;
+    const OptWs w = opt_ws_layout();
+    if ((s = check_ws(ws, ws_bytes, w.total)) != DSTD_OK) return s;
+    const dstd::OptList L = opt_list(list);
+    const dstd::OptNorm nm{at<double>(ws, w.part), norm_given ? -1 : dstd::opt_norm_blocks(L.n_chunks),
+                           norm, max_norm};
+    return hip_status(dstd::launch_grad_clip(L, nm, static_cast<hipStream_t>(stream)), "grad_clip launch");
+}
+
+dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_params *p,
+                            const float *lr, int64_t *step, float *norm, int32_t norm_given,
+                            void *ws, size_t ws_bytes, void *stream) {
+    dstd_status s = check_list(list);
+    if (s != DSTD_OK) return s;
+    if (!p) return fail(DSTD_ERR_NULL, "params is NULL");
+    if (!(isfinite(p->lr) && p->lr >= 0.0)) return fail(DSTD_ERR_PARAM, "lr must be finite and >= 0");
+    if (!(p->beta1 >= 0.0 && p->beta1 < 1.0 && p->beta2 >= 0.0 && p->beta2 < 1.0))
+        return fail(DSTD_ERR_PARAM, "need 0 <= beta1, beta2 < 1");
+    if (!(isfinite((float)p->eps) && (float)p->eps > 0.f))
+        return fail(DSTD_ERR_PARAM, "eps must be finite and > 0 in fp32");
+    if (!(isfinite(p->weight_decay) && p->weight_decay >= 0.0))
+        return fail(DSTD_ERR_PARAM, "weight_decay must be finite and >= 0");
+    if ((s = check_max_norm(p->max_norm)) != DSTD_OK) return s;
+    if ((s = check_norm(norm, norm_given)) != DSTD_OK) return s;
+    if (!step) return fail(DSTD_ERR_NULL, "step is NULL");
+    if (!list->has_weights)
+        return fail(DSTD_ERR_NULL, "a tensor of the list has no weights");
+    const OptWs w = opt_ws_layout();
+    if ((s = check_ws(ws, ws_bytes, w.total)) != DSTD_OK) return s;
+    const dstd::OptList L = opt_list(list);
+    const bool sums = !norm_given && (norm || isfinite(p->max_norm));
+    const dstd::OptNorm nm{at<double>(ws, w.part), sums ? dstd::opt_norm_blocks(L.n_chunks) : -1,
+                           norm, p->max_norm};
+    dstd::OptAdamW hp{};
+    hp.beta1 = p->beta1;
+    hp.beta2 = p->beta2;
+    hp.b1 = (float)p->beta1;
+    hp.b2 = (float)p->beta2;
+    hp.a1 = (float)(1.0 - p->beta1);
+    hp.a2 = (float)(1.0 - p->beta2);
+    hp.eps = (float)p->eps;
+    hp.lr = (float)p->lr;
+    hp.decay = (float)p->weight_decay;
+    return hip_status(dstd::launch_adamw(L, nm, hp, lr, step, at<dstd::OptStep>(ws, w.at),
+                                         static_cast<hipStream_t>(stream)), "adamw launch");
 }
 
 }  // extern "C"

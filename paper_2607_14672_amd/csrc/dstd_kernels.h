@@ -247,4 +247,59 @@ hipError_t launch_exact_backward(const LifConst &C, int64_t B, int64_t N_in, int
                                  const float *grad_t, float4 *P, float4 *PT, float *grad_W,
                                  float *grad_t_in, hipStream_t st);
 
+// ----------------------------------------------------------------- optim --
+// Tensor lists, the global gradient norm, clipping and AdamW (dstd_optim.hip).
+// A list's device memory: its tensors, then its chunks of at most kOptChunk
+// elements in tensor order (empty tensors have none).
+constexpr int64_t kOptChunk = 4096;
+constexpr int kOptMaxPart = 1024;  // partial sums of squares of one norm
+enum OptTypes : uint32_t { kOptGradBf16 = 1, kOptOutBf16 = 2, kOptWeightBf16 = 4 };
+struct OptTensor {
+    void *g, *out, *w;
+    float *w32, *m, *v;
+    float lr_scale, decay_scale;
+    uint32_t types, pad;
+};
+struct OptChunk {
+    int32_t tensor, count;
+    int64_t start;
+};
+struct OptList {
+    const OptTensor *ten;
+    const OptChunk *chunks;
+    int n_chunks;
+};
+// A batch of tensors as kernel arguments (at most 4 KB in all).
+constexpr int kOptBatch = 48;
+struct OptBatch {
+    OptTensor ten[kOptBatch];
+    int64_t n[kOptBatch], chunk0[kOptBatch];
+    int32_t first;
+};
+// The norm of a call: n_part partial sums of squares, or n_part = -1 where it
+// is given in *norm, or not asked for (norm null).
+struct OptNorm {
+    double *part;
+    int n_part;
+    float *norm;
+    double max_norm;
+};
+// What an AdamW step reads of its step number t.
+struct OptStep {
+    int64_t t;
+    float inv_c1, inv_c2;  // 1 / (1 - beta^t)
+};
+struct OptAdamW {
+    double beta1, beta2;
+    float b1, b2, a1, a2;  // betas and 1 - beta
+    float eps, lr, decay;
+};
+int opt_norm_blocks(int n_chunks);
+hipError_t launch_tensor_list(const OptBatch &b, int count, OptTensor *ten, OptChunk *chunks,
+                              hipStream_t st);
+hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st);
+hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st);
+hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp, const float *lr,
+                        int64_t *step, OptStep *at, hipStream_t st);
+
 }  // namespace dstd

@@ -50,6 +50,21 @@ class dstd_synfire_params(C.Structure):
                                          "scale")]
 
 
+class dstd_tensor(C.Structure):
+    _fields_ = ([(k, C.c_void_p) for k in ("g", "out", "w", "w32", "m", "v")] + [("n", C.c_int64)] +
+                [(k, C.c_int32) for k in ("g_dtype", "out_dtype", "w_dtype")] +
+                [(k, C.c_float) for k in ("lr_scale", "decay_scale")])
+
+
+class dstd_tensor_list(C.Structure):
+    _fields_ = [("mem", C.c_void_p), ("n_tensors", C.c_int64), ("n_chunks", C.c_int64),
+                ("n_elems", C.c_int64), ("magic", C.c_uint32), ("has_weights", C.c_uint32)]
+
+
+class dstd_adamw_params(C.Structure):
+    _fields_ = [(k, C.c_double) for k in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")]
+
+
 class DSTDError(RuntimeError):
     def __init__(self, fn: str, status: int):
         lib = _load()
@@ -65,6 +80,7 @@ _L = C.c_int64
 _S = C.c_size_t
 _I = C.c_int
 _F = C.c_float
+_D = C.c_double
 
 # name -> (restype, argtypes)
 _SIGS = {
@@ -97,6 +113,12 @@ _SIGS = {
     "dstd_skip_delay_concat_backward": (_I, [_L, _L, _L, _L, _P, _P, C.c_int32, _P, _P]),
     "dstd_softmax_ce_grad": (_I, [_L, _L, _P, _P, _F, _F, _P, _P, _P]),
     "dstd_mse_grad": (_I, [_L, _L, _P, _P, _P, _P, _P]),
+    "dstd_tensor_list_size": (_S, [_L, _P]),
+    "dstd_tensor_list_build": (_I, [_L, _P, _P, _S, _P, _P]),
+    "dstd_tensor_list_workspace_size": (_S, [_P]),
+    "dstd_grad_norm": (_I, [_P, _P, _P, _S, _P]),
+    "dstd_grad_clip": (_I, [_P, _D, _P, C.c_int32, _P, _S, _P]),
+    "dstd_adamw_step": (_I, [_P, _P, _P, _P, _P, C.c_int32, _P, _S, _P]),
     "dstd_profile_enable": (C.c_int32, [C.c_int32]),
     "dstd_profile_collect": (_I, []),
     "dstd_profile_count": (C.c_int32, []),
@@ -255,6 +277,31 @@ def dstd_softmax_ce_grad(B, N, t_out, labels, tau_soft, t_cap, grad_t, loss, str
 
 def dstd_mse_grad(B, N, t_out, target, grad_t, loss, stream):
     return _load().dstd_mse_grad(B, N, t_out, target, grad_t, loss, stream)
+
+
+def dstd_tensor_list_size(n_tensors, tensors):
+    return _load().dstd_tensor_list_size(n_tensors, _ref(tensors))
+
+
+def dstd_tensor_list_build(n_tensors, tensors, mem, mem_bytes, lst, stream):
+    return _load().dstd_tensor_list_build(n_tensors, _ref(tensors), mem, mem_bytes, _ref(lst), stream)
+
+
+def dstd_tensor_list_workspace_size(lst):
+    return _load().dstd_tensor_list_workspace_size(_ref(lst))
+
+
+def dstd_grad_norm(lst, norm, ws, ws_bytes, stream):
+    return _load().dstd_grad_norm(_ref(lst), norm, ws, ws_bytes, stream)
+
+
+def dstd_grad_clip(lst, max_norm, norm, norm_given, ws, ws_bytes, stream):
+    return _load().dstd_grad_clip(_ref(lst), max_norm, norm, norm_given, ws, ws_bytes, stream)
+
+
+def dstd_adamw_step(lst, p, lr, step, norm, norm_given, ws, ws_bytes, stream):
+    return _load().dstd_adamw_step(_ref(lst), _ref(p), lr, step, norm, norm_given, ws, ws_bytes,
+                                   stream)
 
 
 def dstd_status_string(s):
@@ -657,3 +704,144 @@ def mse_grad(t_out, target):
     _check("dstd_mse_grad", dstd_mse_grad(B, N, _ptr(t_out), _ptr(target), _ptr(grad), _ptr(loss),
                                           _stream(t_out.device)))
     return grad, loss
+
+
+class TensorList:
+    """The tensors of a training step and their table on the device (``c``: the
+    C struct). It keeps the tensors and the table alive; a tensor that is
+    replaced by another needs a new list."""
+
+    def __init__(self, c, mem, tensors, device):
+        self.c, self.mem, self.tensors, self.device = c, mem, tensors, device
+
+
+def _list_array(x, like, dev, dtypes, what):
+    torch = _torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
+    if x.dtype not in dtypes:
+        raise TypeError(f"{what} must be one of {dtypes}, got {x.dtype}")
+    if not x.is_cuda or x.device != dev:
+        raise ValueError(f"{what} must live on the GPU of the list's other tensors")
+    if x.shape != like.shape:
+        raise ValueError(f"{what} has shape {tuple(x.shape)}, its gradient {tuple(like.shape)}")
+    if not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return x.data_ptr()
+
+
+def _per_tensor(x, n, what):
+    x = [None] * n if x is None else list(x)
+    if len(x) != n:
+        raise ValueError(f"{len(x)} {what} for {n} gradients")
+    return x
+
+
+def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None, lr_scale=None,
+                     decay_scale=None) -> TensorList:
+    """List of tensors for grad_norm, grad_clip and adamw_step. `grads` f32 or
+    bf16; `weights` f32 or bf16 with their moments `m`, `v` (f32), and for bf16
+    weights optionally their f32 copies `master`; `out` the tensors grad_clip
+    writes (default: the gradients themselves); `lr_scale`, `decay_scale`
+    factors per tensor (default 1). All contiguous, on one GPU; entries of
+    master and out may be None."""
+    torch = _torch()
+    both = (torch.float32, torch.bfloat16)
+    f32 = (torch.float32,)
+    grads = list(grads)
+    n = len(grads)
+    cols = [_per_tensor(x, n, what) for x, what in
+            ((weights, "weights"), (m, "first moments"), (v, "second moments"),
+             (master, "master weights"), (out, "outputs"))]
+    scales = [[1.0] * n if x is None else _per_tensor(x, n, what) for x, what in
+              ((lr_scale, "learning-rate factors"), (decay_scale, "decay factors"))]
+    if n == 0:
+        raise ValueError("a list needs a tensor")
+    dev = getattr(grads[0], "device", None)
+    arr = (dstd_tensor * n)()
+    for k, (t, g) in enumerate(zip(arr, grads)):
+        t.g = _list_array(g, g, dev, both, f"gradient {k}")
+        t.g_dtype, t.n = _wdtype(g), g.numel()
+        w, mk, vk, w32, o = (c[k] for c in cols)
+        if w is not None:
+            t.w, t.w_dtype = _list_array(w, g, dev, both, f"weight {k}"), _wdtype(w)
+        if mk is not None:
+            t.m = _list_array(mk, g, dev, f32, f"first moment {k}")
+        if vk is not None:
+            t.v = _list_array(vk, g, dev, f32, f"second moment {k}")
+        if w32 is not None:
+            t.w32 = _list_array(w32, g, dev, f32, f"master weight {k}")
+        if o is not None:
+            t.out, t.out_dtype = _list_array(o, g, dev, both, f"output {k}"), _wdtype(o)
+        t.lr_scale, t.decay_scale = (float(s[k]) for s in scales)
+    mem = workspace(dstd_tensor_list_size(n, arr), dev)
+    c = dstd_tensor_list()
+    with torch.cuda.device(dev):
+        _check("dstd_tensor_list_build",
+               dstd_tensor_list_build(n, arr, _ptr(mem), mem.numel(), c, _stream(dev)))
+    return TensorList(c, mem, (grads, *cols), dev)
+
+
+def _scalar(x, dtype, dev, what):
+    if x.dtype != dtype or x.numel() != 1 or x.device != dev:
+        raise ValueError(f"{what} must hold one {dtype} on {dev}")
+    return x.data_ptr()
+
+
+def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
+    """(norm tensor or None, its pointer, workspace) of a call."""
+    torch = _torch()
+    if norm is None:
+        if norm_given:
+            raise ValueError("norm_given needs the norm")
+        if want_norm:
+            norm = torch.empty(1, dtype=torch.float32, device=tl.device)
+    need = dstd_tensor_list_workspace_size(tl.c)
+    if ws is None or ws.numel() < need:
+        ws = workspace(need, tl.device)
+    return norm, None if norm is None else _scalar(norm, torch.float32, tl.device, "norm"), ws
+
+
+def grad_norm(tl: TensorList, norm=None, ws=None):
+    """L2 norm of all gradients of the list together, as a device tensor [1]
+    (written to `norm` if given)."""
+    norm, ptr, ws = _optim_args(tl, norm, False, ws, True)
+    with _torch().cuda.device(tl.device):
+        _check("dstd_grad_norm",
+               dstd_grad_norm(tl.c, ptr, _ptr(ws), ws.numel(), _stream(tl.device)))
+    return norm
+
+
+def grad_clip(tl: TensorList, max_norm: float, norm=None, norm_given: bool = False, ws=None):
+    """Clips the list's gradients to a norm of at most max_norm, in place or
+    into the list's outputs; returns the norm before clipping, a device tensor
+    [1]. With norm_given, `norm` is the norm to clip by."""
+    norm, ptr, ws = _optim_args(tl, norm, norm_given, ws, True)
+    with _torch().cuda.device(tl.device):
+        _check("dstd_grad_clip",
+               dstd_grad_clip(tl.c, float(max_norm), ptr, 1 if norm_given else 0, _ptr(ws),
+                              ws.numel(), _stream(tl.device)))
+    return norm
+
+
+def make_adamw(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=1e-2,
+               max_norm=math.inf) -> dstd_adamw_params:
+    return dstd_adamw_params(float(lr), float(beta1), float(beta2), float(eps),
+                             float(weight_decay), float(max_norm))
+
+
+def adamw_step(tl: TensorList, hp: dstd_adamw_params, step, lr=None, norm=None,
+               norm_given: bool = False, ws=None):
+    """One AdamW step of the list's tensors, their gradients clipped to
+    hp.max_norm on the way. `step` [1] int64: steps done, on the device, counted
+    up; `lr` [1] f32 on the device replaces hp.lr. Returns the norm before
+    clipping (None where none is formed: no `norm` given and hp.max_norm infinite);
+    a step whose norm is not finite changes nothing."""
+    torch = _torch()
+    norm, ptr, ws = _optim_args(tl, norm, norm_given, ws, math.isfinite(hp.max_norm))
+    with torch.cuda.device(tl.device):
+        _check("dstd_adamw_step",
+               dstd_adamw_step(tl.c, hp, None if lr is None else _scalar(lr, torch.float32, tl.device, "lr"),
+                               _scalar(step, torch.int64, tl.device, "step"), ptr,
+                               1 if norm_given else 0, _ptr(ws), ws.numel(), _stream(tl.device)))
+    return norm
