@@ -546,7 +546,8 @@ typedef struct {
 typedef struct {
     const void *mem;
     int64_t n_tensors, n_chunks, n_elems;
-    uint32_t magic, has_weights;
+    int64_t g_bytes, out_bytes, w_bytes;
+    uint32_t magic, has_weights, g_types, reserved;
 } dstd_tensor_list;
 
 /* Bytes of device memory that a list of these tensors needs (only their n

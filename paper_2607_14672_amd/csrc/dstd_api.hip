@@ -1141,7 +1141,8 @@ dstd::OptList opt_list(const dstd_tensor_list *l) {
     const char *mem = static_cast<const char *>(l->mem);
     return dstd::OptList{reinterpret_cast<const dstd::OptTensor *>(mem),
                          reinterpret_cast<const dstd::OptChunk *>(mem + list_tensors_bytes(l->n_tensors)),
-                         (int)l->n_chunks};
+                         (int)l->n_chunks, l->g_bytes, l->out_bytes, l->w_bytes,
+                         l->g_types};
 }
 
 dstd_status check_max_norm(double max_norm) {
@@ -1188,7 +1189,8 @@ dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors
                         (long long)ranges[i - 1].k, (long long)ranges[i].k);
     auto *ten = static_cast<dstd::OptTensor *>(mem);
     auto *chunks = at<dstd::OptChunk>(mem, list_tensors_bytes(n_tensors));
-    int64_t c = 0;
+    int64_t c = 0, gb = 0, ob = 0, wb = 0;
+    uint32_t types = 0;
     for (int64_t k0 = 0; k0 < n_tensors; k0 += dstd::kOptBatch) {
         const int count = (int)std::min<int64_t>(dstd::kOptBatch, n_tensors - k0);
         dstd::OptBatch b{};
@@ -1210,11 +1212,15 @@ dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors
             b.n[i] = t.n;
             b.chunk0[i] = c;
             c += (t.n + dstd::kOptChunk - 1) / dstd::kOptChunk;
+            gb += t.n * dtype_bytes(t.g_dtype);
+            if (t.n > 0) types |= t.g_dtype == DSTD_BF16 ? dstd::kOptListBf16 : dstd::kOptListF32;
+            if (o.out != o.g) ob += t.n * dtype_bytes(t.out_dtype);
+            if (t.w) wb += t.n * (8 + dtype_bytes(t.w_dtype) + (t.w32 ? 4 : 0));
         }
         hipError_t e = dstd::launch_tensor_list(b, count, ten, chunks, static_cast<hipStream_t>(stream));
         if (e != hipSuccess) return hip_status(e, "tensor list launch");
     }
-    *list = dstd_tensor_list{mem, n_tensors, nc, ne, kListMagic, has_weights};
+    *list = dstd_tensor_list{mem, n_tensors, nc, ne, gb, ob, wb, kListMagic, has_weights, types, 0};
     return DSTD_OK;
 } catch (const std::exception &e) {
     return fail(DSTD_ERR_UNSUPPORTED, "tensor list: %s", e.what());

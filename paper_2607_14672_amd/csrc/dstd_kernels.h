@@ -254,6 +254,7 @@ hipError_t launch_exact_backward(const LifConst &C, int64_t B, int64_t N_in, int
 constexpr int64_t kOptChunk = 4096;
 constexpr int kOptMaxPart = 1024;  // partial sums of squares of one norm
 enum OptTypes : uint32_t { kOptGradBf16 = 1, kOptOutBf16 = 2, kOptWeightBf16 = 4 };
+enum OptListTypes : uint32_t { kOptListF32 = 1, kOptListBf16 = 2 };  // of a list's gradients
 struct OptTensor {
     void *g, *out, *w;
     float *w32, *m, *v;
@@ -268,6 +269,9 @@ struct OptList {
     const OptTensor *ten;
     const OptChunk *chunks;
     int n_chunks;
+    // of all gradients; of clipped ones elsewhere; of weights, copies, moments
+    int64_t g_bytes, out_bytes, w_bytes;
+    uint32_t g_types;
 };
 // A batch of tensors as kernel arguments (at most 4 KB in all).
 constexpr int kOptBatch = 48;

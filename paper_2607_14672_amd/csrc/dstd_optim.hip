@@ -44,44 +44,32 @@ __device__ __forceinline__ f32x4 widen(u16x4 h) {
     for (int k = 0; k < 4; ++k) r[k] = bf16_to_f32(h[k]);
     return r;
 }
+__device__ __forceinline__ f32x4 widen(f32x4 v) { return v; }
+template <typename T> struct Vec4;  // four elements of a type
+template <> struct Vec4<gf32> { using type = f32x4; using any = DSTD_GLOBAL f32x4_any; };
+template <> struct Vec4<gu16> { using type = u16x4; using any = DSTD_GLOBAL u16x4_any; };
 
-// Four elements at p as fp32, or the first `left` of them and zeros.
-__device__ __forceinline__ f32x4 load4(const gf32 *p, bool full, int left) {
-    if (full) return *reinterpret_cast<const DSTD_GLOBAL f32x4_any *>(p);
-    f32x4 r = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < left) r[k] = p[k];
-    return r;
+// Four elements at p. NT: marked as an access that nothing repeats soon.
+template <bool NT, typename T>
+__device__ __forceinline__ typename Vec4<T>::type load4(const T *p) {
+    using V = const typename Vec4<T>::any;
+    return NT ? __builtin_nontemporal_load((V *)p) : *(V *)p;
 }
-__device__ __forceinline__ f32x4 load4(const gu16 *p, bool full, int left) {
-    if (full) return widen(*reinterpret_cast<const DSTD_GLOBAL u16x4_any *>(p));
-    u16x4 h = {0, 0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < left) h[k] = p[k];
-    return widen(h);
-}
-
-__device__ __forceinline__ void store4(gf32 *p, f32x4 v, bool full, int left) {
-    if (full) {
-        *reinterpret_cast<DSTD_GLOBAL f32x4_any *>(p) = v;
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < left) p[k] = v[k];
+template <bool NT> __device__ __forceinline__ void store4(gf32 *p, f32x4 v) {
+    if (NT) __builtin_nontemporal_store(v, (DSTD_GLOBAL f32x4_any *)p);
+    else *(DSTD_GLOBAL f32x4_any *)p = v;
 }
 // rounded once, to nearest even
-__device__ __forceinline__ void store4(gu16 *p, f32x4 v, bool full, int left) {
+template <bool NT> __device__ __forceinline__ void store4(gu16 *p, f32x4 v) {
     const u16x4 h = __builtin_bit_cast(u16x4, __builtin_convertvector(v, bf16x4));
-    if (full) {
-        *reinterpret_cast<DSTD_GLOBAL u16x4_any *>(p) = h;
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < left) p[k] = h[k];
+    if (NT) __builtin_nontemporal_store(h, (DSTD_GLOBAL u16x4_any *)p);
+    else *(DSTD_GLOBAL u16x4_any *)p = h;
+}
+__device__ __forceinline__ float load1(const gf32 *p) { return *p; }
+__device__ __forceinline__ float load1(const gu16 *p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void store1(gf32 *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(gu16 *p, float v) {
+    *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
 
 __device__ __forceinline__ gf32 *f32_at(void *p, int64_t start) { return (gf32 *)p + start; }
@@ -102,39 +90,108 @@ __device__ double block_sum(double v, double *sh) {
 
 // Squares are formed and added in 64 bits: the square of an fp32 value is
 // exact there and neither overflows nor underflows.
-template <typename T>
-__device__ __forceinline__ double chunk_squares(const T *g, int count) {
-    double s = 0.0;
-    f32x4 x[kOptGroups];
+__device__ __forceinline__ double add_square(double s, float x) {
+    const double y = x;
+    return fma(y, y, s);
+}
+
+// A thread's vectors of four elements of a gradient chunk, zeros past the last
+// whole one. As read: they are widened where they are used, for a conversion
+// next to the loads would wait for them before the next chunk's are issued.
+template <typename T> struct Share {
+    typename Vec4<T>::type x[kOptGroups];
+};
+template <bool NT, typename T>
+__device__ __forceinline__ void read_share(Share<T> &r, const T *g, int count) {
+    const int n4 = count / 4, tid = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i) {
-        const int e = (i * kOptThreads + threadIdx.x) * 4;
-        x[i] = (e < count) ? load4(g + e, e + 4 <= count, count - e) : f32x4{0.f, 0.f, 0.f, 0.f};
+        r.x[i] = typename Vec4<T>::type{0, 0, 0, 0};
+        if (i * kOptThreads + tid < n4) r.x[i] = load4<NT>(g + (i * kOptThreads + tid) * 4);
     }
+}
+template <typename T> __device__ __forceinline__ double add_share(double s, const Share<T> &r) {
 #pragma unroll
-    for (int i = 0; i < kOptGroups; ++i)
+    for (int i = 0; i < kOptGroups; ++i) {
+        const f32x4 y = widen(r.x[i]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s = fma(static_cast<double>(x[i][k]), static_cast<double>(x[i][k]), s);
+        for (int k = 0; k < 4; ++k) s = add_square(s, y[k]);
+    }
+    return s;
+}
+// the at most three elements behind a chunk's last whole vector
+template <typename T>
+__device__ __forceinline__ double add_rest(double s, const T *g, int count) {
+    if (count % 4 != 0 && static_cast<int>(threadIdx.x) < count % 4)
+        s = add_square(s, load1(g + count / 4 * 4 + threadIdx.x));
     return s;
 }
 
-// Blocks: part[block] = the squares of chunks block, block + gridDim.x, ...
+// The gradient of a chunk, if it is of type T; count 0 else and past the end.
+template <typename T> struct ChunkAt {
+    const T *g;
+    int count;
+};
+template <typename T>
+__device__ __forceinline__ ChunkAt<T> chunk_at(const OptTensor *ten, const OptChunk *chunks,
+                                               int64_t k, int64_t end) {
+    constexpr uint32_t type = sizeof(T) == 2 ? kOptGradBf16 : 0;
+    ChunkAt<T> a{nullptr, 0};
+    if (k < end) {
+        const OptChunk c = chunks[k];
+        const OptTensor &t = ten[c.tensor];
+        a.g = (const T *)t.g + c.start;
+        a.count = (t.types & kOptGradBf16) == type ? c.count : 0;
+    }
+    return a;
+}
+
+// The squares of this block's chunks of type T in [lo, end), some at a time
+// (32 registers of gradients on the way), the places of the next looked up
+// while these are read.
+template <bool NT, typename T>
+__device__ double range_squares(const OptTensor *ten, const OptChunk *chunks, int64_t lo, int64_t end) {
+    constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
+    const int64_t by = gridDim.x;
+    double s = 0.0;
+    ChunkAt<T> a[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) a[j] = chunk_at<T>(ten, chunks, lo + blockIdx.x + j * by, end);
+    for (int64_t k = lo + blockIdx.x; k < end; k += kAtOnce * by) {
+        Share<T> r[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) read_share<NT>(r[j], a[j].g, a[j].count);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) s = add_rest(s, a[j].g, a[j].count);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            a[j] = chunk_at<T>(ten, chunks, k + (kAtOnce + j) * by, end);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) s = add_share(s, r[j]);
+    }
+    return s;
+}
+
+// Blocks: part[block] = the squares of every gridDim.x-th chunk. The first
+// n_stream chunks are read without being kept in the caches, so that the last
+// ones, which the launch that scales the gradients reads first, are still
+// there.
 // Block 0 also takes the step number of an AdamW step and its corrections
 // 1 / (1 - beta^t): the update writes the number, so its other blocks must
 // not read it.
 __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
-    double *__restrict__ part, const int64_t *step, double beta1, double beta2,
-    OptStep *__restrict__ at) {
+    int n_stream, uint32_t types, double *__restrict__ part, const int64_t *step, double beta1,
+    double beta2, OptStep *__restrict__ at) {
     __shared__ double sh[kOptThreads / kWave];
     double s = 0.0;
-    for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
-        const OptChunk c = chunks[k];
-        const OptTensor &t = ten[c.tensor];
-        if (t.types & kOptGradBf16)
-            s += chunk_squares(u16_at(t.g, c.start), c.count);
-        else
-            s += chunk_squares(f32_at(t.g, c.start), c.count);
+    if (types & kOptListF32) {
+        s += range_squares<true, gf32>(ten, chunks, 0, n_stream);
+        s += range_squares<false, gf32>(ten, chunks, n_stream, n_chunks);
+    }
+    if (types & kOptListBf16) {
+        s += range_squares<true, gu16>(ten, chunks, 0, n_stream);
+        s += range_squares<false, gu16>(ten, chunks, n_stream, n_chunks);
     }
     s = block_sum(s, sh);
     if (threadIdx.x == 0) {
@@ -176,38 +233,40 @@ __global__ __launch_bounds__(kOptThreads) void grad_norm_kernel(OptNorm nm) {
     if (threadIdx.x == 0) *nm.norm = f.norm;
 }
 
-template <typename TI, typename TO>
+template <bool NT, typename TI, typename TO>
 __device__ __forceinline__ void scale_chunk(const TI *g, TO *out, int count, float c) {
-    f32x4 x[kOptGroups];
+    typename Vec4<TI>::type x[kOptGroups];
+    const int n4 = count / 4, tid = threadIdx.x, e1 = n4 * 4 + tid;
 #pragma unroll
-    for (int i = 0; i < kOptGroups; ++i) {
-        const int e = (i * kOptThreads + threadIdx.x) * 4;
-        if (e < count) x[i] = load4(g + e, e + 4 <= count, count - e);
-    }
+    for (int i = 0; i < kOptGroups; ++i)
+        if (i * kOptThreads + tid < n4) x[i] = load4<NT>(g + (i * kOptThreads + tid) * 4);
+    const float x1 = e1 < count ? load1(g + e1) : 0.f;
 #pragma unroll
-    for (int i = 0; i < kOptGroups; ++i) {
-        const int e = (i * kOptThreads + threadIdx.x) * 4;
-        if (e < count) store4(out + e, x[i] * c, e + 4 <= count, count - e);
-    }
+    for (int i = 0; i < kOptGroups; ++i)
+        if (i * kOptThreads + tid < n4) store4<NT>(out + (i * kOptThreads + tid) * 4, widen(x[i]) * c);
+    if (e1 < count) store1(out + e1, x1 * c);
 }
 
+// From the last chunk to the first: the norm's launch has read the last ones
+// most recently.
+template <bool NT>
 __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
     OptNorm nm) {
     __shared__ double sh[kOptThreads / kWave];
     const NormFactor f = norm_factor(nm, sh);
     if (nm.n_part >= 0 && nm.norm && blockIdx.x == 0 && threadIdx.x == 0) *nm.norm = f.norm;
-    for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
+    for (int k = n_chunks - 1 - static_cast<int>(blockIdx.x); k >= 0; k -= gridDim.x) {
         const OptChunk ch = chunks[k];
         const OptTensor &t = ten[ch.tensor];
         if (f.c == 1.f && t.g == t.out) continue;  // in place, nothing to clip
         const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
         gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
         gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
-        if (gb && ob) scale_chunk(gh, oh, ch.count, f.c);
-        else if (gb) scale_chunk(gh, of, ch.count, f.c);
-        else if (ob) scale_chunk(gf, oh, ch.count, f.c);
-        else scale_chunk(gf, of, ch.count, f.c);
+        if (gb && ob) scale_chunk<NT>(gh, oh, ch.count, f.c);
+        else if (gb) scale_chunk<NT>(gh, of, ch.count, f.c);
+        else if (ob) scale_chunk<NT>(gf, oh, ch.count, f.c);
+        else scale_chunk<NT>(gf, of, ch.count, f.c);
     }
 }
 
@@ -217,39 +276,53 @@ __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
 struct StepConst {
     float c, b1, b2, a1, a2, inv_c1, inv_c2, eps, lr, decay;
 };
-template <typename GT, int WM>
+__device__ __forceinline__ void adamw_one(const StepConst &q, float g, float &w, float &m, float &v) {
+    g *= q.c;
+    m = fmaf(q.b1, m, q.a1 * g);
+    v = fmaf(q.b2, v, q.a2 * g * g);
+    const float u = (m * q.inv_c1) / (sqrtf(v * q.inv_c2) + q.eps);
+    w -= q.lr * fmaf(q.decay, w, u);
+}
+template <bool NT, bool NTG, typename GT, int WM>
 __device__ __forceinline__ void adamw_chunk(const OptTensor &t, int64_t start, int count,
                                             const StepConst &q) {
     const GT *g = (const GT *)t.g + start;
     gf32 *wf = f32_at(WM == 2 ? t.w32 : t.w, start), *m = f32_at(t.m, start), *v = f32_at(t.v, start);
     gu16 *wh = u16_at(t.w, start);
+    const int n4 = count / 4, tid = threadIdx.x, e1 = n4 * 4 + tid;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i) {
-        const int e = (i * kOptThreads + threadIdx.x) * 4;
-        if (e >= count) continue;
-        const bool full = e + 4 <= count;
-        const int left = count - e;
-        f32x4 gx = load4(g + e, full, left);
-        f32x4 wx = (WM == 1) ? load4(wh + e, full, left) : load4(wf + e, full, left);
-        f32x4 mx = load4(m + e, full, left);
-        f32x4 vx = load4(v + e, full, left);
+        if (i * kOptThreads + tid >= n4) continue;
+        const int e = (i * kOptThreads + tid) * 4;
+        const f32x4 gx = widen(load4<NTG>(g + e));
+        f32x4 wx = (WM == 1) ? widen(load4<NT>(wh + e)) : load4<NT>(wf + e);
+        f32x4 mx = load4<NT>(m + e);
+        f32x4 vx = load4<NT>(v + e);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float gk = gx[k] * q.c;
-            const float mk = fmaf(q.b1, mx[k], q.a1 * gk);
-            const float vk = fmaf(q.b2, vx[k], q.a2 * gk * gk);
-            const float u = (mk * q.inv_c1) / (sqrtf(vk * q.inv_c2) + q.eps);
-            mx[k] = mk;
-            vx[k] = vk;
-            wx[k] = wx[k] - q.lr * fmaf(q.decay, wx[k], u);
+            float w1 = wx[k], m1 = mx[k], v1 = vx[k];
+            adamw_one(q, gx[k], w1, m1, v1);
+            wx[k] = w1;
+            mx[k] = m1;
+            vx[k] = v1;
         }
-        store4(m + e, mx, full, left);
-        store4(v + e, vx, full, left);
-        if (WM != 1) store4(wf + e, wx, full, left);
-        if (WM != 0) store4(wh + e, wx, full, left);
+        store4<NT>(m + e, mx);
+        store4<NT>(v + e, vx);
+        if (WM != 1) store4<NT>(wf + e, wx);
+        if (WM != 0) store4<NT>(wh + e, wx);
+    }
+    if (e1 < count) {
+        float w1 = (WM == 1) ? load1(wh + e1) : wf[e1], m1 = m[e1], v1 = v[e1];
+        adamw_one(q, load1(g + e1), w1, m1, v1);
+        m[e1] = m1;
+        v[e1] = v1;
+        if (WM != 1) wf[e1] = w1;
+        if (WM != 0) store1(wh + e1, w1);
     }
 }
 
+// From the last chunk to the first, as grad_clip_kernel.
+template <bool NT, bool NTG>
 __global__ __launch_bounds__(kOptThreads) void adamw_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
     OptNorm nm, OptAdamW hp, const float *__restrict__ lr, const OptStep *__restrict__ at,
@@ -262,20 +335,20 @@ __global__ __launch_bounds__(kOptThreads) void adamw_kernel(
     if (first) *step = at->t;
     StepConst q{f.c, hp.b1, hp.b2, hp.a1, hp.a2, at->inv_c1, at->inv_c2, hp.eps, 0.f, 0.f};
     const float rate = lr ? *lr : hp.lr;
-    for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
+    for (int k = n_chunks - 1 - static_cast<int>(blockIdx.x); k >= 0; k -= gridDim.x) {
         const OptChunk ch = chunks[k];
         const OptTensor &t = ten[ch.tensor];
         q.lr = rate * t.lr_scale;
         q.decay = hp.decay * t.decay_scale;
         const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
         if (t.types & kOptGradBf16) {
-            if (wm == 0) adamw_chunk<gu16, 0>(t, ch.start, ch.count, q);
-            else if (wm == 1) adamw_chunk<gu16, 1>(t, ch.start, ch.count, q);
-            else adamw_chunk<gu16, 2>(t, ch.start, ch.count, q);
+            if (wm == 0) adamw_chunk<NT, NTG, gu16, 0>(t, ch.start, ch.count, q);
+            else if (wm == 1) adamw_chunk<NT, NTG, gu16, 1>(t, ch.start, ch.count, q);
+            else adamw_chunk<NT, NTG, gu16, 2>(t, ch.start, ch.count, q);
         } else {
-            if (wm == 0) adamw_chunk<gf32, 0>(t, ch.start, ch.count, q);
-            else if (wm == 1) adamw_chunk<gf32, 1>(t, ch.start, ch.count, q);
-            else adamw_chunk<gf32, 2>(t, ch.start, ch.count, q);
+            if (wm == 0) adamw_chunk<NT, NTG, gf32, 0>(t, ch.start, ch.count, q);
+            else if (wm == 1) adamw_chunk<NT, NTG, gf32, 1>(t, ch.start, ch.count, q);
+            else adamw_chunk<NT, NTG, gf32, 2>(t, ch.start, ch.count, q);
         }
     }
 }
@@ -297,12 +370,20 @@ __global__ __launch_bounds__(kOptThreads) void tensor_list_kernel(OptBatch b, Op
 
 int opt_blocks(int n_chunks, int most) { return n_chunks < 1 ? 1 : n_chunks < most ? n_chunks : most; }
 
-hipError_t launch_squares(const OptList &L, const OptNorm &nm, const int64_t *step, double beta1,
-                          double beta2, OptStep *at, hipStream_t st) {
+// Bytes that stay in the last cache level (256 MB) from one launch to the next.
+constexpr int64_t kOptCached = 200 << 20;
+
+// `scaled`: a launch that reads the gradients again follows
+hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, const int64_t *step,
+                          double beta1, double beta2, OptStep *at, hipStream_t st) {
     const bool sums = nm.n_part >= 0;
+    int n_stream = 0;
+    if (L.g_bytes > kOptCached)
+        n_stream = L.n_chunks - (scaled ? static_cast<int>(static_cast<double>(L.n_chunks) * kOptCached / L.g_bytes) : 0);
     ProfScope prof(sums ? "grad_squares" : "adamw_count", st);
     hipLaunchKernelGGL(grad_squares_kernel, dim3(sums ? nm.n_part : 1), dim3(kOptThreads), 0, st,
-                       L.ten, L.chunks, sums ? L.n_chunks : 0, nm.part, step, beta1, beta2, at);
+                       L.ten, L.chunks, sums ? L.n_chunks : 0, n_stream, sums ? L.g_types : 0u, nm.part,
+                       step, beta1, beta2, at);
     return hipGetLastError();
 }
 
@@ -319,7 +400,7 @@ hipError_t launch_tensor_list(const OptBatch &b, int count, OptTensor *ten, OptC
 }
 
 hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st) {
-    hipError_t e = launch_squares(L, nm, nullptr, 0.0, 0.0, nullptr, st);
+    hipError_t e = launch_squares(L, nm, false, nullptr, 0.0, 0.0, nullptr, st);
     if (e != hipSuccess) return e;
     ProfScope prof("grad_norm", st);
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kOptThreads), 0, st, nm);
@@ -328,22 +409,26 @@ hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st)
 
 hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st) {
     if (nm.n_part >= 0) {
-        hipError_t e = launch_squares(L, nm, nullptr, 0.0, 0.0, nullptr, st);
+        hipError_t e = launch_squares(L, nm, true, nullptr, 0.0, 0.0, nullptr, st);
         if (e != hipSuccess) return e;
     }
     ProfScope prof("grad_clip", st);
-    hipLaunchKernelGGL(grad_clip_kernel, dim3(opt_blocks(L.n_chunks, 2048)), dim3(kOptThreads), 0,
-                       st, L.ten, L.chunks, L.n_chunks, nm);
+    const auto kernel = L.g_bytes + L.out_bytes > kOptCached ? grad_clip_kernel<true> : grad_clip_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks, 2048)), dim3(kOptThreads), 0, st, L.ten,
+                       L.chunks, L.n_chunks, nm);
     return hipGetLastError();
 }
 
 hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp, const float *lr,
                         int64_t *step, OptStep *at, hipStream_t st) {
-    hipError_t e = launch_squares(L, nm, step, hp.beta1, hp.beta2, at, st);
+    hipError_t e = launch_squares(L, nm, true, step, hp.beta1, hp.beta2, at, st);
     if (e != hipSuccess) return e;
     ProfScope prof("adamw", st);
-    hipLaunchKernelGGL(adamw_kernel, dim3(opt_blocks(L.n_chunks, 2048)), dim3(kOptThreads), 0, st,
-                       L.ten, L.chunks, L.n_chunks, nm, hp, lr, at, step);
+    const auto kernel = L.g_bytes > kOptCached             ? adamw_kernel<true, true>
+                        : L.g_bytes + L.w_bytes > kOptCached ? adamw_kernel<true, false>
+                                                             : adamw_kernel<false, false>;
+    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks, 2048)), dim3(kOptThreads), 0, st, L.ten,
+                       L.chunks, L.n_chunks, nm, hp, lr, at, step);
     return hipGetLastError();
 }
 

@@ -44,7 +44,7 @@ def _list(has_weights=1):
 def test_structs_match_the_header():
     """Sizes that the header's field lists give (LP64, natural alignment)."""
     assert C.sizeof(dstd.dstd_tensor) == 6 * 8 + 8 + 3 * 4 + 2 * 4 + 4
-    assert C.sizeof(dstd.dstd_tensor_list) == 8 + 3 * 8 + 2 * 4
+    assert C.sizeof(dstd.dstd_tensor_list) == 8 + 6 * 8 + 4 * 4
     assert C.sizeof(dstd.dstd_adamw_params) == 6 * 8
 
 
