@@ -559,7 +559,7 @@ size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
  * `stream` and fills *list. The host array may go once the call returns; mem
  * and the tensors have to stay while the list is used, and a call on another
  * stream has to be ordered behind the build. A tensor that moves needs a new
- * build. n_tensors and any n may be 0; n < 2^40 and fewer than 2^31 chunks
+ * build. n_tensors and any n may be 0; n < 2^35 and fewer than 2^23 chunks
  * of 4096 elements in all. Arrays of one list must not overlap (out = g
  * apart): DSTD_ERR_PARAM.
  */

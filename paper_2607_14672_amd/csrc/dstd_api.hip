@@ -1050,20 +1050,23 @@ dstd_status check_dtype(int32_t t, const char *what) {
 
 int64_t dtype_bytes(int32_t t) { return t == DSTD_BF16 ? 2 : 4; }
 
-// chunks of the whole list, in *n_chunks
+// A launch takes one block of at most 512 threads per chunk, and fewer than
+// 2^32 threads.
+constexpr int64_t kMaxChunks = (int64_t)1 << 23;
+
+// chunks and elements of the whole list
 dstd_status check_counts(int64_t n, const dstd_tensor *t, int64_t *n_chunks, int64_t *n_elems) {
     if (n < 0) return fail(DSTD_ERR_SHAPE, "n_tensors must be >= 0");
     if (n > 0 && !t) return fail(DSTD_ERR_NULL, "tensors is NULL");
-    const int64_t lim = (int64_t)1 << 31;
-    if (n >= lim) return fail(DSTD_ERR_SHAPE, "too many tensors");
+    if (n >= (int64_t)1 << 31) return fail(DSTD_ERR_SHAPE, "too many tensors");
     int64_t c = 0, e = 0;
     for (int64_t k = 0; k < n; ++k) {
-        if (t[k].n < 0 || t[k].n >= (int64_t)1 << 40)
-            return fail(DSTD_ERR_SHAPE, "tensor %lld: n = %lld must be in [0, 2^40)", (long long)k,
+        if (t[k].n < 0 || t[k].n >= kMaxChunks * dstd::kOptChunk)
+            return fail(DSTD_ERR_SHAPE, "tensor %lld: n = %lld must be in [0, 2^35)", (long long)k,
                         (long long)t[k].n);
         c += (t[k].n + dstd::kOptChunk - 1) / dstd::kOptChunk;
         e += t[k].n;
-        if (c >= lim) return fail(DSTD_ERR_SHAPE, "the list's tensors are too large together");
+        if (c >= kMaxChunks) return fail(DSTD_ERR_SHAPE, "the list's tensors are too large together");
     }
     *n_chunks = c;
     *n_elems = e;
@@ -1121,7 +1124,7 @@ dstd_status check_tensor(const dstd_tensor &t, int64_t k, std::vector<Range> &r)
 dstd_status check_list(const dstd_tensor_list *l) {
     if (!l) return fail(DSTD_ERR_NULL, "list is NULL");
     if (l->magic != kListMagic || !l->mem || l->n_tensors < 0 || l->n_chunks < 0 ||
-        l->n_chunks >= (int64_t)1 << 31)
+        l->n_chunks >= kMaxChunks)
         return fail(DSTD_ERR_PARAM, "not a list that dstd_tensor_list_build has filled");
     return DSTD_OK;
 }

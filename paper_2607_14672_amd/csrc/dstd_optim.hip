@@ -15,6 +15,8 @@
 // launch sums the squares of a fixed set of chunks per block (partials), and
 // the launch that follows adds the partials again in every block, in a fixed
 // order, rather than in a launch of its own.
+#include <limits.h>
+
 #include "dstd_internal.h"
 #include "dstd_kernels.h"
 #include "dstd_profile.h"
@@ -23,8 +25,15 @@ namespace dstd {
 
 namespace {
 
+// Threads of a block, and so 4-element vectors of a chunk per thread. The
+// update has seven arrays on the way: with fewer vectors of each per thread its
+// registers leave more waves (201 M weights: 949 us with 256 threads, 920 with
+// 512, 916 with 1024; the norm 121, 128 and 129, clipping 67 M bf16 86, 87 and
+// 126).
 constexpr int kOptThreads = 256;
-constexpr int kOptGroups = static_cast<int>(kOptChunk) / (kOptThreads * 4);  // of 4 elements per thread
+constexpr int kStepThreads = 512;
+template <int kThreads> constexpr int kVecs = static_cast<int>(kOptChunk) / (kThreads * 4);
+constexpr int kOptGroups = kVecs<kOptThreads>;
 
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u16x4 = uint16_t __attribute__((ext_vector_type(4)));
@@ -76,7 +85,7 @@ __device__ __forceinline__ gf32 *f32_at(void *p, int64_t start) { return (gf32 *
 __device__ __forceinline__ gu16 *u16_at(void *p, int64_t start) { return (gu16 *)p + start; }
 
 // Sum over the block, in a fixed order, to every thread. sh: one double per wave.
-__device__ double block_sum(double v, double *sh) {
+template <int kThreads> __device__ double block_sum(double v, double *sh) {
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
     __syncthreads();
@@ -84,7 +93,7 @@ __device__ double block_sum(double v, double *sh) {
     __syncthreads();
     double s = 0.0;
 #pragma unroll
-    for (int k = 0; k < kOptThreads / kWave; ++k) s += sh[k];
+    for (int k = 0; k < kThreads / kWave; ++k) s += sh[k];
     return s;
 }
 
@@ -193,7 +202,7 @@ __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
         s += range_squares<true, gu16>(ten, chunks, 0, n_stream);
         s += range_squares<false, gu16>(ten, chunks, n_stream, n_chunks);
     }
-    s = block_sum(s, sh);
+    s = block_sum<kOptThreads>(s, sh);
     if (threadIdx.x == 0) {
         part[blockIdx.x] = s;
         if (step && blockIdx.x == 0) {
@@ -211,12 +220,12 @@ struct NormFactor {
     float norm, c;
     bool finite;
 };
-__device__ NormFactor norm_factor(const OptNorm &nm, double *sh) {
+template <int kThreads> __device__ NormFactor norm_factor(const OptNorm &nm, double *sh) {
     double n = 0.0;
     if (nm.n_part >= 0) {
         double s = 0.0;
-        for (int k = threadIdx.x; k < nm.n_part; k += kOptThreads) s += nm.part[k];
-        n = sqrt(block_sum(s, sh));
+        for (int k = threadIdx.x; k < nm.n_part; k += kThreads) s += nm.part[k];
+        n = sqrt(block_sum<kThreads>(s, sh));
     } else if (nm.norm) {
         n = static_cast<double>(*nm.norm);
     }
@@ -229,45 +238,49 @@ __device__ NormFactor norm_factor(const OptNorm &nm, double *sh) {
 
 __global__ __launch_bounds__(kOptThreads) void grad_norm_kernel(OptNorm nm) {
     __shared__ double sh[kOptThreads / kWave];
-    const NormFactor f = norm_factor(nm, sh);
+    const NormFactor f = norm_factor<kOptThreads>(nm, sh);
     if (threadIdx.x == 0) *nm.norm = f.norm;
 }
 
 template <bool NT, typename TI, typename TO>
-__device__ __forceinline__ void scale_chunk(const TI *g, TO *out, int count, float c) {
+__device__ __forceinline__ void clip_chunk(const TI *g, TO *out, int count, const OptNorm &nm,
+                                           double *sh) {
     typename Vec4<TI>::type x[kOptGroups];
     const int n4 = count / 4, tid = threadIdx.x, e1 = n4 * 4 + tid;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
         if (i * kOptThreads + tid < n4) x[i] = load4<NT>(g + (i * kOptThreads + tid) * 4);
     const float x1 = e1 < count ? load1(g + e1) : 0.f;
+    const float c = norm_factor<kOptThreads>(nm, sh).c;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
         if (i * kOptThreads + tid < n4) store4<NT>(out + (i * kOptThreads + tid) * 4, widen(x[i]) * c);
     if (e1 < count) store1(out + e1, x1 * c);
 }
 
-// From the last chunk to the first: the norm's launch has read the last ones
-// most recently.
+// One chunk a block, from the last to the first: the norm's launch has read
+// the last ones most recently. The chunk is on its way while the partials are
+// added.
 template <bool NT>
 __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
     OptNorm nm) {
     __shared__ double sh[kOptThreads / kWave];
-    const NormFactor f = norm_factor(nm, sh);
-    if (nm.n_part >= 0 && nm.norm && blockIdx.x == 0 && threadIdx.x == 0) *nm.norm = f.norm;
-    for (int k = n_chunks - 1 - static_cast<int>(blockIdx.x); k >= 0; k -= gridDim.x) {
-        const OptChunk ch = chunks[k];
-        const OptTensor &t = ten[ch.tensor];
-        if (f.c == 1.f && t.g == t.out) continue;  // in place, nothing to clip
-        const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
-        gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
-        gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
-        if (gb && ob) scale_chunk<NT>(gh, oh, ch.count, f.c);
-        else if (gb) scale_chunk<NT>(gh, of, ch.count, f.c);
-        else if (ob) scale_chunk<NT>(gf, oh, ch.count, f.c);
-        else scale_chunk<NT>(gf, of, ch.count, f.c);
+    if (nm.n_part >= 0 && nm.norm && blockIdx.x == 0) {
+        const NormFactor f = norm_factor<kOptThreads>(nm, sh);
+        if (threadIdx.x == 0) *nm.norm = f.norm;
     }
+    if (n_chunks == 0) return;
+    const OptChunk ch = chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)];
+    const OptTensor &t = ten[ch.tensor];
+    if (t.g == t.out && norm_factor<kOptThreads>(nm, sh).c == 1.f) return;  // in place, nothing to clip
+    const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
+    gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
+    gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
+    if (gb && ob) clip_chunk<NT>(gh, oh, ch.count, nm, sh);
+    else if (gb) clip_chunk<NT>(gh, of, ch.count, nm, sh);
+    else if (ob) clip_chunk<NT>(gf, oh, ch.count, nm, sh);
+    else clip_chunk<NT>(gf, of, ch.count, nm, sh);
 }
 
 // One chunk's update in fp32. WM: 0 = fp32 weights, 1 = bf16 weights (the
@@ -283,33 +296,57 @@ __device__ __forceinline__ void adamw_one(const StepConst &q, float g, float &w,
     const float u = (m * q.inv_c1) / (sqrtf(v * q.inv_c2) + q.eps);
     w -= q.lr * fmaf(q.decay, w, u);
 }
+// What the chunks of a step share.
+struct StepArgs {
+    OptNorm nm;
+    OptAdamW hp;
+    const float *lr;
+    const OptStep *at;
+    int64_t *step;
+};
 template <bool NT, bool NTG, typename GT, int WM>
 __device__ __forceinline__ void adamw_chunk(const OptTensor &t, int64_t start, int count,
-                                            const StepConst &q) {
+                                            const StepArgs &a, double *sh) {
     const GT *g = (const GT *)t.g + start;
     gf32 *wf = f32_at(WM == 2 ? t.w32 : t.w, start), *m = f32_at(t.m, start), *v = f32_at(t.v, start);
     gu16 *wh = u16_at(t.w, start);
     const int n4 = count / 4, tid = threadIdx.x, e1 = n4 * 4 + tid;
+    typename Vec4<GT>::type gx[kVecs<kStepThreads>];
+    f32x4 wx[kVecs<kStepThreads>], mx[kVecs<kStepThreads>], vx[kVecs<kStepThreads>];
+    u16x4 hx[kVecs<kStepThreads>];
 #pragma unroll
-    for (int i = 0; i < kOptGroups; ++i) {
-        if (i * kOptThreads + tid >= n4) continue;
-        const int e = (i * kOptThreads + tid) * 4;
-        const f32x4 gx = widen(load4<NTG>(g + e));
-        f32x4 wx = (WM == 1) ? widen(load4<NT>(wh + e)) : load4<NT>(wf + e);
-        f32x4 mx = load4<NT>(m + e);
-        f32x4 vx = load4<NT>(v + e);
+    for (int i = 0; i < kVecs<kStepThreads>; ++i) {
+        if (i * kStepThreads + tid >= n4) continue;
+        const int e = (i * kStepThreads + tid) * 4;
+        gx[i] = load4<NTG>(g + e);
+        if (WM == 1) hx[i] = load4<NT>(wh + e);
+        else wx[i] = load4<NT>(wf + e);
+        mx[i] = load4<NT>(m + e);
+        vx[i] = load4<NT>(v + e);
+    }
+    const NormFactor f = norm_factor<kStepThreads>(a.nm, sh);
+    if (!f.finite) return;  // the step is skipped
+    const float rate = a.lr ? *a.lr : a.hp.lr;
+    const StepConst q{f.c, a.hp.b1, a.hp.b2, a.hp.a1, a.hp.a2, a.at->inv_c1, a.at->inv_c2, a.hp.eps,
+                      rate * t.lr_scale, a.hp.decay * t.decay_scale};
+#pragma unroll
+    for (int i = 0; i < kVecs<kStepThreads>; ++i) {
+        if (i * kStepThreads + tid >= n4) continue;
+        const int e = (i * kStepThreads + tid) * 4;
+        const f32x4 g4 = widen(gx[i]);
+        if (WM == 1) wx[i] = widen(hx[i]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            float w1 = wx[k], m1 = mx[k], v1 = vx[k];
-            adamw_one(q, gx[k], w1, m1, v1);
-            wx[k] = w1;
-            mx[k] = m1;
-            vx[k] = v1;
+            float w1 = wx[i][k], m1 = mx[i][k], v1 = vx[i][k];
+            adamw_one(q, g4[k], w1, m1, v1);
+            wx[i][k] = w1;
+            mx[i][k] = m1;
+            vx[i][k] = v1;
         }
-        store4<NT>(m + e, mx);
-        store4<NT>(v + e, vx);
-        if (WM != 1) store4<NT>(wf + e, wx);
-        if (WM != 0) store4<NT>(wh + e, wx);
+        store4<NT>(m + e, mx[i]);
+        store4<NT>(v + e, vx[i]);
+        if (WM != 1) store4<NT>(wf + e, wx[i]);
+        if (WM != 0) store4<NT>(wh + e, wx[i]);
     }
     if (e1 < count) {
         float w1 = (WM == 1) ? load1(wh + e1) : wf[e1], m1 = m[e1], v1 = v[e1];
@@ -321,35 +358,31 @@ __device__ __forceinline__ void adamw_chunk(const OptTensor &t, int64_t start, i
     }
 }
 
-// From the last chunk to the first, as grad_clip_kernel.
+// One chunk a block, from the last to the first, as grad_clip_kernel.
 template <bool NT, bool NTG>
-__global__ __launch_bounds__(kOptThreads) void adamw_kernel(
+__global__ __launch_bounds__(kStepThreads) void adamw_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
-    OptNorm nm, OptAdamW hp, const float *__restrict__ lr, const OptStep *__restrict__ at,
-    int64_t *step) {
-    __shared__ double sh[kOptThreads / kWave];
-    const NormFactor f = norm_factor(nm, sh);
-    const bool first = blockIdx.x == 0 && threadIdx.x == 0;
-    if (nm.n_part >= 0 && nm.norm && first) *nm.norm = f.norm;
-    if (!f.finite) return;  // the step is skipped
-    if (first) *step = at->t;
-    StepConst q{f.c, hp.b1, hp.b2, hp.a1, hp.a2, at->inv_c1, at->inv_c2, hp.eps, 0.f, 0.f};
-    const float rate = lr ? *lr : hp.lr;
-    for (int k = n_chunks - 1 - static_cast<int>(blockIdx.x); k >= 0; k -= gridDim.x) {
-        const OptChunk ch = chunks[k];
-        const OptTensor &t = ten[ch.tensor];
-        q.lr = rate * t.lr_scale;
-        q.decay = hp.decay * t.decay_scale;
-        const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
-        if (t.types & kOptGradBf16) {
-            if (wm == 0) adamw_chunk<NT, NTG, gu16, 0>(t, ch.start, ch.count, q);
-            else if (wm == 1) adamw_chunk<NT, NTG, gu16, 1>(t, ch.start, ch.count, q);
-            else adamw_chunk<NT, NTG, gu16, 2>(t, ch.start, ch.count, q);
-        } else {
-            if (wm == 0) adamw_chunk<NT, NTG, gf32, 0>(t, ch.start, ch.count, q);
-            else if (wm == 1) adamw_chunk<NT, NTG, gf32, 1>(t, ch.start, ch.count, q);
-            else adamw_chunk<NT, NTG, gf32, 2>(t, ch.start, ch.count, q);
+    StepArgs a) {
+    __shared__ double sh[kStepThreads / kWave];
+    if (blockIdx.x == 0) {
+        const NormFactor f = norm_factor<kStepThreads>(a.nm, sh);
+        if (threadIdx.x == 0) {
+            if (a.nm.n_part >= 0 && a.nm.norm) *a.nm.norm = f.norm;
+            if (f.finite) *a.step = a.at->t;
         }
+    }
+    if (n_chunks == 0) return;
+    const OptChunk ch = chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)];
+    const OptTensor &t = ten[ch.tensor];
+    const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
+    if (t.types & kOptGradBf16) {
+        if (wm == 0) adamw_chunk<NT, NTG, gu16, 0>(t, ch.start, ch.count, a, sh);
+        else if (wm == 1) adamw_chunk<NT, NTG, gu16, 1>(t, ch.start, ch.count, a, sh);
+        else adamw_chunk<NT, NTG, gu16, 2>(t, ch.start, ch.count, a, sh);
+    } else {
+        if (wm == 0) adamw_chunk<NT, NTG, gf32, 0>(t, ch.start, ch.count, a, sh);
+        else if (wm == 1) adamw_chunk<NT, NTG, gf32, 1>(t, ch.start, ch.count, a, sh);
+        else adamw_chunk<NT, NTG, gf32, 2>(t, ch.start, ch.count, a, sh);
     }
 }
 
@@ -368,10 +401,10 @@ __global__ __launch_bounds__(kOptThreads) void tensor_list_kernel(OptBatch b, Op
     }
 }
 
-int opt_blocks(int n_chunks, int most) { return n_chunks < 1 ? 1 : n_chunks < most ? n_chunks : most; }
+int opt_blocks(int n_chunks, int most = INT_MAX) { return n_chunks < 1 ? 1 : n_chunks < most ? n_chunks : most; }
 
 // Bytes that stay in the last cache level (256 MB) from one launch to the next.
-constexpr int64_t kOptCached = 200 << 20;
+constexpr int64_t kOptCached = 240 << 20;
 
 // `scaled`: a launch that reads the gradients again follows
 hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, const int64_t *step,
@@ -414,7 +447,7 @@ hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st)
     }
     ProfScope prof("grad_clip", st);
     const auto kernel = L.g_bytes + L.out_bytes > kOptCached ? grad_clip_kernel<true> : grad_clip_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks, 2048)), dim3(kOptThreads), 0, st, L.ten,
+    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks)), dim3(kOptThreads), 0, st, L.ten,
                        L.chunks, L.n_chunks, nm);
     return hipGetLastError();
 }
@@ -427,8 +460,8 @@ hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp,
     const auto kernel = L.g_bytes > kOptCached             ? adamw_kernel<true, true>
                         : L.g_bytes + L.w_bytes > kOptCached ? adamw_kernel<true, false>
                                                              : adamw_kernel<false, false>;
-    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks, 2048)), dim3(kOptThreads), 0, st, L.ten,
-                       L.chunks, L.n_chunks, nm, hp, lr, at, step);
+    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks)), dim3(kStepThreads), 0, st, L.ten,
+                       L.chunks, L.n_chunks, StepArgs{nm, hp, lr, at, step});
     return hipGetLastError();
 }
 
