@@ -32,6 +32,14 @@ namespace {
 // 126).
 constexpr int kOptThreads = 256;
 constexpr int kStepThreads = 512;
+// Lists of up to so many chunks take one launch of one block: a pass is then
+// bound by what the host spends on a launch (3.6 us), and two launches cost
+// 7.5 us (an AdamW step 8.5) whatever such a list holds. One block takes 4.0 us
+// for the norm of 1 chunk, 6.2 for 20 (one round of reads) and 8.4 for 24;
+// clipping 4.5 us for 1, 7.1 for 6, 7.8 for 8; a step 6.4 us for 1, 7.5 for 2,
+// 10.6 for 4.
+constexpr int kSoloThreads = 1024;
+constexpr int kSoloNormChunks = 20, kSoloClipChunks = 6, kSoloStepChunks = 2;
 template <int kThreads> constexpr int kVecs = static_cast<int>(kOptChunk) / (kThreads * 4);
 constexpr int kOptGroups = kVecs<kOptThreads>;
 
@@ -111,8 +119,8 @@ template <typename T> struct Share {
     typename Vec4<T>::type x[kOptGroups];
 };
 template <bool NT, typename T>
-__device__ __forceinline__ void read_share(Share<T> &r, const T *g, int count) {
-    const int n4 = count / 4, tid = threadIdx.x;
+__device__ __forceinline__ void read_share(Share<T> &r, const T *g, int count, int tid) {
+    const int n4 = count / 4;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i) {
         r.x[i] = typename Vec4<T>::type{0, 0, 0, 0};
@@ -130,9 +138,8 @@ template <typename T> __device__ __forceinline__ double add_share(double s, cons
 }
 // the at most three elements behind a chunk's last whole vector
 template <typename T>
-__device__ __forceinline__ double add_rest(double s, const T *g, int count) {
-    if (count % 4 != 0 && static_cast<int>(threadIdx.x) < count % 4)
-        s = add_square(s, load1(g + count / 4 * 4 + threadIdx.x));
+__device__ __forceinline__ double add_rest(double s, const T *g, int count, int tid) {
+    if (count % 4 != 0 && tid < count % 4) s = add_square(s, load1(g + count / 4 * 4 + tid));
     return s;
 }
 
@@ -155,30 +162,38 @@ __device__ __forceinline__ ChunkAt<T> chunk_at(const OptTensor *ten, const OptCh
     return a;
 }
 
-// The squares of this block's chunks of type T in [lo, end), some at a time
-// (32 registers of gradients on the way), the places of the next looked up
-// while these are read.
-template <bool NT, typename T>
-__device__ double range_squares(const OptTensor *ten, const OptChunk *chunks, int64_t lo, int64_t end) {
-    constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
-    const int64_t by = gridDim.x;
+// The squares of the chunks first, first + by, ... of type T in [lo, end), by
+// the kOptThreads threads `tid`: kAtOnce of them at a time, the places of the
+// next looked up while these are read.
+template <int kAtOnce, bool NT, typename T>
+__device__ double range_squares(const OptTensor *ten, const OptChunk *chunks, int64_t lo, int64_t end,
+                                int first, int by, int tid) {
     double s = 0.0;
     ChunkAt<T> a[kAtOnce];
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) a[j] = chunk_at<T>(ten, chunks, lo + blockIdx.x + j * by, end);
-    for (int64_t k = lo + blockIdx.x; k < end; k += kAtOnce * by) {
+    for (int j = 0; j < kAtOnce; ++j)
+        a[j] = chunk_at<T>(ten, chunks, lo + first + static_cast<int64_t>(j) * by, end);
+    for (int64_t k = lo + first; k < end; k += static_cast<int64_t>(kAtOnce) * by) {
         Share<T> r[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) read_share<NT>(r[j], a[j].g, a[j].count);
+        for (int j = 0; j < kAtOnce; ++j) read_share<NT>(r[j], a[j].g, a[j].count, tid);
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) s = add_rest(s, a[j].g, a[j].count);
+        for (int j = 0; j < kAtOnce; ++j) s = add_rest(s, a[j].g, a[j].count, tid);
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            a[j] = chunk_at<T>(ten, chunks, k + (kAtOnce + j) * by, end);
+            a[j] = chunk_at<T>(ten, chunks, k + static_cast<int64_t>(kAtOnce + j) * by, end);
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) s = add_share(s, r[j]);
     }
     return s;
+}
+
+__device__ OptStep step_at(const int64_t *step, double beta1, double beta2) {
+    OptStep r;
+    r.t = *step + 1;
+    r.inv_c1 = static_cast<float>(1.0 / (1.0 - pow(beta1, static_cast<double>(r.t))));
+    r.inv_c2 = static_cast<float>(1.0 / (1.0 - pow(beta2, static_cast<double>(r.t))));
+    return r;
 }
 
 // Blocks: part[block] = the squares of every gridDim.x-th chunk. The first
@@ -194,23 +209,20 @@ __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
     double beta2, OptStep *__restrict__ at) {
     __shared__ double sh[kOptThreads / kWave];
     double s = 0.0;
+    const int b = blockIdx.x, by = gridDim.x, tid = threadIdx.x;
+    // 32 registers of gradients on the way
     if (types & kOptListF32) {
-        s += range_squares<true, gf32>(ten, chunks, 0, n_stream);
-        s += range_squares<false, gf32>(ten, chunks, n_stream, n_chunks);
+        s += range_squares<2, true, gf32>(ten, chunks, 0, n_stream, b, by, tid);
+        s += range_squares<2, false, gf32>(ten, chunks, n_stream, n_chunks, b, by, tid);
     }
     if (types & kOptListBf16) {
-        s += range_squares<true, gu16>(ten, chunks, 0, n_stream);
-        s += range_squares<false, gu16>(ten, chunks, n_stream, n_chunks);
+        s += range_squares<4, true, gu16>(ten, chunks, 0, n_stream, b, by, tid);
+        s += range_squares<4, false, gu16>(ten, chunks, n_stream, n_chunks, b, by, tid);
     }
     s = block_sum<kOptThreads>(s, sh);
     if (threadIdx.x == 0) {
         part[blockIdx.x] = s;
-        if (step && blockIdx.x == 0) {
-            const int64_t t = *step + 1;
-            at->t = t;
-            at->inv_c1 = static_cast<float>(1.0 / (1.0 - pow(beta1, static_cast<double>(t))));
-            at->inv_c2 = static_cast<float>(1.0 / (1.0 - pow(beta2, static_cast<double>(t))));
-        }
+        if (step && blockIdx.x == 0) *at = step_at(step, beta1, beta2);
     }
 }
 
@@ -220,6 +232,13 @@ struct NormFactor {
     float norm, c;
     bool finite;
 };
+__device__ NormFactor factor_of(double n, double max_norm) {
+    NormFactor r;
+    r.norm = static_cast<float>(n);
+    r.finite = isfinite(r.norm);
+    r.c = (r.finite && n > max_norm) ? static_cast<float>(max_norm / n) : 1.f;
+    return r;
+}
 template <int kThreads> __device__ NormFactor norm_factor(const OptNorm &nm, double *sh) {
     double n = 0.0;
     if (nm.n_part >= 0) {
@@ -229,11 +248,7 @@ template <int kThreads> __device__ NormFactor norm_factor(const OptNorm &nm, dou
     } else if (nm.norm) {
         n = static_cast<double>(*nm.norm);
     }
-    NormFactor r;
-    r.norm = static_cast<float>(n);
-    r.finite = isfinite(r.norm);
-    r.c = (r.finite && n > nm.max_norm) ? static_cast<float>(nm.max_norm / n) : 1.f;
-    return r;
+    return factor_of(n, nm.max_norm);
 }
 
 __global__ __launch_bounds__(kOptThreads) void grad_norm_kernel(OptNorm nm) {
@@ -242,45 +257,51 @@ __global__ __launch_bounds__(kOptThreads) void grad_norm_kernel(OptNorm nm) {
     if (threadIdx.x == 0) *nm.norm = f.norm;
 }
 
-template <bool NT, typename TI, typename TO>
-__device__ __forceinline__ void clip_chunk(const TI *g, TO *out, int count, const OptNorm &nm,
-                                           double *sh) {
+// One chunk by kOptThreads threads. The factor is asked for once the chunk's
+// reads are on their way.
+template <bool NT, typename TI, typename TO, typename F>
+__device__ __forceinline__ void clip_values(const TI *g, TO *out, int count, int tid, const F &factor) {
     typename Vec4<TI>::type x[kOptGroups];
-    const int n4 = count / 4, tid = threadIdx.x, e1 = n4 * 4 + tid;
+    const int n4 = count / 4, e1 = n4 * 4 + tid;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
         if (i * kOptThreads + tid < n4) x[i] = load4<NT>(g + (i * kOptThreads + tid) * 4);
     const float x1 = e1 < count ? load1(g + e1) : 0.f;
-    const float c = norm_factor<kOptThreads>(nm, sh).c;
+    const float c = factor().c;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
         if (i * kOptThreads + tid < n4) store4<NT>(out + (i * kOptThreads + tid) * 4, widen(x[i]) * c);
     if (e1 < count) store1(out + e1, x1 * c);
 }
 
+template <bool NT, typename F>
+__device__ __forceinline__ void clip_chunk(const OptTensor *ten, const OptChunk &ch, int tid,
+                                           const F &factor) {
+    const OptTensor &t = ten[ch.tensor];
+    if (t.g == t.out && factor().c == 1.f) return;  // in place, nothing to clip
+    const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
+    gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
+    gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
+    if (gb && ob) clip_values<NT>(gh, oh, ch.count, tid, factor);
+    else if (gb) clip_values<NT>(gh, of, ch.count, tid, factor);
+    else if (ob) clip_values<NT>(gf, oh, ch.count, tid, factor);
+    else clip_values<NT>(gf, of, ch.count, tid, factor);
+}
+
 // One chunk a block, from the last to the first: the norm's launch has read
-// the last ones most recently. The chunk is on its way while the partials are
-// added.
+// the last ones most recently.
 template <bool NT>
 __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
     OptNorm nm) {
     __shared__ double sh[kOptThreads / kWave];
+    const auto factor = [&] { return norm_factor<kOptThreads>(nm, sh); };
     if (nm.n_part >= 0 && nm.norm && blockIdx.x == 0) {
-        const NormFactor f = norm_factor<kOptThreads>(nm, sh);
+        const NormFactor f = factor();
         if (threadIdx.x == 0) *nm.norm = f.norm;
     }
     if (n_chunks == 0) return;
-    const OptChunk ch = chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)];
-    const OptTensor &t = ten[ch.tensor];
-    if (t.g == t.out && norm_factor<kOptThreads>(nm, sh).c == 1.f) return;  // in place, nothing to clip
-    const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
-    gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
-    gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
-    if (gb && ob) clip_chunk<NT>(gh, oh, ch.count, nm, sh);
-    else if (gb) clip_chunk<NT>(gh, of, ch.count, nm, sh);
-    else if (ob) clip_chunk<NT>(gf, oh, ch.count, nm, sh);
-    else clip_chunk<NT>(gf, of, ch.count, nm, sh);
+    clip_chunk<NT>(ten, chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], threadIdx.x, factor);
 }
 
 // One chunk's update in fp32. WM: 0 = fp32 weights, 1 = bf16 weights (the
@@ -296,43 +317,49 @@ __device__ __forceinline__ void adamw_one(const StepConst &q, float g, float &w,
     const float u = (m * q.inv_c1) / (sqrtf(v * q.inv_c2) + q.eps);
     w -= q.lr * fmaf(q.decay, w, u);
 }
-// What the chunks of a step share.
+// What a step's chunks wait for.
+struct StepIn {
+    NormFactor f;
+    OptStep at;
+};
 struct StepArgs {
     OptNorm nm;
     OptAdamW hp;
     const float *lr;
-    const OptStep *at;
+    OptStep *at;
     int64_t *step;
 };
-template <bool NT, bool NTG, typename GT, int WM>
-__device__ __forceinline__ void adamw_chunk(const OptTensor &t, int64_t start, int count,
-                                            const StepArgs &a, double *sh) {
+// One chunk by kThreads threads. `in` is asked for once the chunk's reads are
+// on their way.
+template <int kThreads, bool NT, bool NTG, typename GT, int WM, typename F>
+__device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, int count,
+                                             const StepArgs &a, int tid, const F &in) {
     const GT *g = (const GT *)t.g + start;
     gf32 *wf = f32_at(WM == 2 ? t.w32 : t.w, start), *m = f32_at(t.m, start), *v = f32_at(t.v, start);
     gu16 *wh = u16_at(t.w, start);
-    const int n4 = count / 4, tid = threadIdx.x, e1 = n4 * 4 + tid;
-    typename Vec4<GT>::type gx[kVecs<kStepThreads>];
-    f32x4 wx[kVecs<kStepThreads>], mx[kVecs<kStepThreads>], vx[kVecs<kStepThreads>];
-    u16x4 hx[kVecs<kStepThreads>];
+    const int n4 = count / 4, e1 = n4 * 4 + tid;
+    typename Vec4<GT>::type gx[kVecs<kThreads>];
+    f32x4 wx[kVecs<kThreads>], mx[kVecs<kThreads>], vx[kVecs<kThreads>];
+    u16x4 hx[kVecs<kThreads>];
 #pragma unroll
-    for (int i = 0; i < kVecs<kStepThreads>; ++i) {
-        if (i * kStepThreads + tid >= n4) continue;
-        const int e = (i * kStepThreads + tid) * 4;
+    for (int i = 0; i < kVecs<kThreads>; ++i) {
+        if (i * kThreads + tid >= n4) continue;
+        const int e = (i * kThreads + tid) * 4;
         gx[i] = load4<NTG>(g + e);
         if (WM == 1) hx[i] = load4<NT>(wh + e);
         else wx[i] = load4<NT>(wf + e);
         mx[i] = load4<NT>(m + e);
         vx[i] = load4<NT>(v + e);
     }
-    const NormFactor f = norm_factor<kStepThreads>(a.nm, sh);
-    if (!f.finite) return;  // the step is skipped
+    const StepIn si = in();
+    if (!si.f.finite) return;  // the step is skipped
     const float rate = a.lr ? *a.lr : a.hp.lr;
-    const StepConst q{f.c, a.hp.b1, a.hp.b2, a.hp.a1, a.hp.a2, a.at->inv_c1, a.at->inv_c2, a.hp.eps,
+    const StepConst q{si.f.c, a.hp.b1, a.hp.b2, a.hp.a1, a.hp.a2, si.at.inv_c1, si.at.inv_c2, a.hp.eps,
                       rate * t.lr_scale, a.hp.decay * t.decay_scale};
 #pragma unroll
-    for (int i = 0; i < kVecs<kStepThreads>; ++i) {
-        if (i * kStepThreads + tid >= n4) continue;
-        const int e = (i * kStepThreads + tid) * 4;
+    for (int i = 0; i < kVecs<kThreads>; ++i) {
+        if (i * kThreads + tid >= n4) continue;
+        const int e = (i * kThreads + tid) * 4;
         const f32x4 g4 = widen(gx[i]);
         if (WM == 1) wx[i] = widen(hx[i]);
 #pragma unroll
@@ -358,32 +385,78 @@ __device__ __forceinline__ void adamw_chunk(const OptTensor &t, int64_t start, i
     }
 }
 
+template <int kThreads, bool NT, bool NTG, typename F>
+__device__ __forceinline__ void adamw_chunk(const OptTensor *ten, const OptChunk &ch,
+                                            const StepArgs &a, int tid, const F &in) {
+    const OptTensor &t = ten[ch.tensor];
+    const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
+    if (t.types & kOptGradBf16) {
+        if (wm == 0) adamw_values<kThreads, NT, NTG, gu16, 0>(t, ch.start, ch.count, a, tid, in);
+        else if (wm == 1) adamw_values<kThreads, NT, NTG, gu16, 1>(t, ch.start, ch.count, a, tid, in);
+        else adamw_values<kThreads, NT, NTG, gu16, 2>(t, ch.start, ch.count, a, tid, in);
+    } else {
+        if (wm == 0) adamw_values<kThreads, NT, NTG, gf32, 0>(t, ch.start, ch.count, a, tid, in);
+        else if (wm == 1) adamw_values<kThreads, NT, NTG, gf32, 1>(t, ch.start, ch.count, a, tid, in);
+        else adamw_values<kThreads, NT, NTG, gf32, 2>(t, ch.start, ch.count, a, tid, in);
+    }
+}
+
 // One chunk a block, from the last to the first, as grad_clip_kernel.
 template <bool NT, bool NTG>
 __global__ __launch_bounds__(kStepThreads) void adamw_kernel(
     const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
     StepArgs a) {
     __shared__ double sh[kStepThreads / kWave];
+    const auto in = [&] { return StepIn{norm_factor<kStepThreads>(a.nm, sh), *a.at}; };
     if (blockIdx.x == 0) {
-        const NormFactor f = norm_factor<kStepThreads>(a.nm, sh);
+        const StepIn si = in();
         if (threadIdx.x == 0) {
-            if (a.nm.n_part >= 0 && a.nm.norm) *a.nm.norm = f.norm;
-            if (f.finite) *a.step = a.at->t;
+            if (a.nm.n_part >= 0 && a.nm.norm) *a.nm.norm = si.f.norm;
+            if (si.f.finite) *a.step = si.at.t;
         }
     }
     if (n_chunks == 0) return;
-    const OptChunk ch = chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)];
-    const OptTensor &t = ten[ch.tensor];
-    const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
-    if (t.types & kOptGradBf16) {
-        if (wm == 0) adamw_chunk<NT, NTG, gu16, 0>(t, ch.start, ch.count, a, sh);
-        else if (wm == 1) adamw_chunk<NT, NTG, gu16, 1>(t, ch.start, ch.count, a, sh);
-        else adamw_chunk<NT, NTG, gu16, 2>(t, ch.start, ch.count, a, sh);
-    } else {
-        if (wm == 0) adamw_chunk<NT, NTG, gf32, 0>(t, ch.start, ch.count, a, sh);
-        else if (wm == 1) adamw_chunk<NT, NTG, gf32, 1>(t, ch.start, ch.count, a, sh);
-        else adamw_chunk<NT, NTG, gf32, 2>(t, ch.start, ch.count, a, sh);
+    adamw_chunk<kStepThreads, NT, NTG>(ten, chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], a,
+                                       threadIdx.x, in);
+}
+
+// A small list in one launch of one block, four teams of kOptThreads that
+// share its chunks: the squares, the norm, and then what is done with it.
+enum SoloOp { kSoloNorm, kSoloClip, kSoloStep };
+template <SoloOp kOp>
+__global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptTensor *__restrict__ ten,
+                                                            const OptChunk *__restrict__ chunks,
+                                                            int n_chunks, uint32_t types, StepArgs a) {
+    constexpr int kTeams = kSoloThreads / kOptThreads;
+    __shared__ double sh[kSoloThreads / kWave];
+    __shared__ OptStep at;
+    const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / kOptThreads);
+    const int tid = threadIdx.x % kOptThreads;
+    // by the one thread that also writes the step number, off the first wave
+    const bool last = threadIdx.x == kSoloThreads - 1;
+    if (kOp == kSoloStep && last) at = step_at(a.step, a.hp.beta1, a.hp.beta2);
+    double n = 0.0;
+    if (a.nm.n_part >= 0) {
+        double s = 0.0;
+        constexpr int kAtOnce = kOp == kSoloNorm ? kSoloNormChunks / kTeams : 4;
+        if (types & kOptListF32)
+            s += range_squares<kAtOnce, false, gf32>(ten, chunks, 0, n_chunks, team, kTeams, tid);
+        if (types & kOptListBf16)
+            s += range_squares<kAtOnce, false, gu16>(ten, chunks, 0, n_chunks, team, kTeams, tid);
+        n = sqrt(block_sum<kSoloThreads>(s, sh));
+    } else if (a.nm.norm) {
+        n = static_cast<double>(*a.nm.norm);
     }
+    __syncthreads();  // every gradient is read, and `at` written
+    const NormFactor f = factor_of(n, a.nm.max_norm);
+    if (a.nm.n_part >= 0 && a.nm.norm && threadIdx.x == 0) *a.nm.norm = f.norm;
+    if (kOp == kSoloStep && last && f.finite) *a.step = at.t;
+    if (kOp == kSoloClip)
+        for (int k = team; k < n_chunks; k += kTeams)
+            clip_chunk<false>(ten, chunks[k], tid, [&] { return f; });
+    if (kOp == kSoloStep)
+        for (int k = team; k < n_chunks; k += kTeams)
+            adamw_chunk<kOptThreads, false, false>(ten, chunks[k], a, tid, [&] { return StepIn{f, at}; });
 }
 
 // Writes a batch of a list's tensors, which come as kernel arguments (no host
@@ -433,6 +506,12 @@ hipError_t launch_tensor_list(const OptBatch &b, int count, OptTensor *ten, OptC
 }
 
 hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st) {
+    if (L.n_chunks <= kSoloNormChunks) {
+        ProfScope prof("grad_norm", st);
+        hipLaunchKernelGGL(solo_kernel<kSoloNorm>, dim3(1), dim3(kSoloThreads), 0, st, L.ten, L.chunks,
+                           L.n_chunks, L.g_types, StepArgs{nm, {}, nullptr, nullptr, nullptr});
+        return hipGetLastError();
+    }
     hipError_t e = launch_squares(L, nm, false, nullptr, 0.0, 0.0, nullptr, st);
     if (e != hipSuccess) return e;
     ProfScope prof("grad_norm", st);
@@ -441,6 +520,12 @@ hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st)
 }
 
 hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st) {
+    if (L.n_chunks <= kSoloClipChunks) {
+        ProfScope prof("grad_clip", st);
+        hipLaunchKernelGGL(solo_kernel<kSoloClip>, dim3(1), dim3(kSoloThreads), 0, st, L.ten, L.chunks,
+                           L.n_chunks, L.g_types, StepArgs{nm, {}, nullptr, nullptr, nullptr});
+        return hipGetLastError();
+    }
     if (nm.n_part >= 0) {
         hipError_t e = launch_squares(L, nm, true, nullptr, 0.0, 0.0, nullptr, st);
         if (e != hipSuccess) return e;
@@ -454,6 +539,12 @@ hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st)
 
 hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp, const float *lr,
                         int64_t *step, OptStep *at, hipStream_t st) {
+    if (L.n_chunks <= kSoloStepChunks) {
+        ProfScope prof("adamw", st);
+        hipLaunchKernelGGL(solo_kernel<kSoloStep>, dim3(1), dim3(kSoloThreads), 0, st, L.ten, L.chunks,
+                           L.n_chunks, L.g_types, StepArgs{nm, hp, lr, at, step});
+        return hipGetLastError();
+    }
     hipError_t e = launch_squares(L, nm, true, step, hp.beta1, hp.beta2, at, st);
     if (e != hipSuccess) return e;
     ProfScope prof("adamw", st);

@@ -715,6 +715,7 @@ class TensorList:
 
     def __init__(self, c, mem, tensors, device):
         self.c, self.mem, self.tensors, self.device = c, mem, tensors, device
+        self.ws_bytes = dstd_tensor_list_workspace_size(c)
 
 
 def _list_array(x, like, dev, dtypes, what):
@@ -792,25 +793,37 @@ def _scalar(x, dtype, dev, what):
 
 def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
     """(norm tensor or None, its pointer, workspace) of a call."""
-    torch = _torch()
     if norm is None:
         if norm_given:
             raise ValueError("norm_given needs the norm")
         if want_norm:
+            torch = _torch()
             norm = torch.empty(1, dtype=torch.float32, device=tl.device)
-    need = dstd_tensor_list_workspace_size(tl.c)
-    if ws is None or ws.numel() < need:
-        ws = workspace(need, tl.device)
-    return norm, None if norm is None else _scalar(norm, torch.float32, tl.device, "norm"), ws
+    if ws is None or ws.numel() < tl.ws_bytes:
+        ws = workspace(tl.ws_bytes, tl.device)
+    if norm is None:
+        return None, None, ws
+    return norm, _scalar(norm, _torch().float32, tl.device, "norm"), ws
+
+
+def _launch(tl: TensorList, name, fn, *args):
+    """One call on the list's device (launches go to the current one) and on
+    that device's current stream."""
+    torch = _torch()
+    dev = tl.device.index
+    stream = torch._C._cuda_getCurrentRawStream(dev)  # current_stream() builds an object: 2 us
+    if torch.cuda.current_device() == dev:
+        _check(name, fn(*args, stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(name, fn(*args, stream))
 
 
 def grad_norm(tl: TensorList, norm=None, ws=None):
     """L2 norm of all gradients of the list together, as a device tensor [1]
     (written to `norm` if given)."""
     norm, ptr, ws = _optim_args(tl, norm, False, ws, True)
-    with _torch().cuda.device(tl.device):
-        _check("dstd_grad_norm",
-               dstd_grad_norm(tl.c, ptr, _ptr(ws), ws.numel(), _stream(tl.device)))
+    _launch(tl, "dstd_grad_norm", dstd_grad_norm, tl.c, ptr, _ptr(ws), ws.numel())
     return norm
 
 
@@ -819,10 +832,8 @@ def grad_clip(tl: TensorList, max_norm: float, norm=None, norm_given: bool = Fal
     into the list's outputs; returns the norm before clipping, a device tensor
     [1]. With norm_given, `norm` is the norm to clip by."""
     norm, ptr, ws = _optim_args(tl, norm, norm_given, ws, True)
-    with _torch().cuda.device(tl.device):
-        _check("dstd_grad_clip",
-               dstd_grad_clip(tl.c, float(max_norm), ptr, 1 if norm_given else 0, _ptr(ws),
-                              ws.numel(), _stream(tl.device)))
+    _launch(tl, "dstd_grad_clip", dstd_grad_clip, tl.c, float(max_norm), ptr,
+            1 if norm_given else 0, _ptr(ws), ws.numel())
     return norm
 
 
@@ -839,11 +850,10 @@ def adamw_step(tl: TensorList, hp: dstd_adamw_params, step, lr=None, norm=None,
     up; `lr` [1] f32 on the device replaces hp.lr. Returns the norm before
     clipping (None where none is formed: no `norm` given and hp.max_norm infinite);
     a step whose norm is not finite changes nothing."""
-    torch = _torch()
     norm, ptr, ws = _optim_args(tl, norm, norm_given, ws, math.isfinite(hp.max_norm))
-    with torch.cuda.device(tl.device):
-        _check("dstd_adamw_step",
-               dstd_adamw_step(tl.c, hp, None if lr is None else _scalar(lr, torch.float32, tl.device, "lr"),
-                               _scalar(step, torch.int64, tl.device, "step"), ptr,
-                               1 if norm_given else 0, _ptr(ws), ws.numel(), _stream(tl.device)))
+    torch = _torch()
+    _launch(tl, "dstd_adamw_step", dstd_adamw_step, tl.c, hp,
+            None if lr is None else _scalar(lr, torch.float32, tl.device, "lr"),
+            _scalar(step, torch.int64, tl.device, "step"), ptr, 1 if norm_given else 0, _ptr(ws),
+            ws.numel())
     return norm
