@@ -11,7 +11,9 @@ Prints ONE JSON line (rank 0) with the throughput in samples/s, the roofline
 of the dominant kernel (timed with the library's hipEvent timer on the stream
 the kernels run on) and the fp64 CPU oracle timed on the host as a baseline.
 
-  python bench.py [--steps K] [--warmup W] [--workload conv9] [--no-configs]
+  python bench.py [--steps K] [--warmup W] [--workload conv9] [--no-configs] [--optimizer]
+
+With --optimizer a step also updates all weights (AdamW, gradients clipped).
 """
 from __future__ import annotations
 
@@ -56,7 +58,7 @@ def kernel_source_sha():
 class Net:
     """Preallocated buffers and raw C-ABI calls for one workload."""
 
-    def __init__(self, wl, dev, contract="auto"):
+    def __init__(self, wl, dev, contract="auto", optimizer=None):
         import torch
         from paper_2607_14672_amd import dstd, workloads
         self.torch, self.dstd, self.wl, self.dev = torch, dstd, wl, dev
@@ -139,6 +141,30 @@ class Net:
         else:
             self.targets = torch.from_numpy(d.targets).to(dev)
         self.loss = torch.empty((B + 1,), dtype=torch.float32, device=dev)  # total, per sample
+        self.opt = None
+        if optimizer is not None:
+            self._init_optimizer(optimizer)
+
+    def _init_optimizer(self, hp):
+        """The weights' moments (and fp32 copies of bf16 weights), the list of
+        them all with their gradients, and what an AdamW step with constants
+        `hp` reads and writes on the device."""
+        torch, ds, dev = self.torch, self.dstd, self.dev
+        W, gW = [e["W"] for e in self.L], [e["gW"] for e in self.L]
+        m, v = ([torch.zeros(w.shape, device=dev) for w in W] for _ in range(2))
+        w32 = [w.float() if w.dtype == torch.bfloat16 else None for w in W]
+        tl = ds.make_tensor_list(gW, weights=W, m=m, v=v, master=w32)
+        self.opt = dict(hp=hp, list=tl, m=m, v=v, w32=w32,
+                        lr=torch.full((1,), hp.lr, device=dev),
+                        steps=torch.zeros(1, dtype=torch.int64, device=dev),
+                        norm=torch.zeros(1, device=dev), ws=ds.workspace(tl.ws_bytes, dev))
+
+    def update(self):
+        """One AdamW step on the gradients in place, clipped to hp.max_norm."""
+        o = self.opt
+        self._ck("dstd_adamw_step", self.dstd.dstd_adamw_step(
+            o["list"].c, o["hp"], o["lr"].data_ptr(), o["steps"].data_ptr(), o["norm"].data_ptr(), 0,
+            o["ws"].data_ptr(), o["ws"].numel(), self.stream))
 
     def _ck(self, name, st):
         if st != 0:
@@ -216,6 +242,8 @@ class Net:
         self.forward()
         self.loss_grad()
         self.backward()
+        if self.opt is not None:
+            self.update()
 
     def capture(self, warmup=3):
         """Record one whole step into a HIP graph (the library's calls are
@@ -628,6 +656,8 @@ def main():
     ap.add_argument("--eager", action="store_true",
                     help="launch every kernel from Python each step instead of replaying a "
                          "HIP graph of the step")
+    ap.add_argument("--optimizer", action="store_true",
+                    help="end each step with a clipped AdamW update of all weights (max_norm 1)")
     ap.add_argument("--layer-profile", action="store_true",
                     help="add per-layer kernel times to the detail section")
     ap.add_argument("--copy-probe", action="store_true",
@@ -665,8 +695,9 @@ def main():
                           "rows": multispike_bench(torch, dstd, dev)}), flush=True)
         return
     wl = workloads.get(args.workload)
+    hp = dstd.make_adamw(max_norm=1.0) if args.optimizer else None
     head = measure(torch, dstd, wl, dev, args.steps, args.warmup, args.profile_steps, args.eager,
-                   args.contract)
+                   args.contract, hp)
     net = head.pop("net")
 
     if args.copy_probe:
@@ -683,7 +714,7 @@ def main():
     if not args.no_configs:
         for name in [x for x in args.configs.split(",") if x and x != args.workload]:
             r = measure(torch, dstd, workloads.get(name), dev, args.config_steps,
-                        max(3, args.config_steps // 5), 5, args.eager, args.contract)
+                        max(3, args.config_steps // 5), 5, args.eager, args.contract, hp)
             r.pop("net")
             others.append(dict(workload=name, description=workloads.get(name).description,
                                batch=workloads.get(name).batch, value=r["value"], unit="samples/s",
@@ -703,7 +734,8 @@ def main():
         "config": {"workload": wl.description, "name": wl.name, "global_batch": wl.batch,
                    "layers": [layer_desc(lay) for lay in wl.layers],
                    "parallelism": "single GPU",
-                   "execution": "eager launches" if args.eager else "HIP graph of the step"},
+                   "execution": "eager launches" if args.eager else "HIP graph of the step",
+                   **({"optimizer": "AdamW, gradients clipped to norm 1"} if hp else {})},
         "roofline": head["roofline"],
         "roofline_mfma": head["roofline_mfma"],
         "cpu_baseline": cpu,
@@ -716,12 +748,12 @@ def main():
     print(json.dumps(out), flush=True)
 
 
-def measure(torch, dstd, wl, dev, steps, warmup, profile_steps, eager, contract="auto"):
+def measure(torch, dstd, wl, dev, steps, warmup, profile_steps, eager, contract="auto", hp=None):
     """Time `steps` whole training steps of workload `wl` (HIP graph replays
     unless eager), then one profiling pass with the library's hipEvent timer:
     samples/s, per-kernel ms per step, the dominant kernel's roofline and the
     HBM rate of the bandwidth-bound kernels that have committed counters."""
-    net = Net(wl, dev, contract)
+    net = Net(wl, dev, contract, hp)
     run = net.step
     if not eager:
         graph = net.capture()

@@ -724,7 +724,7 @@ def _list_array(x, like, dev, dtypes, what):
         raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
     if x.dtype not in dtypes:
         raise TypeError(f"{what} must be one of {dtypes}, got {x.dtype}")
-    if not x.is_cuda or x.device != dev:
+    if dev < 0 or x.get_device() != dev:
         raise ValueError(f"{what} must live on the GPU of the list's other tensors")
     if x.shape != like.shape:
         raise ValueError(f"{what} has shape {tuple(x.shape)}, its gradient {tuple(like.shape)}")
@@ -760,7 +760,7 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
               ((lr_scale, "learning-rate factors"), (decay_scale, "decay factors"))]
     if n == 0:
         raise ValueError("a list needs a tensor")
-    dev = getattr(grads[0], "device", None)
+    dev = grads[0].get_device() if isinstance(grads[0], torch.Tensor) else -1
     arr = (dstd_tensor * n)()
     for k, (t, g) in enumerate(zip(arr, grads)):
         t.g = _list_array(g, g, dev, both, f"gradient {k}")
@@ -777,12 +777,13 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
         if o is not None:
             t.out, t.out_dtype = _list_array(o, g, dev, both, f"output {k}"), _wdtype(o)
         t.lr_scale, t.decay_scale = (float(s[k]) for s in scales)
-    mem = workspace(dstd_tensor_list_size(n, arr), dev)
+    device = torch.device("cuda", dev)
+    mem = workspace(dstd_tensor_list_size(n, arr), device)
     c = dstd_tensor_list()
-    with torch.cuda.device(dev):
+    with torch.cuda.device(device):
         _check("dstd_tensor_list_build",
-               dstd_tensor_list_build(n, arr, _ptr(mem), mem.numel(), c, _stream(dev)))
-    return TensorList(c, mem, (grads, *cols), dev)
+               dstd_tensor_list_build(n, arr, _ptr(mem), mem.numel(), c, _stream(device)))
+    return TensorList(c, mem, (grads, *cols), device)
 
 
 def _scalar(x, dtype, dev, what):

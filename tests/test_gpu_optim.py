@@ -538,3 +538,76 @@ def test_refusals_of_the_helpers(dev):
     with pytest.raises(ValueError, match="lr"):
         dstd.adamw_step(tl, dstd.make_adamw(), torch.zeros(1, dtype=torch.int64, device=dev),
                         lr=torch.zeros(2, device=dev))
+
+
+# ------------------------------------------------------------ all together --
+def _workload(name, batch):
+    """The named workload, or a small conv net of non-leaky neurons (whose
+    potential stays: every layer fires)."""
+    from paper_2607_14672_amd import workloads
+    if name != "small-conv":
+        return workloads.with_batch(workloads.get(name), batch)
+    inf, M = math.inf, 16
+    L = [workloads._conv_layer(1, 3, 12, 12, 8, M, inf, inf),
+         workloads._conv_layer(2, 8, 12, 12, 12, M, inf, inf, pool_in=2),
+         workloads._conv_layer(3, 12, 6, 6, 20, M, inf, inf, stride=2),
+         workloads.LayerSpec("dense", 20 * 3 * 3, 10, M, 3.0, 1.0 / M, inf, inf)]
+    return workloads.Workload(name, batch, L, "one_minus_u", seed=7, extra={"k": [2.0] * 4})
+
+
+# (the 20-layer net's last layers are silent at its initial weights: no gradient
+# anywhere, and the step is the decay alone)
+@pytest.mark.parametrize("name,batch", [("mlp3", 16), ("small-conv", 5), ("conv20", 2), ("wide-M8", 4)])
+def test_training_steps_eager_and_captured(dev, name, batch):
+    """Whole training steps: every layer's forward and backward, the loss, and a
+    clipped AdamW step of all weights. Each eager step's update follows the
+    formula from the gradients it was given; a captured step, replayed with eager
+    work between, reaches the same bits."""
+    import bench
+    import torch
+    from paper_2607_14672_amd import dstd
+    hp = dstd.make_adamw(lr=1e-3, max_norm=0.01, **HP)
+    wl = _workload(name, batch)
+    a, b = bench.Net(wl, dev, optimizer=hp), bench.Net(wl, dev, optimizer=hp)
+
+    def weights(net):
+        return [e["W"] if w is None else w for e, w in zip(net.L, net.opt["w32"])]
+
+    def f64(ts):
+        return [t.double().cpu().numpy().reshape(-1) for t in ts]
+
+    losses = []
+    for k in range(3):
+        w, m, v = f64(weights(a)), f64(a.opt["m"]), f64(a.opt["v"])
+        a.step()
+        torch.cuda.synchronize()
+        g = f64(e["gW"] for e in a.L)
+        ref = _norm64(g)
+        fires = bool((a.L[-1]["q"] >= 0).any())
+        assert (ref > 0.0) == fires == (name != "conv20")
+        _close(a.opt["norm"].cpu().numpy(), [ref], [U * MORE * ref], "norm")
+        c = min(1.0, 0.01 / ref) if fires else 1.0
+        for i, (w1, m1, v1) in enumerate(zip(f64(weights(a)), f64(a.opt["m"]), f64(a.opt["v"]))):
+            want, err = _adamw64(g[i], w[i], m[i], v[i], k + 1, HP, c, 1e-3)
+            # products of tiny gradients leave the normal range of fp32: each of
+            # the at most four of them is off by half of 2^-149
+            for got, x, e, what in zip((w1, m1, v1), want, err, "wmv"):
+                _close(got, x, e + (0.0 if what == "w" else 2.0 ** -148), f"{what} of layer {i}")
+        losses.append(a.loss[0].item())
+        assert a.opt["steps"].item() == k + 1
+    assert name == "conv20" or len(set(losses)) > 1  # the steps act on the next forward
+
+    b.step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.stream = torch.cuda.current_stream(dev).cuda_stream
+        b.step()
+    for k in range(2):
+        graph.replay()
+        dstd.grad_norm(b.opt["list"])  # eager work between the replays
+        torch.cuda.synchronize()
+        assert b.loss[0].item() == losses[k + 1]
+    for x, y in zip(weights(a) + a.opt["m"] + a.opt["v"], weights(b) + b.opt["m"] + b.opt["v"]):
+        assert torch.equal(x, y)
+    assert torch.equal(a.opt["norm"], b.opt["norm"]) and b.opt["steps"].item() == 3
