@@ -545,9 +545,9 @@ typedef struct {
  */
 typedef struct {
     const void *mem;
-    int64_t n_tensors, n_chunks, n_elems;
+    int64_t n_tensors, n_chunks;
     int64_t g_bytes, out_bytes, w_bytes;
-    uint32_t magic, has_weights, g_types, reserved;
+    uint32_t magic, has_weights, g_types;
 } dstd_tensor_list;
 
 /* Bytes of device memory that a list of these tensors needs (only their n

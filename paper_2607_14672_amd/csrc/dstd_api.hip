@@ -1054,22 +1054,20 @@ int64_t dtype_bytes(int32_t t) { return t == DSTD_BF16 ? 2 : 4; }
 // 2^32 threads.
 constexpr int64_t kMaxChunks = (int64_t)1 << 23;
 
-// chunks and elements of the whole list
-dstd_status check_counts(int64_t n, const dstd_tensor *t, int64_t *n_chunks, int64_t *n_elems) {
+// chunks of the whole list
+dstd_status check_counts(int64_t n, const dstd_tensor *t, int64_t *n_chunks) {
     if (n < 0) return fail(DSTD_ERR_SHAPE, "n_tensors must be >= 0");
     if (n > 0 && !t) return fail(DSTD_ERR_NULL, "tensors is NULL");
     if (n >= (int64_t)1 << 31) return fail(DSTD_ERR_SHAPE, "too many tensors");
-    int64_t c = 0, e = 0;
+    int64_t c = 0;
     for (int64_t k = 0; k < n; ++k) {
         if (t[k].n < 0 || t[k].n >= kMaxChunks * dstd::kOptChunk)
             return fail(DSTD_ERR_SHAPE, "tensor %lld: n = %lld must be in [0, 2^35)", (long long)k,
                         (long long)t[k].n);
         c += (t[k].n + dstd::kOptChunk - 1) / dstd::kOptChunk;
-        e += t[k].n;
         if (c >= kMaxChunks) return fail(DSTD_ERR_SHAPE, "the list's tensors are too large together");
     }
     *n_chunks = c;
-    *n_elems = e;
     return DSTD_OK;
 }
 
@@ -1164,15 +1162,15 @@ dstd_status check_norm(const float *norm, int32_t norm_given) {
 extern "C" {
 
 size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors) {
-    int64_t nc, ne;
-    if (check_counts(n_tensors, tensors, &nc, &ne) != DSTD_OK) return 0;
+    int64_t nc;
+    if (check_counts(n_tensors, tensors, &nc) != DSTD_OK) return 0;
     return list_bytes(n_tensors, nc);
 }
 
 dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
                                    size_t mem_bytes, dstd_tensor_list *list, void *stream) try {
-    int64_t nc, ne;
-    dstd_status s = check_counts(n_tensors, tensors, &nc, &ne);
+    int64_t nc;
+    dstd_status s = check_counts(n_tensors, tensors, &nc);
     if (s != DSTD_OK) return s;
     if (!list) return fail(DSTD_ERR_NULL, "list is NULL");
     const size_t need = list_bytes(n_tensors, nc);
@@ -1223,7 +1221,7 @@ dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors
         hipError_t e = dstd::launch_tensor_list(b, count, ten, chunks, static_cast<hipStream_t>(stream));
         if (e != hipSuccess) return hip_status(e, "tensor list launch");
     }
-    *list = dstd_tensor_list{mem, n_tensors, nc, ne, gb, ob, wb, kListMagic, has_weights, types, 0};
+    *list = dstd_tensor_list{mem, n_tensors, nc, gb, ob, wb, kListMagic, has_weights, types};
     return DSTD_OK;
 } catch (const std::exception &e) {
     return fail(DSTD_ERR_UNSUPPORTED, "tensor list: %s", e.what());

@@ -15,8 +15,6 @@
 // launch sums the squares of a fixed set of chunks per block (partials), and
 // the launch that follows adds the partials again in every block, in a fixed
 // order, rather than in a launch of its own.
-#include <limits.h>
-
 #include "dstd_internal.h"
 #include "dstd_kernels.h"
 #include "dstd_profile.h"
@@ -34,12 +32,12 @@ constexpr int kOptThreads = 256;
 constexpr int kStepThreads = 512;
 // Lists of up to so many chunks take one launch of one block: a pass is then
 // bound by what the host spends on a launch (3.6 us), and two launches cost
-// 7.5 us (an AdamW step 8.5) whatever such a list holds. One block takes 4.0 us
-// for the norm of 1 chunk, 6.2 for 20 (one round of reads) and 8.4 for 24;
-// clipping 4.5 us for 1, 7.1 for 6, 7.8 for 8; a step 6.4 us for 1, 7.5 for 2,
-// 10.6 for 4.
+// 7.6 us (an AdamW step 8.5) whatever such a list holds. One block takes 4.1 us
+// for the norm of 1 chunk, 6.3 for 20 (one round of reads) and 8.4 for 24;
+// clipping 4.3 us for 1, 7.2 for 8, 8.0 for 10; a step 6.1 us for 1, 8.1 for 3,
+// 9.4 for 4.
 constexpr int kSoloThreads = 1024;
-constexpr int kSoloNormChunks = 20, kSoloClipChunks = 6, kSoloStepChunks = 2;
+constexpr int kSoloNormChunks = 20, kSoloClipChunks = 8, kSoloStepChunks = 3;
 template <int kThreads> constexpr int kVecs = static_cast<int>(kOptChunk) / (kThreads * 4);
 constexpr int kOptGroups = kVecs<kOptThreads>;
 
@@ -300,7 +298,6 @@ __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
         const NormFactor f = factor();
         if (threadIdx.x == 0) *nm.norm = f.norm;
     }
-    if (n_chunks == 0) return;
     clip_chunk<NT>(ten, chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], threadIdx.x, factor);
 }
 
@@ -351,6 +348,13 @@ __device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, 
         mx[i] = load4<NT>(m + e);
         vx[i] = load4<NT>(v + e);
     }
+    float g1 = 0.f, w1 = 0.f, m1 = 0.f, v1 = 0.f;  // of the elements behind the last vector
+    if (e1 < count) {
+        g1 = load1(g + e1);
+        w1 = (WM == 1) ? load1(wh + e1) : wf[e1];
+        m1 = m[e1];
+        v1 = v[e1];
+    }
     const StepIn si = in();
     if (!si.f.finite) return;  // the step is skipped
     const float rate = a.lr ? *a.lr : a.hp.lr;
@@ -364,11 +368,11 @@ __device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, 
         if (WM == 1) wx[i] = widen(hx[i]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            float w1 = wx[i][k], m1 = mx[i][k], v1 = vx[i][k];
-            adamw_one(q, g4[k], w1, m1, v1);
-            wx[i][k] = w1;
-            mx[i][k] = m1;
-            vx[i][k] = v1;
+            float wk = wx[i][k], mk = mx[i][k], vk = vx[i][k];
+            adamw_one(q, g4[k], wk, mk, vk);
+            wx[i][k] = wk;
+            mx[i][k] = mk;
+            vx[i][k] = vk;
         }
         store4<NT>(m + e, mx[i]);
         store4<NT>(v + e, vx[i]);
@@ -376,8 +380,7 @@ __device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, 
         if (WM != 0) store4<NT>(wh + e, wx[i]);
     }
     if (e1 < count) {
-        float w1 = (WM == 1) ? load1(wh + e1) : wf[e1], m1 = m[e1], v1 = v[e1];
-        adamw_one(q, load1(g + e1), w1, m1, v1);
+        adamw_one(q, g1, w1, m1, v1);
         m[e1] = m1;
         v[e1] = v1;
         if (WM != 1) wf[e1] = w1;
@@ -415,7 +418,6 @@ __global__ __launch_bounds__(kStepThreads) void adamw_kernel(
             if (si.f.finite) *a.step = si.at.t;
         }
     }
-    if (n_chunks == 0) return;
     adamw_chunk<kStepThreads, NT, NTG>(ten, chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], a,
                                        threadIdx.x, in);
 }
@@ -423,6 +425,7 @@ __global__ __launch_bounds__(kStepThreads) void adamw_kernel(
 // A small list in one launch of one block, four teams of kOptThreads that
 // share its chunks: the squares, the norm, and then what is done with it.
 enum SoloOp { kSoloNorm, kSoloClip, kSoloStep };
+constexpr int kSoloChunks[] = {kSoloNormChunks, kSoloClipChunks, kSoloStepChunks};
 template <SoloOp kOp>
 __global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptTensor *__restrict__ ten,
                                                             const OptChunk *__restrict__ chunks,
@@ -438,7 +441,7 @@ __global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptTensor *__r
     double n = 0.0;
     if (a.nm.n_part >= 0) {
         double s = 0.0;
-        constexpr int kAtOnce = kOp == kSoloNorm ? kSoloNormChunks / kTeams : 4;
+        constexpr int kAtOnce = (kSoloChunks[kOp] + kTeams - 1) / kTeams;  // one round of reads
         if (types & kOptListF32)
             s += range_squares<kAtOnce, false, gf32>(ten, chunks, 0, n_chunks, team, kTeams, tid);
         if (types & kOptListBf16)
@@ -474,10 +477,17 @@ __global__ __launch_bounds__(kOptThreads) void tensor_list_kernel(OptBatch b, Op
     }
 }
 
-int opt_blocks(int n_chunks, int most = INT_MAX) { return n_chunks < 1 ? 1 : n_chunks < most ? n_chunks : most; }
-
-// Bytes that stay in the last cache level (256 MB) from one launch to the next.
+// Which accesses are marked non-temporal, for a last cache level of 256 MB.
+// Gradients of up to kOptCached bytes, or the last so many, stay there from the
+// norm's launch to the one that scales them (201 M weights: a step takes 1061 us
+// with 240 MB, 1067 with 200, 1079 with 160 and 1175 if no read is marked).
+// What a step or a clip writes stays there for the next one only if the list
+// leaves room for all that runs between: lists beyond kOptKept bytes are
+// streamed (three lists in turn, 4 / 6 / 8 M weights of 16 bytes each: 22 / 36 /
+// 50 us kept, 25 / 36 / 44 streamed; one list alone 22 / 32 / 40 kept, 24 / 35 /
+// 43 streamed).
 constexpr int64_t kOptCached = 240 << 20;
+constexpr int64_t kOptKept = 96 << 20;
 
 // `scaled`: a launch that reads the gradients again follows
 hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, const int64_t *step,
@@ -495,7 +505,7 @@ hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, cons
 
 }  // namespace
 
-int opt_norm_blocks(int n_chunks) { return opt_blocks(n_chunks, kOptMaxPart); }
+int opt_norm_blocks(int n_chunks) { return n_chunks < kOptMaxPart ? n_chunks : kOptMaxPart; }
 
 hipError_t launch_tensor_list(const OptBatch &b, int count, OptTensor *ten, OptChunk *chunks,
                               hipStream_t st) {
@@ -531,8 +541,8 @@ hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st)
         if (e != hipSuccess) return e;
     }
     ProfScope prof("grad_clip", st);
-    const auto kernel = L.g_bytes + L.out_bytes > kOptCached ? grad_clip_kernel<true> : grad_clip_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks)), dim3(kOptThreads), 0, st, L.ten,
+    const auto kernel = L.g_bytes + L.out_bytes > kOptKept ? grad_clip_kernel<true> : grad_clip_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(L.n_chunks)), dim3(kOptThreads), 0, st, L.ten,
                        L.chunks, L.n_chunks, nm);
     return hipGetLastError();
 }
@@ -549,9 +559,9 @@ hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp,
     if (e != hipSuccess) return e;
     ProfScope prof("adamw", st);
     const auto kernel = L.g_bytes > kOptCached             ? adamw_kernel<true, true>
-                        : L.g_bytes + L.w_bytes > kOptCached ? adamw_kernel<true, false>
+                        : L.g_bytes + L.w_bytes > kOptKept ? adamw_kernel<true, false>
                                                              : adamw_kernel<false, false>;
-    hipLaunchKernelGGL(kernel, dim3(opt_blocks(L.n_chunks)), dim3(kStepThreads), 0, st, L.ten,
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(L.n_chunks)), dim3(kStepThreads), 0, st, L.ten,
                        L.chunks, L.n_chunks, StepArgs{nm, hp, lr, at, step});
     return hipGetLastError();
 }

@@ -58,9 +58,8 @@ class dstd_tensor(C.Structure):
 
 class dstd_tensor_list(C.Structure):
     _fields_ = [("mem", C.c_void_p), ("n_tensors", C.c_int64), ("n_chunks", C.c_int64),
-                ("n_elems", C.c_int64), ("g_bytes", C.c_int64), ("out_bytes", C.c_int64),
-                ("w_bytes", C.c_int64), ("magic", C.c_uint32), ("has_weights", C.c_uint32),
-                ("g_types", C.c_uint32), ("reserved", C.c_uint32)]
+                ("g_bytes", C.c_int64), ("out_bytes", C.c_int64), ("w_bytes", C.c_int64),
+                ("magic", C.c_uint32), ("has_weights", C.c_uint32), ("g_types", C.c_uint32)]
 
 
 class dstd_adamw_params(C.Structure):
