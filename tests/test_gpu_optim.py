@@ -36,6 +36,11 @@ SIZES = {
     "few": [2, 3, 5, 7, 11],
     "tiny": [1 + k % 9 for k in range(700)],      # more than one batch of tensors
     "long": [1_300_003, 4096 * 1024, 77],          # more chunks than partial sums
+    # the most chunks of 4096 that a step, a clip and a norm take in one launch
+    # of one block, and one element more
+    "step": [3 * 4096], "step+": [4096, 8193],
+    "clip": [8 * 4096], "clip+": [8 * 4096 + 1],
+    "norm": [5 * 4096, 15 * 4096], "norm+": [20 * 4096 + 1],
 }
 
 
@@ -271,14 +276,14 @@ def _adamw64(g, w, m, v, t, hp, c, lr, ls=1.0, ds=1.0):
     g = g * c
     m1 = hp["beta1"] * m + (1 - hp["beta1"]) * g
     v1 = hp["beta2"] * v + (1 - hp["beta2"]) * g * g
-    em = U * (2 * hp["beta1"] * np.abs(m) + 5 * (1 - hp["beta1"]) * np.abs(g))
+    em = U * (2 * hp["beta1"] * abs(m) + 5 * (1 - hp["beta1"]) * abs(g))
     ev = U * 8 * v1
     c1, c2 = 1 / (1 - hp["beta1"] ** t), 1 / (1 - hp["beta2"] ** t)
-    den = np.sqrt(v1 * c2) + hp["eps"]
+    den = (v1 * c2) ** 0.5 + hp["eps"]
     step = m1 * c1 / den
     rate, decay = lr * ls, hp["weight_decay"] * ds
     w1 = w - rate * (step + decay * w)
-    ew = rate * (em * c1 / den + 15 * U * np.abs(step) + 6 * U * decay * np.abs(w)) + U * np.abs(w1)
+    ew = rate * (em * c1 / den + 15 * U * abs(step) + 6 * U * decay * abs(w)) + U * abs(w1)
     return (w1, m1, v1), (MORE * ew, MORE * em, MORE * ev)
 
 
@@ -423,7 +428,112 @@ def test_adamw_by_a_given_norm(dev):
     _check_step(tr, before, 1, HP, 0.25, 1e-3)
 
 
+def test_mixed_types_in_one_list(dev):
+    """Gradients, weights and outputs of both types side by side, in a list for
+    one block and in one for many."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    for scale in (1, 40):
+        rng = np.random.default_rng(11)
+        kinds = [(g, w, ms) for g in ("f32", "bf16") for w, ms in (("f32", False), ("bf16", False), ("bf16", True))]
+        sizes = [scale * (301 + 97 * k) for k in range(len(kinds))]
+        vals = [_normal(rng, sizes, sc) for sc in (0.02, 0.3, 0.01, 0.02)]
+
+        def put(v, t):
+            return torch.from_numpy(v).to(dev).to(_dt(t))
+
+        g = [put(v, k[0]) for v, k in zip(vals[0], kinds)]
+        w = [put(v, k[1]) for v, k in zip(vals[1], kinds)]
+        w32 = [put(v, "f32") if k[2] else None for v, k in zip(vals[1], kinds)]
+        m = [put(v, "f32") for v in vals[2]]
+        v2 = [put(v * v, "f32") for v in vals[3]]
+        out = [None if k[2] else torch.zeros_like(x, dtype=_dt("bf16" if k[0] == "f32" else "f32"))
+               for x, k in zip(g, kinds)]
+        tl = dstd.make_tensor_list(g, weights=w, m=m, v=v2, master=w32, out=out)
+
+        def f64(x):
+            return x.double().cpu().numpy()
+
+        g0, m0, v0 = ([f64(x) for x in c] for c in (g, m, v2))
+        w0 = [f64(a if b is None else b) for a, b in zip(w, w32)]
+        ref = _norm64(g0)
+        step = torch.full((1,), 4, dtype=torch.int64, device=dev)
+        norm = dstd.adamw_step(tl, dstd.make_adamw(lr=1e-3, max_norm=0.5 * ref, **HP), step)
+        _close(norm.cpu().numpy(), [ref], [U * MORE * ref], "norm")
+        for k, (gt, wt, ms) in enumerate(kinds):
+            want, err = _adamw64(g0[k], w0[k], m0[k], v0[k], 5, HP, 0.5, 1e-3)
+            more = U16 * MORE * abs(want[0]) if wt == "bf16" and not ms else 0.0
+            _close(f64(w32[k] if ms else w[k]), want[0], err[0] + more, f"w of {kinds[k]}")
+            _close(f64(m[k]), want[1], err[1], f"m of {kinds[k]}")
+            _close(f64(v2[k]), want[2], err[2], f"v of {kinds[k]}")
+        dstd.grad_clip(tl, 0.25 * ref)
+        for k, (gt, wt, ms) in enumerate(kinds):
+            got = f64(g[k] if ms else out[k])
+            half = U16 if (gt == "bf16") == ms else 0.0  # in place, or into the other type
+            _close(got, 0.25 * g0[k], abs(0.25 * g0[k]) * MORE * (2 * U + half), f"clip of {kinds[k]}")
+
+
+def _gpu_close(got, ref, bound, what):
+    bad = int((~((got.double() - ref).abs() <= bound)).sum())
+    assert bad == 0, f"{what}: {bad} of {ref.numel()} beyond their bound"
+
+
+# lists past the sizes from which their accesses are streamed: of all arrays
+# (96 MB), and of the gradients alone (240 MB)
+@pytest.mark.parametrize("n,g_type", [(7_000_001, "f32"), (66_000_003, "f32"), (130_000_001, "bf16")])
+def test_lists_that_exceed_the_caches(dev, n, g_type):
+    import torch
+    from paper_2607_14672_amd import dstd
+    torch.manual_seed(12)
+    cut = n // 3 | 1  # the second tensor starts off every alignment
+    flat = {k: torch.randn(n, device=dev) for k in "gwm"}
+    flat["g"] = flat["g"].to(_dt(g_type))
+    flat["v"] = torch.rand(n, device=dev)
+    parts = {k: [x[:cut], x[cut:]] for k, x in flat.items()}
+    out = [torch.empty_like(x, dtype=torch.bfloat16) for x in parts["g"]]
+    tl = dstd.make_tensor_list(parts["g"], weights=parts["w"], m=parts["m"], v=parts["v"], out=out)
+    old = {k: x.clone() for k, x in flat.items()}
+    g = old["g"].double()
+    ref = float(g.square().sum().sqrt())
+    norm = dstd.grad_norm(tl).item()
+    _close([norm], [ref], [U * MORE * ref], "norm")
+    dstd.grad_clip(tl, 0.5 * ref)
+    for i, sl in ((0, slice(0, cut)), (1, slice(cut, None))):
+        _gpu_close(out[i], 0.5 * g[sl], 0.5 * g[sl].abs() * MORE * (2 * U + U16), "clipped")
+    step = torch.full((1,), 2, dtype=torch.int64, device=dev)
+    dstd.adamw_step(tl, dstd.make_adamw(lr=1e-3, max_norm=0.5 * ref, **HP), step)
+    for i in range(0, n, 33_000_000):  # the reference a part at a time
+        sl = slice(i, min(n, i + 33_000_000))
+        want, err = _adamw64(g[sl], *(old[k][sl].double() for k in "wmv"), 3, HP, 0.5, 1e-3)
+        for k, x, e in zip("wmv", want, err):
+            _gpu_close(flat[k][sl], x, e, k)
+    assert torch.equal(flat["g"], old["g"]) and step.item() == 3
+    # in place, the last of all
+    tl = dstd.make_tensor_list(parts["g"])
+    dstd.grad_clip(tl, 0.5 * ref)
+    half = U16 if g_type == "bf16" else 0.0
+    _gpu_close(flat["g"], 0.5 * g, 0.5 * g.abs() * MORE * (2 * U + half), "clipped in place")
+
+
 # --------------------------------------------------- streams, graphs, lists --
+def test_one_list_on_two_streams_at_once(dev):
+    """Norms of one list on two streams, each with its workspace."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    g = Arena(_normal(np.random.default_rng(13), [900_001, 50]), "f32", 1, dev)
+    tl = dstd.make_tensor_list(g.t)
+    ref = dstd.grad_norm(tl)
+    streams = [torch.cuda.Stream(dev) for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for st in streams:
+            with torch.cuda.stream(st):
+                got.append(dstd.grad_norm(tl))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, ref) for x in got)
+
+
 def test_other_streams_and_two_lists_at_once(dev):
     """Each list on a stream of its own, with its own workspace, gives the bits
     that one after the other on the default stream gives."""
@@ -448,7 +558,8 @@ def test_other_streams_and_two_lists_at_once(dev):
     assert all(torch.equal(a, b) for a, b in zip(steps(False), steps(True)))
 
 
-def test_graph_replays_match_eager(dev):
+@pytest.mark.parametrize("sizes", [[70_000, 4097, 1], [5000, 7]])
+def test_graph_replays_match_eager(dev, sizes):
     """A captured step, replayed between eager work, does what eager calls do:
     its step number and learning rate are read at each replay. Two graphs share
     a list and a workspace."""
@@ -457,7 +568,7 @@ def test_graph_replays_match_eager(dev):
     hp = dstd.make_adamw(max_norm=0.7, **HP)
 
     def fresh():
-        tr = Train(dev, [70_000, 4097, 1], "f32", "bf16", True, seed=9)
+        tr = Train(dev, sizes, "f32", "bf16", True, seed=9)
         return dict(tr=tr, step=torch.zeros(1, dtype=torch.int64, device=dev),
                     lr=torch.full((1,), 1e-3, device=dev), norm=torch.zeros(1, device=dev),
                     ws=dstd.workspace(dstd.dstd_tensor_list_workspace_size(tr.tl.c), dev))
