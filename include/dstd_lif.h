@@ -550,8 +550,9 @@ typedef struct {
     uint32_t magic, has_weights, g_types;
 } dstd_tensor_list;
 
-/* Bytes of device memory that a list of these tensors needs (only their n
-   counts); 0 for invalid arguments (the build then reports the error). */
+/* Bytes of device memory that a list of these tensors needs, wherever they
+   lie (only their n counts); 0 for invalid arguments (the build then reports
+   the error). */
 size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
 
 /*
@@ -560,7 +561,7 @@ size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
  * and the tensors have to stay while the list is used, and a call on another
  * stream has to be ordered behind the build. A tensor that moves needs a new
  * build. n_tensors and any n may be 0; n < 2^35 and fewer than 2^23 chunks
- * of 4096 elements in all. Arrays of one list must not overlap (out = g
+ * of 4096 elements in all (each tensor with 63 elements more). Arrays of one list must not overlap (out = g
  * apart): DSTD_ERR_PARAM.
  */
 dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,

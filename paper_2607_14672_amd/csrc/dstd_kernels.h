@@ -250,8 +250,13 @@ hipError_t launch_exact_backward(const LifConst &C, int64_t B, int64_t N_in, int
 // ----------------------------------------------------------------- optim --
 // Tensor lists, the global gradient norm, clipping and AdamW (dstd_optim.hip).
 // A list's device memory: its tensors, then its chunks of at most kOptChunk
-// elements in tensor order (empty tensors have none).
+// elements in tensor order (empty tensors have none). Chunks end where
+// (element + phase) is a multiple of kOptChunk: phase is the place of the
+// tensor's first element among kOptAlign elements (256 bytes of fp32, 128 of
+// bf16), so that chunks start at whole cache lines. `lead` elements of a
+// chunk (of a tensor's first, if phase > 0) lie before its first whole line.
 constexpr int64_t kOptChunk = 4096;
+constexpr int kOptAlign = 64;
 constexpr int kOptMaxPart = 1024;  // partial sums of squares of one norm
 enum OptTypes : uint32_t { kOptGradBf16 = 1, kOptOutBf16 = 2, kOptWeightBf16 = 4 };
 enum OptListTypes : uint32_t { kOptListF32 = 1, kOptListBf16 = 2 };  // of a list's gradients
@@ -259,12 +264,17 @@ struct OptTensor {
     void *g, *out, *w;
     float *w32, *m, *v;
     float lr_scale, decay_scale;
-    uint32_t types, pad;
+    uint32_t types, phase;
 };
 struct OptChunk {
-    int32_t tensor, count;
+    int32_t tensor;
+    uint16_t count, lead;
     int64_t start;
 };
+// chunks of n elements whose first has place `phase` (0 for none)
+__host__ __device__ inline int64_t opt_chunks(int64_t n, int64_t phase) {
+    return n > 0 ? (n + phase + kOptChunk - 1) / kOptChunk : 0;
+}
 struct OptList {
     const OptTensor *ten;
     const OptChunk *chunks;

@@ -110,6 +110,21 @@ __device__ __forceinline__ double add_square(double s, float x) {
     return fma(y, y, s);
 }
 
+// A chunk's elements: n4 vectors of four from its first whole line on, and at
+// most kOptAlign + 2 single ones before and behind them, the one of thread tid
+// at `one`, if it is below `count`.
+struct Span {
+    int lead, n4, one, count;
+};
+__device__ __forceinline__ Span span_of(int count, int lead, int tid) {
+    Span p;
+    p.lead = lead;
+    p.n4 = (count - lead) / 4;
+    p.one = tid < lead ? tid : p.n4 * 4 + tid;
+    p.count = count;
+    return p;
+}
+
 // A thread's vectors of four elements of a gradient chunk, zeros past the last
 // whole one. As read: they are widened where they are used, for a conversion
 // next to the loads would wait for them before the next chunk's are issued.
@@ -117,12 +132,12 @@ template <typename T> struct Share {
     typename Vec4<T>::type x[kOptGroups];
 };
 template <bool NT, typename T>
-__device__ __forceinline__ void read_share(Share<T> &r, const T *g, int count, int tid) {
-    const int n4 = count / 4;
+__device__ __forceinline__ void read_share(Share<T> &r, const T *g, const Span &p, int tid) {
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i) {
         r.x[i] = typename Vec4<T>::type{0, 0, 0, 0};
-        if (i * kOptThreads + tid < n4) r.x[i] = load4<NT>(g + (i * kOptThreads + tid) * 4);
+        if (i * kOptThreads + tid < p.n4)
+            r.x[i] = load4<NT>(g + p.lead + (i * kOptThreads + tid) * 4);
     }
 }
 template <typename T> __device__ __forceinline__ double add_share(double s, const Share<T> &r) {
@@ -134,28 +149,31 @@ template <typename T> __device__ __forceinline__ double add_share(double s, cons
     }
     return s;
 }
-// the at most three elements behind a chunk's last whole vector
+// the single elements
 template <typename T>
-__device__ __forceinline__ double add_rest(double s, const T *g, int count, int tid) {
-    if (count % 4 != 0 && tid < count % 4) s = add_square(s, load1(g + count / 4 * 4 + tid));
+__device__ __forceinline__ double add_rest(double s, const T *g, const Span &p) {
+    if (p.n4 * 4 < p.count && p.one < p.count) s = add_square(s, load1(g + p.one));
     return s;
 }
 
 // The gradient of a chunk, if it is of type T; count 0 else and past the end.
 template <typename T> struct ChunkAt {
     const T *g;
-    int count;
+    int count, lead;
 };
 template <typename T>
 __device__ __forceinline__ ChunkAt<T> chunk_at(const OptTensor *ten, const OptChunk *chunks,
                                                int64_t k, int64_t end) {
     constexpr uint32_t type = sizeof(T) == 2 ? kOptGradBf16 : 0;
-    ChunkAt<T> a{nullptr, 0};
+    ChunkAt<T> a{nullptr, 0, 0};
     if (k < end) {
         const OptChunk c = chunks[k];
         const OptTensor &t = ten[c.tensor];
         a.g = (const T *)t.g + c.start;
-        a.count = (t.types & kOptGradBf16) == type ? c.count : 0;
+        if ((t.types & kOptGradBf16) == type) {
+            a.count = c.count;
+            a.lead = c.lead;
+        }
     }
     return a;
 }
@@ -174,9 +192,11 @@ __device__ double range_squares(const OptTensor *ten, const OptChunk *chunks, in
     for (int64_t k = lo + first; k < end; k += static_cast<int64_t>(kAtOnce) * by) {
         Share<T> r[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) read_share<NT>(r[j], a[j].g, a[j].count, tid);
+        for (int j = 0; j < kAtOnce; ++j)
+            read_share<NT>(r[j], a[j].g, span_of(a[j].count, a[j].lead, tid), tid);
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) s = add_rest(s, a[j].g, a[j].count, tid);
+        for (int j = 0; j < kAtOnce; ++j)
+            s = add_rest(s, a[j].g, span_of(a[j].count, a[j].lead, tid));
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
             a[j] = chunk_at<T>(ten, chunks, k + static_cast<int64_t>(kAtOnce + j) * by, end);
@@ -258,18 +278,19 @@ __global__ __launch_bounds__(kOptThreads) void grad_norm_kernel(OptNorm nm) {
 // One chunk by kOptThreads threads. The factor is asked for once the chunk's
 // reads are on their way.
 template <bool NT, typename TI, typename TO, typename F>
-__device__ __forceinline__ void clip_values(const TI *g, TO *out, int count, int tid, const F &factor) {
+__device__ __forceinline__ void clip_values(const TI *g, TO *out, const Span &p, int tid,
+                                            const F &factor) {
     typename Vec4<TI>::type x[kOptGroups];
-    const int n4 = count / 4, e1 = n4 * 4 + tid;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
-        if (i * kOptThreads + tid < n4) x[i] = load4<NT>(g + (i * kOptThreads + tid) * 4);
-    const float x1 = e1 < count ? load1(g + e1) : 0.f;
+        if (i * kOptThreads + tid < p.n4) x[i] = load4<NT>(g + p.lead + (i * kOptThreads + tid) * 4);
+    const float x1 = p.one < p.count ? load1(g + p.one) : 0.f;
     const float c = factor().c;
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
-        if (i * kOptThreads + tid < n4) store4<NT>(out + (i * kOptThreads + tid) * 4, widen(x[i]) * c);
-    if (e1 < count) store1(out + e1, x1 * c);
+        if (i * kOptThreads + tid < p.n4)
+            store4<NT>(out + p.lead + (i * kOptThreads + tid) * 4, widen(x[i]) * c);
+    if (p.one < p.count) store1(out + p.one, x1 * c);
 }
 
 template <bool NT, typename F>
@@ -280,10 +301,11 @@ __device__ __forceinline__ void clip_chunk(const OptTensor *ten, const OptChunk 
     const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
     gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
     gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
-    if (gb && ob) clip_values<NT>(gh, oh, ch.count, tid, factor);
-    else if (gb) clip_values<NT>(gh, of, ch.count, tid, factor);
-    else if (ob) clip_values<NT>(gf, oh, ch.count, tid, factor);
-    else clip_values<NT>(gf, of, ch.count, tid, factor);
+    const Span p = span_of(ch.count, ch.lead, tid);
+    if (gb && ob) clip_values<NT>(gh, oh, p, tid, factor);
+    else if (gb) clip_values<NT>(gh, of, p, tid, factor);
+    else if (ob) clip_values<NT>(gf, oh, p, tid, factor);
+    else clip_values<NT>(gf, of, p, tid, factor);
 }
 
 // One chunk a block, from the last to the first: the norm's launch has read
@@ -329,31 +351,30 @@ struct StepArgs {
 // One chunk by kThreads threads. `in` is asked for once the chunk's reads are
 // on their way.
 template <int kThreads, bool NT, bool NTG, typename GT, int WM, typename F>
-__device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, int count,
+__device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, const Span &p,
                                              const StepArgs &a, int tid, const F &in) {
     const GT *g = (const GT *)t.g + start;
     gf32 *wf = f32_at(WM == 2 ? t.w32 : t.w, start), *m = f32_at(t.m, start), *v = f32_at(t.v, start);
     gu16 *wh = u16_at(t.w, start);
-    const int n4 = count / 4, e1 = n4 * 4 + tid;
     typename Vec4<GT>::type gx[kVecs<kThreads>];
     f32x4 wx[kVecs<kThreads>], mx[kVecs<kThreads>], vx[kVecs<kThreads>];
     u16x4 hx[kVecs<kThreads>];
 #pragma unroll
     for (int i = 0; i < kVecs<kThreads>; ++i) {
-        if (i * kThreads + tid >= n4) continue;
-        const int e = (i * kThreads + tid) * 4;
+        if (i * kThreads + tid >= p.n4) continue;
+        const int e = p.lead + (i * kThreads + tid) * 4;
         gx[i] = load4<NTG>(g + e);
         if (WM == 1) hx[i] = load4<NT>(wh + e);
         else wx[i] = load4<NT>(wf + e);
         mx[i] = load4<NT>(m + e);
         vx[i] = load4<NT>(v + e);
     }
-    float g1 = 0.f, w1 = 0.f, m1 = 0.f, v1 = 0.f;  // of the elements behind the last vector
-    if (e1 < count) {
-        g1 = load1(g + e1);
-        w1 = (WM == 1) ? load1(wh + e1) : wf[e1];
-        m1 = m[e1];
-        v1 = v[e1];
+    float g1 = 0.f, w1 = 0.f, m1 = 0.f, v1 = 0.f;  // of the single element
+    if (p.one < p.count) {
+        g1 = load1(g + p.one);
+        w1 = (WM == 1) ? load1(wh + p.one) : wf[p.one];
+        m1 = m[p.one];
+        v1 = v[p.one];
     }
     const StepIn si = in();
     if (!si.f.finite) return;  // the step is skipped
@@ -362,8 +383,8 @@ __device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, 
                       rate * t.lr_scale, a.hp.decay * t.decay_scale};
 #pragma unroll
     for (int i = 0; i < kVecs<kThreads>; ++i) {
-        if (i * kThreads + tid >= n4) continue;
-        const int e = (i * kThreads + tid) * 4;
+        if (i * kThreads + tid >= p.n4) continue;
+        const int e = p.lead + (i * kThreads + tid) * 4;
         const f32x4 g4 = widen(gx[i]);
         if (WM == 1) wx[i] = widen(hx[i]);
 #pragma unroll
@@ -379,12 +400,12 @@ __device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, 
         if (WM != 1) store4<NT>(wf + e, wx[i]);
         if (WM != 0) store4<NT>(wh + e, wx[i]);
     }
-    if (e1 < count) {
+    if (p.one < p.count) {
         adamw_one(q, g1, w1, m1, v1);
-        m[e1] = m1;
-        v[e1] = v1;
-        if (WM != 1) wf[e1] = w1;
-        if (WM != 0) store1(wh + e1, w1);
+        m[p.one] = m1;
+        v[p.one] = v1;
+        if (WM != 1) wf[p.one] = w1;
+        if (WM != 0) store1(wh + p.one, w1);
     }
 }
 
@@ -393,14 +414,15 @@ __device__ __forceinline__ void adamw_chunk(const OptTensor *ten, const OptChunk
                                             const StepArgs &a, int tid, const F &in) {
     const OptTensor &t = ten[ch.tensor];
     const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
+    const Span p = span_of(ch.count, ch.lead, tid);
     if (t.types & kOptGradBf16) {
-        if (wm == 0) adamw_values<kThreads, NT, NTG, gu16, 0>(t, ch.start, ch.count, a, tid, in);
-        else if (wm == 1) adamw_values<kThreads, NT, NTG, gu16, 1>(t, ch.start, ch.count, a, tid, in);
-        else adamw_values<kThreads, NT, NTG, gu16, 2>(t, ch.start, ch.count, a, tid, in);
+        if (wm == 0) adamw_values<kThreads, NT, NTG, gu16, 0>(t, ch.start, p, a, tid, in);
+        else if (wm == 1) adamw_values<kThreads, NT, NTG, gu16, 1>(t, ch.start, p, a, tid, in);
+        else adamw_values<kThreads, NT, NTG, gu16, 2>(t, ch.start, p, a, tid, in);
     } else {
-        if (wm == 0) adamw_values<kThreads, NT, NTG, gf32, 0>(t, ch.start, ch.count, a, tid, in);
-        else if (wm == 1) adamw_values<kThreads, NT, NTG, gf32, 1>(t, ch.start, ch.count, a, tid, in);
-        else adamw_values<kThreads, NT, NTG, gf32, 2>(t, ch.start, ch.count, a, tid, in);
+        if (wm == 0) adamw_values<kThreads, NT, NTG, gf32, 0>(t, ch.start, p, a, tid, in);
+        else if (wm == 1) adamw_values<kThreads, NT, NTG, gf32, 1>(t, ch.start, p, a, tid, in);
+        else adamw_values<kThreads, NT, NTG, gf32, 2>(t, ch.start, p, a, tid, in);
     }
 }
 
@@ -468,12 +490,13 @@ __global__ __launch_bounds__(kOptThreads) void tensor_list_kernel(OptBatch b, Op
                                                                   OptChunk *chunks) {
     const int k = blockIdx.x;
     if (threadIdx.x == 0) ten[b.first + k] = b.ten[k];
-    const int64_t n = b.n[k], nc = (n + kOptChunk - 1) / kOptChunk;
+    const int64_t n = b.n[k], phase = b.ten[k].phase, nc = opt_chunks(n, phase);
     for (int64_t c = threadIdx.x; c < nc; c += kOptThreads) {
-        const int64_t start = c * kOptChunk;
-        const int64_t left = n - start;
-        chunks[b.chunk0[k] + c] =
-            OptChunk{b.first + k, static_cast<int>(left < kOptChunk ? left : kOptChunk), start};
+        const int64_t start = max<int64_t>(c * kOptChunk - phase, 0);
+        const int64_t count = min((c + 1) * kOptChunk - phase, n) - start;
+        const int64_t lead = (c == 0 && phase > 0) ? min<int64_t>(kOptAlign - phase, count) : 0;
+        chunks[b.chunk0[k] + c] = OptChunk{b.first + k, static_cast<uint16_t>(count),
+                                           static_cast<uint16_t>(lead), start};
     }
 }
 

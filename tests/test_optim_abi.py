@@ -58,7 +58,7 @@ def test_list_size_counts_tensors_and_chunks():
     assert dstd.dstd_tensor_list_size(1, None) == 0
     assert dstd.dstd_tensor_list_size(1, _tensors(dict(n=-1))) == 0
     assert dstd.dstd_tensor_list_size(1, _tensors(dict(n=1 << 35))) == 0
-    big = _tensors(*[dict(n=1 << 32)] * 8)  # 2^20 chunks each: one chunk too many together
+    big = _tensors(*[dict(n=(1 << 32) - 63)] * 8)  # 2^20 chunks each: one too many together
     assert dstd.dstd_tensor_list_size(7, big) > 0
     assert dstd.dstd_tensor_list_size(8, big) == 0
     big[7].n -= 4096
