@@ -1071,9 +1071,8 @@ dstd_status check_counts(int64_t n, const dstd_tensor *t, int64_t *n_chunks) {
     return DSTD_OK;
 }
 
-size_t list_tensors_bytes(int64_t n) { return align_up((size_t)n * sizeof(dstd::OptTensor)); }
-size_t list_bytes(int64_t n, int64_t n_chunks) {
-    return std::max(kAlign, list_tensors_bytes(n) + align_up((size_t)n_chunks * sizeof(dstd::OptChunk)));
+size_t list_bytes(int64_t n_chunks) {
+    return std::max(kAlign, align_up((size_t)n_chunks * sizeof(dstd::OptChunk)));
 }
 
 struct Range { uintptr_t lo, hi; int64_t k; };
@@ -1130,14 +1129,14 @@ dstd_status check_list(const dstd_tensor_list *l) {
 // The place of a tensor's first element among kOptAlign elements that most of
 // its arrays share (views at one offset of flat buffers share it; the others'
 // accesses are right at any place, 5 to 25 % slower where they split lines).
-uint32_t tensor_phase(const dstd_tensor &t) {
+uint16_t tensor_phase(const dstd_tensor &t) {
     const struct { const void *p; int64_t bytes; } arr[] = {
         {t.g, dtype_bytes(t.g_dtype)}, {t.w, dtype_bytes(t.w_dtype)}, {t.w32, 4}, {t.m, 4}, {t.v, 4},
         {t.out, dtype_bytes(t.out_dtype)}};
     const auto place = [](const void *p, int64_t bytes) {
-        return (uint32_t)((uintptr_t)p / (uintptr_t)bytes % dstd::kOptAlign);
+        return (uint16_t)((uintptr_t)p / (uintptr_t)bytes % dstd::kOptAlign);
     };
-    uint32_t best = 0;
+    uint16_t best = 0;
     int most = 0;
     for (const auto &a : arr) {
         if (!a.p) continue;
@@ -1163,10 +1162,7 @@ OptWs opt_ws_layout() {
 }
 
 dstd::OptList opt_list(const dstd_tensor_list *l) {
-    const char *mem = static_cast<const char *>(l->mem);
-    return dstd::OptList{reinterpret_cast<const dstd::OptTensor *>(mem),
-                         reinterpret_cast<const dstd::OptChunk *>(mem + list_tensors_bytes(l->n_tensors)),
-                         (int)l->n_chunks, l->g_bytes, l->out_bytes, l->w_bytes,
+    return dstd::OptList{static_cast<const dstd::OptChunk *>(l->mem), (int)l->n_chunks, l->g_bytes, l->out_bytes, l->w_bytes,
                          l->g_types};
 }
 
@@ -1188,7 +1184,7 @@ extern "C" {
 size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors) {
     int64_t nc;
     if (check_counts(n_tensors, tensors, &nc) != DSTD_OK) return 0;
-    return list_bytes(n_tensors, nc);
+    return list_bytes(nc);
 }
 
 dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
@@ -1197,7 +1193,7 @@ dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors
     dstd_status s = check_counts(n_tensors, tensors, &nc);
     if (s != DSTD_OK) return s;
     if (!list) return fail(DSTD_ERR_NULL, "list is NULL");
-    const size_t need = list_bytes(n_tensors, nc);
+    const size_t need = list_bytes(nc);
     std::vector<Range> ranges;
     ranges.reserve((size_t)n_tensors * 6 + 1);
     uint32_t has_weights = 1;
@@ -1212,17 +1208,15 @@ dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors
         if (ranges[i].lo < ranges[i - 1].hi)
             return fail(DSTD_ERR_PARAM, "arrays of tensors %lld and %lld overlap (-1: the list's own memory)",
                         (long long)ranges[i - 1].k, (long long)ranges[i].k);
-    auto *ten = static_cast<dstd::OptTensor *>(mem);
-    auto *chunks = at<dstd::OptChunk>(mem, list_tensors_bytes(n_tensors));
+    auto *chunks = static_cast<dstd::OptChunk *>(mem);
     int64_t c = 0, gb = 0, ob = 0, wb = 0;
     uint32_t types = 0;
     for (int64_t k0 = 0; k0 < n_tensors; k0 += dstd::kOptBatch) {
         const int count = (int)std::min<int64_t>(dstd::kOptBatch, n_tensors - k0);
         dstd::OptBatch b{};
-        b.first = (int32_t)k0;
         for (int i = 0; i < count; ++i) {
             const dstd_tensor &t = tensors[k0 + i];
-            dstd::OptTensor &o = b.ten[i];
+            dstd::OptChunk &o = b.ten[i];
             o.g = t.g;
             o.out = t.out ? t.out : t.g;
             o.w = t.w;
@@ -1234,16 +1228,16 @@ dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors
             o.types = (t.g_dtype == DSTD_BF16 ? dstd::kOptGradBf16 : 0) |
                       ((t.out ? t.out_dtype : t.g_dtype) == DSTD_BF16 ? dstd::kOptOutBf16 : 0) |
                       (t.w_dtype == DSTD_BF16 ? dstd::kOptWeightBf16 : 0);
-            o.phase = tensor_phase(t);
+            o.lead = tensor_phase(t);
             b.n[i] = t.n;
             b.chunk0[i] = c;
-            c += dstd::opt_chunks(t.n, o.phase);
+            c += dstd::opt_chunks(t.n, o.lead);
             gb += t.n * dtype_bytes(t.g_dtype);
             if (t.n > 0) types |= t.g_dtype == DSTD_BF16 ? dstd::kOptListBf16 : dstd::kOptListF32;
             if (o.out != o.g) ob += t.n * dtype_bytes(t.out_dtype);
             if (t.w) wb += t.n * (8 + dtype_bytes(t.w_dtype) + (t.w32 ? 4 : 0));
         }
-        hipError_t e = dstd::launch_tensor_list(b, count, ten, chunks, static_cast<hipStream_t>(stream));
+        hipError_t e = dstd::launch_tensor_list(b, count, chunks, static_cast<hipStream_t>(stream));
         if (e != hipSuccess) return hip_status(e, "tensor list launch");
     }
     *list = dstd_tensor_list{mem, n_tensors, c, gb, ob, wb, kListMagic, has_weights, types};

@@ -249,8 +249,9 @@ hipError_t launch_exact_backward(const LifConst &C, int64_t B, int64_t N_in, int
 
 // ----------------------------------------------------------------- optim --
 // Tensor lists, the global gradient norm, clipping and AdamW (dstd_optim.hip).
-// A list's device memory: its tensors, then its chunks of at most kOptChunk
-// elements in tensor order (empty tensors have none). Chunks end where
+// A list's device memory: its chunks of at most kOptChunk elements, in tensor
+// order (empty tensors have none), with all that a block has to know of them in
+// one 64-byte record. Chunks end where
 // (element + phase) is a multiple of kOptChunk: phase is the place of the
 // tensor's first element among kOptAlign elements (256 bytes of fp32, 128 of
 // bf16), so that chunks start at whole cache lines. `lead` elements of a
@@ -260,23 +261,18 @@ constexpr int kOptAlign = 64;
 constexpr int kOptMaxPart = 1024;  // partial sums of squares of one norm
 enum OptTypes : uint32_t { kOptGradBf16 = 1, kOptOutBf16 = 2, kOptWeightBf16 = 4 };
 enum OptListTypes : uint32_t { kOptListF32 = 1, kOptListBf16 = 2 };  // of a list's gradients
-struct OptTensor {
+struct OptChunk {
     void *g, *out, *w;
     float *w32, *m, *v;
     float lr_scale, decay_scale;
-    uint32_t types, phase;
-};
-struct OptChunk {
-    int32_t tensor;
+    uint32_t types;
     uint16_t count, lead;
-    int64_t start;
 };
 // chunks of n elements whose first has place `phase` (0 for none)
 __host__ __device__ inline int64_t opt_chunks(int64_t n, int64_t phase) {
     return n > 0 ? (n + phase + kOptChunk - 1) / kOptChunk : 0;
 }
 struct OptList {
-    const OptTensor *ten;
     const OptChunk *chunks;
     int n_chunks;
     // of all gradients; of clipped ones elsewhere; of weights, copies, moments
@@ -286,9 +282,8 @@ struct OptList {
 // A batch of tensors as kernel arguments (at most 4 KB in all).
 constexpr int kOptBatch = 48;
 struct OptBatch {
-    OptTensor ten[kOptBatch];
+    OptChunk ten[kOptBatch];  // as one chunk that begins with the tensor; `lead` is its phase
     int64_t n[kOptBatch], chunk0[kOptBatch];
-    int32_t first;
 };
 // The norm of a call: n_part partial sums of squares, or n_part = -1 where it
 // is given in *norm, or not asked for (norm null).
@@ -309,8 +304,7 @@ struct OptAdamW {
     float eps, lr, decay;
 };
 int opt_norm_blocks(int n_chunks);
-hipError_t launch_tensor_list(const OptBatch &b, int count, OptTensor *ten, OptChunk *chunks,
-                              hipStream_t st);
+hipError_t launch_tensor_list(const OptBatch &b, int count, OptChunk *chunks, hipStream_t st);
 hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st);
 hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st);
 hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp, const float *lr,

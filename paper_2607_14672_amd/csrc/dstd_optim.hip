@@ -9,9 +9,8 @@
 //          w -= lr (m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps) + decay w)
 //
 // All three stream their arrays once and are bound by HBM. A list's tensors
-// are cut into chunks of kOptChunk elements; a table in device memory gives
-// each chunk its tensor, so that one launch covers any number of tensors of
-// any sizes. The norm needs every gradient before the first is scaled: one
+// are cut into chunks of kOptChunk elements; a table of the chunks in device
+// memory lets one launch cover any number of tensors of any sizes. The norm needs every gradient before the first is scaled: one
 // launch sums the squares of a fixed set of chunks per block (partials), and
 // the launch that follows adds the partials again in every block, in a fixed
 // order, rather than in a launch of its own.
@@ -87,9 +86,6 @@ __device__ __forceinline__ void store1(gu16 *p, float v) {
     *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
 
-__device__ __forceinline__ gf32 *f32_at(void *p, int64_t start) { return (gf32 *)p + start; }
-__device__ __forceinline__ gu16 *u16_at(void *p, int64_t start) { return (gu16 *)p + start; }
-
 // Sum over the block, in a fixed order, to every thread. sh: one double per wave.
 template <int kThreads> __device__ double block_sum(double v, double *sh) {
 #pragma unroll
@@ -162,15 +158,13 @@ template <typename T> struct ChunkAt {
     int count, lead;
 };
 template <typename T>
-__device__ __forceinline__ ChunkAt<T> chunk_at(const OptTensor *ten, const OptChunk *chunks,
-                                               int64_t k, int64_t end) {
+__device__ __forceinline__ ChunkAt<T> chunk_at(const OptChunk *chunks, int64_t k, int64_t end) {
     constexpr uint32_t type = sizeof(T) == 2 ? kOptGradBf16 : 0;
     ChunkAt<T> a{nullptr, 0, 0};
     if (k < end) {
-        const OptChunk c = chunks[k];
-        const OptTensor &t = ten[c.tensor];
-        a.g = (const T *)t.g + c.start;
-        if ((t.types & kOptGradBf16) == type) {
+        const OptChunk &c = chunks[k];
+        a.g = (const T *)c.g;
+        if ((c.types & kOptGradBf16) == type) {
             a.count = c.count;
             a.lead = c.lead;
         }
@@ -182,13 +176,13 @@ __device__ __forceinline__ ChunkAt<T> chunk_at(const OptTensor *ten, const OptCh
 // the kOptThreads threads `tid`: kAtOnce of them at a time, the places of the
 // next looked up while these are read.
 template <int kAtOnce, bool NT, typename T>
-__device__ double range_squares(const OptTensor *ten, const OptChunk *chunks, int64_t lo, int64_t end,
-                                int first, int by, int tid) {
+__device__ double range_squares(const OptChunk *chunks, int64_t lo, int64_t end, int first, int by,
+                                int tid) {
     double s = 0.0;
     ChunkAt<T> a[kAtOnce];
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j)
-        a[j] = chunk_at<T>(ten, chunks, lo + first + static_cast<int64_t>(j) * by, end);
+        a[j] = chunk_at<T>(chunks, lo + first + static_cast<int64_t>(j) * by, end);
     for (int64_t k = lo + first; k < end; k += static_cast<int64_t>(kAtOnce) * by) {
         Share<T> r[kAtOnce];
 #pragma unroll
@@ -199,7 +193,7 @@ __device__ double range_squares(const OptTensor *ten, const OptChunk *chunks, in
             s = add_rest(s, a[j].g, span_of(a[j].count, a[j].lead, tid));
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            a[j] = chunk_at<T>(ten, chunks, k + static_cast<int64_t>(kAtOnce + j) * by, end);
+            a[j] = chunk_at<T>(chunks, k + static_cast<int64_t>(kAtOnce + j) * by, end);
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) s = add_share(s, r[j]);
     }
@@ -222,20 +216,19 @@ __device__ OptStep step_at(const int64_t *step, double beta1, double beta2) {
 // 1 / (1 - beta^t): the update writes the number, so its other blocks must
 // not read it.
 __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
-    const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
-    int n_stream, uint32_t types, double *__restrict__ part, const int64_t *step, double beta1,
+    const OptChunk *__restrict__ chunks, int n_chunks, int n_stream, uint32_t types, double *__restrict__ part, const int64_t *step, double beta1,
     double beta2, OptStep *__restrict__ at) {
     __shared__ double sh[kOptThreads / kWave];
     double s = 0.0;
     const int b = blockIdx.x, by = gridDim.x, tid = threadIdx.x;
     // 32 registers of gradients on the way
     if (types & kOptListF32) {
-        s += range_squares<2, true, gf32>(ten, chunks, 0, n_stream, b, by, tid);
-        s += range_squares<2, false, gf32>(ten, chunks, n_stream, n_chunks, b, by, tid);
+        s += range_squares<2, true, gf32>(chunks, 0, n_stream, b, by, tid);
+        s += range_squares<2, false, gf32>(chunks, n_stream, n_chunks, b, by, tid);
     }
     if (types & kOptListBf16) {
-        s += range_squares<4, true, gu16>(ten, chunks, 0, n_stream, b, by, tid);
-        s += range_squares<4, false, gu16>(ten, chunks, n_stream, n_chunks, b, by, tid);
+        s += range_squares<4, true, gu16>(chunks, 0, n_stream, b, by, tid);
+        s += range_squares<4, false, gu16>(chunks, n_stream, n_chunks, b, by, tid);
     }
     s = block_sum<kOptThreads>(s, sh);
     if (threadIdx.x == 0) {
@@ -294,14 +287,12 @@ __device__ __forceinline__ void clip_values(const TI *g, TO *out, const Span &p,
 }
 
 template <bool NT, typename F>
-__device__ __forceinline__ void clip_chunk(const OptTensor *ten, const OptChunk &ch, int tid,
-                                           const F &factor) {
-    const OptTensor &t = ten[ch.tensor];
+__device__ __forceinline__ void clip_chunk(const OptChunk &t, int tid, const F &factor) {
     if (t.g == t.out && factor().c == 1.f) return;  // in place, nothing to clip
     const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
-    gu16 *gh = u16_at(t.g, ch.start), *oh = u16_at(t.out, ch.start);
-    gf32 *gf = f32_at(t.g, ch.start), *of = f32_at(t.out, ch.start);
-    const Span p = span_of(ch.count, ch.lead, tid);
+    gu16 *gh = (gu16 *)t.g, *oh = (gu16 *)t.out;
+    gf32 *gf = (gf32 *)t.g, *of = (gf32 *)t.out;
+    const Span p = span_of(t.count, t.lead, tid);
     if (gb && ob) clip_values<NT>(gh, oh, p, tid, factor);
     else if (gb) clip_values<NT>(gh, of, p, tid, factor);
     else if (ob) clip_values<NT>(gf, oh, p, tid, factor);
@@ -312,15 +303,14 @@ __device__ __forceinline__ void clip_chunk(const OptTensor *ten, const OptChunk 
 // the last ones most recently.
 template <bool NT>
 __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
-    const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
-    OptNorm nm) {
+    const OptChunk *__restrict__ chunks, int n_chunks, OptNorm nm) {
     __shared__ double sh[kOptThreads / kWave];
     const auto factor = [&] { return norm_factor<kOptThreads>(nm, sh); };
     if (nm.n_part >= 0 && nm.norm && blockIdx.x == 0) {
         const NormFactor f = factor();
         if (threadIdx.x == 0) *nm.norm = f.norm;
     }
-    clip_chunk<NT>(ten, chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], threadIdx.x, factor);
+    clip_chunk<NT>(chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], threadIdx.x, factor);
 }
 
 // One chunk's update in fp32. WM: 0 = fp32 weights, 1 = bf16 weights (the
@@ -351,11 +341,11 @@ struct StepArgs {
 // One chunk by kThreads threads. `in` is asked for once the chunk's reads are
 // on their way.
 template <int kThreads, bool NT, bool NTG, typename GT, int WM, typename F>
-__device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, const Span &p,
-                                             const StepArgs &a, int tid, const F &in) {
-    const GT *g = (const GT *)t.g + start;
-    gf32 *wf = f32_at(WM == 2 ? t.w32 : t.w, start), *m = f32_at(t.m, start), *v = f32_at(t.v, start);
-    gu16 *wh = u16_at(t.w, start);
+__device__ __forceinline__ void adamw_values(const OptChunk &t, const Span &p, const StepArgs &a,
+                                             int tid, const F &in) {
+    const GT *g = (const GT *)t.g;
+    gf32 *wf = (gf32 *)(WM == 2 ? t.w32 : t.w), *m = (gf32 *)t.m, *v = (gf32 *)t.v;
+    gu16 *wh = (gu16 *)t.w;
     typename Vec4<GT>::type gx[kVecs<kThreads>];
     f32x4 wx[kVecs<kThreads>], mx[kVecs<kThreads>], vx[kVecs<kThreads>];
     u16x4 hx[kVecs<kThreads>];
@@ -410,27 +400,25 @@ __device__ __forceinline__ void adamw_values(const OptTensor &t, int64_t start, 
 }
 
 template <int kThreads, bool NT, bool NTG, typename F>
-__device__ __forceinline__ void adamw_chunk(const OptTensor *ten, const OptChunk &ch,
-                                            const StepArgs &a, int tid, const F &in) {
-    const OptTensor &t = ten[ch.tensor];
+__device__ __forceinline__ void adamw_chunk(const OptChunk &t, const StepArgs &a, int tid,
+                                            const F &in) {
     const int wm = (t.types & kOptWeightBf16) ? (t.w32 ? 2 : 1) : 0;
-    const Span p = span_of(ch.count, ch.lead, tid);
+    const Span p = span_of(t.count, t.lead, tid);
     if (t.types & kOptGradBf16) {
-        if (wm == 0) adamw_values<kThreads, NT, NTG, gu16, 0>(t, ch.start, p, a, tid, in);
-        else if (wm == 1) adamw_values<kThreads, NT, NTG, gu16, 1>(t, ch.start, p, a, tid, in);
-        else adamw_values<kThreads, NT, NTG, gu16, 2>(t, ch.start, p, a, tid, in);
+        if (wm == 0) adamw_values<kThreads, NT, NTG, gu16, 0>(t, p, a, tid, in);
+        else if (wm == 1) adamw_values<kThreads, NT, NTG, gu16, 1>(t, p, a, tid, in);
+        else adamw_values<kThreads, NT, NTG, gu16, 2>(t, p, a, tid, in);
     } else {
-        if (wm == 0) adamw_values<kThreads, NT, NTG, gf32, 0>(t, ch.start, p, a, tid, in);
-        else if (wm == 1) adamw_values<kThreads, NT, NTG, gf32, 1>(t, ch.start, p, a, tid, in);
-        else adamw_values<kThreads, NT, NTG, gf32, 2>(t, ch.start, p, a, tid, in);
+        if (wm == 0) adamw_values<kThreads, NT, NTG, gf32, 0>(t, p, a, tid, in);
+        else if (wm == 1) adamw_values<kThreads, NT, NTG, gf32, 1>(t, p, a, tid, in);
+        else adamw_values<kThreads, NT, NTG, gf32, 2>(t, p, a, tid, in);
     }
 }
 
 // One chunk a block, from the last to the first, as grad_clip_kernel.
 template <bool NT, bool NTG>
-__global__ __launch_bounds__(kStepThreads) void adamw_kernel(
-    const OptTensor *__restrict__ ten, const OptChunk *__restrict__ chunks, int n_chunks,
-    StepArgs a) {
+__global__ __launch_bounds__(kStepThreads) void adamw_kernel(const OptChunk *__restrict__ chunks,
+                                                             int n_chunks, StepArgs a) {
     __shared__ double sh[kStepThreads / kWave];
     const auto in = [&] { return StepIn{norm_factor<kStepThreads>(a.nm, sh), *a.at}; };
     if (blockIdx.x == 0) {
@@ -440,7 +428,7 @@ __global__ __launch_bounds__(kStepThreads) void adamw_kernel(
             if (si.f.finite) *a.step = si.at.t;
         }
     }
-    adamw_chunk<kStepThreads, NT, NTG>(ten, chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], a,
+    adamw_chunk<kStepThreads, NT, NTG>(chunks[n_chunks - 1 - static_cast<int>(blockIdx.x)], a,
                                        threadIdx.x, in);
 }
 
@@ -449,8 +437,7 @@ __global__ __launch_bounds__(kStepThreads) void adamw_kernel(
 enum SoloOp { kSoloNorm, kSoloClip, kSoloStep };
 constexpr int kSoloChunks[] = {kSoloNormChunks, kSoloClipChunks, kSoloStepChunks};
 template <SoloOp kOp>
-__global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptTensor *__restrict__ ten,
-                                                            const OptChunk *__restrict__ chunks,
+__global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptChunk *__restrict__ chunks,
                                                             int n_chunks, uint32_t types, StepArgs a) {
     constexpr int kTeams = kSoloThreads / kOptThreads;
     __shared__ double sh[kSoloThreads / kWave];
@@ -465,9 +452,9 @@ __global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptTensor *__r
         double s = 0.0;
         constexpr int kAtOnce = (kSoloChunks[kOp] + kTeams - 1) / kTeams;  // one round of reads
         if (types & kOptListF32)
-            s += range_squares<kAtOnce, false, gf32>(ten, chunks, 0, n_chunks, team, kTeams, tid);
+            s += range_squares<kAtOnce, false, gf32>(chunks, 0, n_chunks, team, kTeams, tid);
         if (types & kOptListBf16)
-            s += range_squares<kAtOnce, false, gu16>(ten, chunks, 0, n_chunks, team, kTeams, tid);
+            s += range_squares<kAtOnce, false, gu16>(chunks, 0, n_chunks, team, kTeams, tid);
         n = sqrt(block_sum<kSoloThreads>(s, sh));
     } else if (a.nm.norm) {
         n = static_cast<double>(*a.nm.norm);
@@ -478,25 +465,34 @@ __global__ __launch_bounds__(kSoloThreads) void solo_kernel(const OptTensor *__r
     if (kOp == kSoloStep && last && f.finite) *a.step = at.t;
     if (kOp == kSoloClip)
         for (int k = team; k < n_chunks; k += kTeams)
-            clip_chunk<false>(ten, chunks[k], tid, [&] { return f; });
+            clip_chunk<false>(chunks[k], tid, [&] { return f; });
     if (kOp == kSoloStep)
         for (int k = team; k < n_chunks; k += kTeams)
-            adamw_chunk<kOptThreads, false, false>(ten, chunks[k], a, tid, [&] { return StepIn{f, at}; });
+            adamw_chunk<kOptThreads, false, false>(chunks[k], a, tid, [&] { return StepIn{f, at}; });
 }
 
-// Writes a batch of a list's tensors, which come as kernel arguments (no host
-// memory to keep alive, and capturable), and their chunks: one block a tensor.
-__global__ __launch_bounds__(kOptThreads) void tensor_list_kernel(OptBatch b, OptTensor *ten,
-                                                                  OptChunk *chunks) {
-    const int k = blockIdx.x;
-    if (threadIdx.x == 0) ten[b.first + k] = b.ten[k];
-    const int64_t n = b.n[k], phase = b.ten[k].phase, nc = opt_chunks(n, phase);
+// Writes the chunks of a batch of a list's tensors, which come as kernel
+// arguments (no host memory to keep alive, and capturable): one block a tensor.
+__global__ __launch_bounds__(kOptThreads) void tensor_list_kernel(OptBatch b, OptChunk *chunks) {
+    const OptChunk t = b.ten[blockIdx.x];
+    const int64_t n = b.n[blockIdx.x], phase = t.lead, nc = opt_chunks(n, phase);
+    const auto at = [](void *p, int64_t start, uint32_t bf16) {
+        return static_cast<void *>(static_cast<char *>(p) + start * (bf16 ? 2 : 4));
+    };
     for (int64_t c = threadIdx.x; c < nc; c += kOptThreads) {
         const int64_t start = max<int64_t>(c * kOptChunk - phase, 0);
         const int64_t count = min((c + 1) * kOptChunk - phase, n) - start;
         const int64_t lead = (c == 0 && phase > 0) ? min<int64_t>(kOptAlign - phase, count) : 0;
-        chunks[b.chunk0[k] + c] = OptChunk{b.first + k, static_cast<uint16_t>(count),
-                                           static_cast<uint16_t>(lead), start};
+        OptChunk r = t;
+        r.g = at(t.g, start, t.types & kOptGradBf16);
+        r.out = at(t.out, start, t.types & kOptOutBf16);
+        if (t.w) r.w = at(t.w, start, t.types & kOptWeightBf16);
+        if (t.w32) r.w32 = t.w32 + start;
+        if (t.m) r.m = t.m + start;
+        if (t.v) r.v = t.v + start;
+        r.count = static_cast<uint16_t>(count);
+        r.lead = static_cast<uint16_t>(lead);
+        chunks[b.chunk0[blockIdx.x] + c] = r;
     }
 }
 
@@ -521,7 +517,7 @@ hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, cons
         n_stream = L.n_chunks - (scaled ? static_cast<int>(static_cast<double>(L.n_chunks) * kOptCached / L.g_bytes) : 0);
     ProfScope prof(sums ? "grad_squares" : "adamw_count", st);
     hipLaunchKernelGGL(grad_squares_kernel, dim3(sums ? nm.n_part : 1), dim3(kOptThreads), 0, st,
-                       L.ten, L.chunks, sums ? L.n_chunks : 0, n_stream, sums ? L.g_types : 0u, nm.part,
+                       L.chunks, sums ? L.n_chunks : 0, n_stream, sums ? L.g_types : 0u, nm.part,
                        step, beta1, beta2, at);
     return hipGetLastError();
 }
@@ -530,18 +526,17 @@ hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, cons
 
 int opt_norm_blocks(int n_chunks) { return n_chunks < kOptMaxPart ? n_chunks : kOptMaxPart; }
 
-hipError_t launch_tensor_list(const OptBatch &b, int count, OptTensor *ten, OptChunk *chunks,
-                              hipStream_t st) {
+hipError_t launch_tensor_list(const OptBatch &b, int count, OptChunk *chunks, hipStream_t st) {
     ProfScope prof("tensor_list", st);
     hipLaunchKernelGGL(tensor_list_kernel, dim3(static_cast<unsigned>(count)), dim3(kOptThreads), 0,
-                       st, b, ten, chunks);
+                       st, b, chunks);
     return hipGetLastError();
 }
 
 hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st) {
     if (L.n_chunks <= kSoloNormChunks) {
         ProfScope prof("grad_norm", st);
-        hipLaunchKernelGGL(solo_kernel<kSoloNorm>, dim3(1), dim3(kSoloThreads), 0, st, L.ten, L.chunks,
+        hipLaunchKernelGGL(solo_kernel<kSoloNorm>, dim3(1), dim3(kSoloThreads), 0, st, L.chunks,
                            L.n_chunks, L.g_types, StepArgs{nm, {}, nullptr, nullptr, nullptr});
         return hipGetLastError();
     }
@@ -555,7 +550,7 @@ hipError_t launch_grad_norm(const OptList &L, const OptNorm &nm, hipStream_t st)
 hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st) {
     if (L.n_chunks <= kSoloClipChunks) {
         ProfScope prof("grad_clip", st);
-        hipLaunchKernelGGL(solo_kernel<kSoloClip>, dim3(1), dim3(kSoloThreads), 0, st, L.ten, L.chunks,
+        hipLaunchKernelGGL(solo_kernel<kSoloClip>, dim3(1), dim3(kSoloThreads), 0, st, L.chunks,
                            L.n_chunks, L.g_types, StepArgs{nm, {}, nullptr, nullptr, nullptr});
         return hipGetLastError();
     }
@@ -565,7 +560,7 @@ hipError_t launch_grad_clip(const OptList &L, const OptNorm &nm, hipStream_t st)
     }
     ProfScope prof("grad_clip", st);
     const auto kernel = L.g_bytes + L.out_bytes > kOptKept ? grad_clip_kernel<true> : grad_clip_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(L.n_chunks)), dim3(kOptThreads), 0, st, L.ten,
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(L.n_chunks)), dim3(kOptThreads), 0, st,
                        L.chunks, L.n_chunks, nm);
     return hipGetLastError();
 }
@@ -574,7 +569,7 @@ hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp,
                         int64_t *step, OptStep *at, hipStream_t st) {
     if (L.n_chunks <= kSoloStepChunks) {
         ProfScope prof("adamw", st);
-        hipLaunchKernelGGL(solo_kernel<kSoloStep>, dim3(1), dim3(kSoloThreads), 0, st, L.ten, L.chunks,
+        hipLaunchKernelGGL(solo_kernel<kSoloStep>, dim3(1), dim3(kSoloThreads), 0, st, L.chunks,
                            L.n_chunks, L.g_types, StepArgs{nm, hp, lr, at, step});
         return hipGetLastError();
     }
@@ -584,7 +579,7 @@ hipError_t launch_adamw(const OptList &L, const OptNorm &nm, const OptAdamW &hp,
     const auto kernel = L.g_bytes > kOptCached             ? adamw_kernel<true, true>
                         : L.g_bytes + L.w_bytes > kOptKept ? adamw_kernel<true, false>
                                                              : adamw_kernel<false, false>;
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(L.n_chunks)), dim3(kStepThreads), 0, st, L.ten,
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(L.n_chunks)), dim3(kStepThreads), 0, st,
                        L.chunks, L.n_chunks, StepArgs{nm, hp, lr, at, step});
     return hipGetLastError();
 }
