@@ -561,8 +561,9 @@ size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
  * and the tensors have to stay while the list is used, and a call on another
  * stream has to be ordered behind the build. A tensor that moves needs a new
  * build. n_tensors and any n may be 0; n < 2^35 and fewer than 2^23 chunks
- * of 4096 elements in all (each tensor with 63 elements more). Arrays of one list must not overlap (out = g
- * apart): DSTD_ERR_PARAM.
+ * of 4096 elements in all (each tensor with 63 elements more). Arrays of one
+ * list must not overlap (out = g apart): DSTD_ERR_PARAM. The calls' other
+ * arguments (norm, lr, step, ws) lie outside them.
  */
 dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
                                    size_t mem_bytes, dstd_tensor_list *list, void *stream);
@@ -582,8 +583,8 @@ dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, 
 
 /*
  * Clips the gradients to a norm of at most max_norm (> 0 or +INFINITY):
- * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c rounded
- * to fp32 once, each product once to its type). A norm that is not finite
+ * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c and the
+ * products in fp32, rounded to bf16 where out is). A norm that is not finite
  * clips nothing (c = 1).
  *  norm [1]   norm_given = 0: out, the norm before clipping, or NULL;
  *             norm_given = 1: in, the norm to clip by, for gradients that are
@@ -594,8 +595,8 @@ dstd_status dstd_grad_clip(const dstd_tensor_list *list, double max_norm, float 
                            int32_t norm_given, void *ws, size_t ws_bytes, void *stream);
 
 /*
- * AdamW's constants: 0 <= beta < 1, eps > 0 (not 0 in fp32), lr and
- * weight_decay finite and >= 0, max_norm > 0 or +INFINITY
+ * AdamW's constants: 0 <= beta < 1, eps > 0, lr and weight_decay >= 0 (the
+ * three finite in fp32, and eps not 0 there), max_norm > 0 or +INFINITY
  * (DSTD_ERR_PARAM otherwise).
  */
 typedef struct {

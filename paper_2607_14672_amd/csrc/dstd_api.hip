@@ -1283,12 +1283,12 @@ dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_param
     dstd_status s = check_list(list);
     if (s != DSTD_OK) return s;
     if (!p) return fail(DSTD_ERR_NULL, "params is NULL");
-    if (!(isfinite(p->lr) && p->lr >= 0.0)) return fail(DSTD_ERR_PARAM, "lr must be finite and >= 0");
+    if (!(isfinite((float)p->lr) && p->lr >= 0.0)) return fail(DSTD_ERR_PARAM, "lr must be finite and >= 0");
     if (!(p->beta1 >= 0.0 && p->beta1 < 1.0 && p->beta2 >= 0.0 && p->beta2 < 1.0))
         return fail(DSTD_ERR_PARAM, "need 0 <= beta1, beta2 < 1");
     if (!(isfinite((float)p->eps) && (float)p->eps > 0.f))
         return fail(DSTD_ERR_PARAM, "eps must be finite and > 0 in fp32");
-    if (!(isfinite(p->weight_decay) && p->weight_decay >= 0.0))
+    if (!(isfinite((float)p->weight_decay) && p->weight_decay >= 0.0))
         return fail(DSTD_ERR_PARAM, "weight_decay must be finite and >= 0");
     if ((s = check_max_norm(p->max_norm)) != DSTD_OK) return s;
     if ((s = check_norm(norm, norm_given)) != DSTD_OK) return s;

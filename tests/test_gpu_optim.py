@@ -391,6 +391,28 @@ def test_adamw_silent_weights_stay(dev):
     assert torch.equal(w, kept * 0.75) and step.item() == 2  # powers of two: exact
 
 
+def test_adamw_of_empty_tensors_counts_its_step(dev):
+    import torch
+    from paper_2607_14672_amd import dstd
+    e = [torch.empty(s, device=dev) for s in ((0,), (3, 0)) * 4]
+    tl = dstd.make_tensor_list(e[:2], weights=e[2:4], m=e[4:6], v=e[6:])
+    step = torch.full((1,), 7, dtype=torch.int64, device=dev)
+    norm = dstd.adamw_step(tl, dstd.make_adamw(max_norm=1.0), step)
+    assert norm.item() == 0.0 and step.item() == 8
+    assert dstd.grad_clip(tl, 1.0).item() == 0.0
+
+
+def test_scalar_tensors_and_learning_rate_zero(dev):
+    """Tensors without dimensions; a rate of zero moves moments alone."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    g, w, m, v = (torch.tensor(x, device=dev) for x in (2.0, 1.0, 0.0, 0.0))
+    step = torch.zeros(1, dtype=torch.int64, device=dev)
+    tl = dstd.make_tensor_list([g], weights=[w], m=[m], v=[v])
+    dstd.adamw_step(tl, dstd.make_adamw(beta1=0.5, beta2=0.5), step, lr=torch.zeros(1, device=dev))
+    assert (w.item(), m.item(), v.item(), step.item()) == (1.0, 1.0, 2.0, 1)
+
+
 @pytest.mark.parametrize("value", [math.inf, math.nan])
 def test_adamw_skips_a_step_whose_norm_is_not_finite(dev, value):
     import torch

@@ -162,7 +162,7 @@ def test_norm_clip_and_step_arguments():
 
 
 @pytest.mark.parametrize("kw", [
-    dict(lr=-1e-3), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=-0.1), dict(beta1=1.0),
+    dict(lr=-1e-3), dict(lr=math.nan), dict(lr=math.inf), dict(lr=1e60), dict(weight_decay=1e60), dict(beta1=-0.1), dict(beta1=1.0),
     dict(beta1=math.nan), dict(beta2=1.0), dict(beta2=2.0), dict(eps=0.0), dict(eps=-1e-8),
     dict(eps=1e-60), dict(eps=math.inf), dict(weight_decay=-0.1), dict(weight_decay=math.inf),
     dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=math.nan),
