@@ -717,18 +717,18 @@ class TensorList:
         self.ws_bytes = dstd_tensor_list_workspace_size(c)
 
 
-def _list_array(x, like, dev, dtypes, what):
-    torch = _torch()
+def _list_array(torch, x, like, dev, dtypes, what, k):
+    """Address of one array of tensor k of a list, checked."""
     if not isinstance(x, torch.Tensor):
-        raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
+        raise TypeError(f"{what} {k} must be a tensor, got {type(x).__name__}")
     if x.dtype not in dtypes:
-        raise TypeError(f"{what} must be one of {dtypes}, got {x.dtype}")
+        raise TypeError(f"{what} {k} must be one of {list(dtypes)}, got {x.dtype}")
     if dev < 0 or x.get_device() != dev:
-        raise ValueError(f"{what} must live on the GPU of the list's other tensors")
-    if x.shape != like.shape:
-        raise ValueError(f"{what} has shape {tuple(x.shape)}, its gradient {tuple(like.shape)}")
+        raise ValueError(f"{what} {k} must live on the GPU of the list's other tensors")
+    if x is not like and x.shape != like.shape:
+        raise ValueError(f"{what} {k} has shape {tuple(x.shape)}, its gradient {tuple(like.shape)}")
     if not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
+        raise ValueError(f"{what} {k} must be contiguous")
     return x.data_ptr()
 
 
@@ -748,7 +748,7 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
     factors per tensor (default 1). All contiguous, on one GPU; entries of
     master and out may be None."""
     torch = _torch()
-    both = (torch.float32, torch.bfloat16)
+    code = {torch.float32: DSTD_F32, torch.bfloat16: DSTD_BF16}
     f32 = (torch.float32,)
     grads = list(grads)
     n = len(grads)
@@ -761,21 +761,22 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
         raise ValueError("a list needs a tensor")
     dev = grads[0].get_device() if isinstance(grads[0], torch.Tensor) else -1
     arr = (dstd_tensor * n)()
-    for k, (t, g) in enumerate(zip(arr, grads)):
-        t.g = _list_array(g, g, dev, both, f"gradient {k}")
-        t.g_dtype, t.n = _wdtype(g), g.numel()
-        w, mk, vk, w32, o = (c[k] for c in cols)
+    for k, (t, g, w, mk, vk, w32, o, ls, ds) in enumerate(zip(arr, grads, *cols, *scales)):
+        t.g = _list_array(torch, g, g, dev, code, "gradient", k)
+        t.g_dtype, t.n = code[g.dtype], g.numel()
         if w is not None:
-            t.w, t.w_dtype = _list_array(w, g, dev, both, f"weight {k}"), _wdtype(w)
+            t.w = _list_array(torch, w, g, dev, code, "weight", k)
+            t.w_dtype = code[w.dtype]
         if mk is not None:
-            t.m = _list_array(mk, g, dev, f32, f"first moment {k}")
+            t.m = _list_array(torch, mk, g, dev, f32, "first moment", k)
         if vk is not None:
-            t.v = _list_array(vk, g, dev, f32, f"second moment {k}")
+            t.v = _list_array(torch, vk, g, dev, f32, "second moment", k)
         if w32 is not None:
-            t.w32 = _list_array(w32, g, dev, f32, f"master weight {k}")
+            t.w32 = _list_array(torch, w32, g, dev, f32, "master weight", k)
         if o is not None:
-            t.out, t.out_dtype = _list_array(o, g, dev, both, f"output {k}"), _wdtype(o)
-        t.lr_scale, t.decay_scale = (float(s[k]) for s in scales)
+            t.out = _list_array(torch, o, g, dev, code, "output", k)
+            t.out_dtype = code[o.dtype]
+        t.lr_scale, t.decay_scale = ls, ds
     device = torch.device("cuda", dev)
     mem = workspace(dstd_tensor_list_size(n, arr), device)
     c = dstd_tensor_list()
