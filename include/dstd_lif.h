@@ -612,7 +612,7 @@ typedef struct {
  * in fp32 (the powers in 64 bits).
  *  lr [1]     learning rate on the device, for schedules under a captured
  *             graph, or NULL: p->lr.
- *  step [1]   in/out, on the device: steps done (>= 0).
+ *  step [1]   in/out, on the device: steps done (>= 0); every list has its own.
  *  norm [1]   as in dstd_grad_clip. The norm is summed if norm is not NULL or
  *             max_norm is finite; a step whose norm is then not finite leaves
  *             w, w32, m, v and step as they were. With norm = NULL and

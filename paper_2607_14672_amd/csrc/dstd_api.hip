@@ -1162,8 +1162,8 @@ OptWs opt_ws_layout() {
 }
 
 dstd::OptList opt_list(const dstd_tensor_list *l) {
-    return dstd::OptList{static_cast<const dstd::OptChunk *>(l->mem), (int)l->n_chunks, l->g_bytes, l->out_bytes, l->w_bytes,
-                         l->g_types};
+    return dstd::OptList{static_cast<const dstd::OptChunk *>(l->mem), (int)l->n_chunks, l->g_bytes,
+                         l->out_bytes, l->w_bytes, l->g_types};
 }
 
 dstd_status check_max_norm(double max_norm) {

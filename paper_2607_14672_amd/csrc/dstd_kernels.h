@@ -251,11 +251,11 @@ hipError_t launch_exact_backward(const LifConst &C, int64_t B, int64_t N_in, int
 // Tensor lists, the global gradient norm, clipping and AdamW (dstd_optim.hip).
 // A list's device memory: its chunks of at most kOptChunk elements, in tensor
 // order (empty tensors have none), with all that a block has to know of them in
-// one 64-byte record. Chunks end where
-// (element + phase) is a multiple of kOptChunk: phase is the place of the
-// tensor's first element among kOptAlign elements (256 bytes of fp32, 128 of
-// bf16), so that chunks start at whole cache lines. `lead` elements of a
-// chunk (of a tensor's first, if phase > 0) lie before its first whole line.
+// one 64-byte record. Chunks end where (element + phase) is a multiple of
+// kOptChunk: phase is the place of the tensor's first element among kOptAlign
+// elements (256 bytes of fp32, 128 of bf16), so that chunks start at whole
+// cache lines. `lead` elements of a chunk (of a tensor's first, if phase > 0)
+// lie before its first whole line.
 constexpr int64_t kOptChunk = 4096;
 constexpr int kOptAlign = 64;
 constexpr int kOptMaxPart = 1024;  // partial sums of squares of one norm
@@ -268,6 +268,7 @@ struct OptChunk {
     uint32_t types;
     uint16_t count, lead;
 };
+static_assert(sizeof(OptChunk) == 64, "one record, one cache line");
 // chunks of n elements whose first has place `phase` (0 for none)
 __host__ __device__ inline int64_t opt_chunks(int64_t n, int64_t phase) {
     return n > 0 ? (n + phase + kOptChunk - 1) / kOptChunk : 0;
@@ -285,6 +286,7 @@ struct OptBatch {
     OptChunk ten[kOptBatch];  // as one chunk that begins with the tensor; `lead` is its phase
     int64_t n[kOptBatch], chunk0[kOptBatch];
 };
+static_assert(sizeof(OptBatch) <= 4096 - 64, "kernel arguments");
 // The norm of a call: n_part partial sums of squares, or n_part = -1 where it
 // is given in *norm, or not asked for (norm null).
 struct OptNorm {

@@ -712,8 +712,8 @@ class TensorList:
     C struct). It keeps the tensors and the table alive; a tensor that is
     replaced by another needs a new list."""
 
-    def __init__(self, c, mem, tensors, device):
-        self.c, self.mem, self.tensors, self.device = c, mem, tensors, device
+    def __init__(self, c, mem, tensors, device, stream):
+        self.c, self.mem, self.tensors, self.device, self.stream = c, mem, tensors, device, stream
         self.ws_bytes = dstd_tensor_list_workspace_size(c)
 
 
@@ -780,10 +780,11 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
     device = torch.device("cuda", dev)
     mem = workspace(dstd_tensor_list_size(n, arr), device)
     c = dstd_tensor_list()
+    stream = _stream(device)
     with torch.cuda.device(device):
         _check("dstd_tensor_list_build",
-               dstd_tensor_list_build(n, arr, _ptr(mem), mem.numel(), c, _stream(device)))
-    return TensorList(c, mem, (grads, *cols), device)
+               dstd_tensor_list_build(n, arr, _ptr(mem), mem.numel(), c, stream))
+    return TensorList(c, mem, (grads, *cols), device, stream)
 
 
 def _scalar(x, dtype, dev, what):
@@ -802,6 +803,8 @@ def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
             norm = torch.empty(1, dtype=torch.float32, device=tl.device)
     if ws is None or ws.numel() < tl.ws_bytes:
         ws = workspace(tl.ws_bytes, tl.device)
+    elif ws.device != tl.device:
+        raise ValueError(f"ws must be on {tl.device}")
     if norm is None:
         return None, None, ws
     return norm, _scalar(norm, _torch().float32, tl.device, "norm"), ws
@@ -813,6 +816,8 @@ def _launch(tl: TensorList, name, fn, *args):
     torch = _torch()
     dev = tl.device.index
     stream = torch._C._cuda_getCurrentRawStream(dev)  # current_stream() builds an object: 2 us
+    if stream != tl.stream:  # the table may not be reused before this stream has read it
+        tl.mem.record_stream(torch.cuda.current_stream(dev))
     if torch.cuda.current_device() == dev:
         _check(name, fn(*args, stream))
     else:
@@ -848,7 +853,7 @@ def adamw_step(tl: TensorList, hp: dstd_adamw_params, step, lr=None, norm=None,
                norm_given: bool = False, ws=None):
     """One AdamW step of the list's tensors, their gradients clipped to
     hp.max_norm on the way. `step` [1] int64: steps done, on the device, counted
-    up; `lr` [1] f32 on the device replaces hp.lr. Returns the norm before
+    up (one for each list); `lr` [1] f32 on the device replaces hp.lr. Returns the norm before
     clipping (None where none is formed: no `norm` given and hp.max_norm infinite);
     a step whose norm is not finite changes nothing."""
     norm, ptr, ws = _optim_args(tl, norm, norm_given, ws, math.isfinite(hp.max_norm))

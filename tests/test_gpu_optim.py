@@ -538,6 +538,27 @@ def test_lists_that_exceed_the_caches(dev, n, g_type):
 
 
 # --------------------------------------------------- streams, graphs, lists --
+def test_a_list_dropped_while_another_stream_reads_it(dev):
+    """Built and freed on one stream, used on another: its table stays until
+    that stream is through, whatever is allocated meanwhile."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    g = [torch.ones(1000, device=dev) for _ in range(2000)]
+    side = torch.cuda.Stream(dev)
+    got = []
+    for _ in range(10):
+        tl = dstd.make_tensor_list(g)
+        size = tl.mem.numel()
+        side.wait_stream(torch.cuda.current_stream(dev))
+        with torch.cuda.stream(side):
+            got.append(dstd.grad_norm(tl))
+        del tl
+        torch.zeros(size, dtype=torch.uint8, device=dev)
+    torch.cuda.synchronize()
+    want = math.sqrt(2e6)
+    _close([x.item() for x in got], [want] * 10, [U * MORE * want] * 10, "norm")
+
+
 def test_one_list_on_two_streams_at_once(dev):
     """Norms of one list on two streams, each with its workspace."""
     import torch
@@ -664,6 +685,8 @@ def test_refusals_of_the_helpers(dev):
         dstd.grad_clip(tl, 1.0, norm_given=True)
     with pytest.raises(ValueError, match="norm"):
         dstd.grad_norm(tl, norm=torch.zeros(1))
+    with pytest.raises(ValueError, match="ws"):
+        dstd.grad_norm(tl, ws=torch.zeros(tl.ws_bytes, dtype=torch.uint8))
     w = [torch.zeros(8, 6, device=dev) for _ in range(3)]
     tl = dstd.make_tensor_list([g], weights=w[:1], m=w[1:2], v=w[2:])
     with pytest.raises(ValueError, match="step"):
