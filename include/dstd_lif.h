@@ -558,12 +558,14 @@ size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
 /*
  * Writes the table of `tensors` (host array) to mem (256-byte aligned) on
  * `stream` and fills *list. The host array may go once the call returns; mem
- * and the tensors have to stay while the list is used, and a call on another
- * stream has to be ordered behind the build. A tensor that moves needs a new
- * build. n_tensors and any n may be 0; n < 2^35 and fewer than 2^23 chunks
- * of 4096 elements in all (each tensor with 63 elements more). Arrays of one
- * list must not overlap (out = g apart): DSTD_ERR_PARAM. The calls' other
- * arguments (norm, lr, step, ws) lie outside them.
+ * and the tensors have to stay while the list is used, or a graph that calls
+ * were captured into is replayed, and a call on another stream has to be
+ * ordered behind the build (a build that is captured writes the table when its
+ * graph is replayed). A tensor that moves needs a new build. n_tensors and any
+ * n may be 0; n < 2^35 and fewer than 2^23 chunks of 4096 elements in all (each
+ * tensor with 63 elements more). Arrays of one list must not overlap (out = g
+ * apart): DSTD_ERR_PARAM. The calls' other arguments (norm, lr, step, ws) lie
+ * outside them.
  */
 dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
                                    size_t mem_bytes, dstd_tensor_list *list, void *stream);

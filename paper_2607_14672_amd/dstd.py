@@ -710,10 +710,18 @@ def mse_grad(t_out, target):
 class TensorList:
     """The tensors of a training step and their table on the device (``c``: the
     C struct). It keeps the tensors and the table alive; a tensor that is
-    replaced by another needs a new list."""
+    replaced by another, or moved to other memory (``.data``, ``set_``,
+    ``resize_``), needs a new list, and a graph that calls were captured into
+    needs the list for as long as it is replayed.
 
-    def __init__(self, c, mem, tensors, device, stream):
+    The table is written on the stream that is current when the list is built
+    (``stream``; ``built``: the event behind it). Calls on another stream wait
+    for it. A list built inside a capture (``captured``) has its table once the
+    graph is replayed, and is for calls inside captures alone."""
+
+    def __init__(self, c, mem, tensors, device, stream, built=None, captured=False):
         self.c, self.mem, self.tensors, self.device, self.stream = c, mem, tensors, device, stream
+        self.built, self.captured = built, captured
         self.ws_bytes = dstd_tensor_list_workspace_size(c)
 
 
@@ -784,7 +792,9 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
     with torch.cuda.device(device):
         _check("dstd_tensor_list_build",
                dstd_tensor_list_build(n, arr, _ptr(mem), mem.numel(), c, stream))
-    return TensorList(c, mem, (grads, *cols), device, stream)
+        captured = torch.cuda.is_current_stream_capturing()
+        built = None if captured else torch.cuda.current_stream(device).record_event()
+    return TensorList(c, mem, (grads, *cols), device, stream, built, captured)
 
 
 def _scalar(x, dtype, dev, what):
@@ -810,14 +820,33 @@ def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
     return norm, _scalar(norm, _torch().float32, tl.device, "norm"), ws
 
 
+def _behind_build(torch, tl: TensorList, dev):
+    """Orders the current stream behind the launches that write the list's table,
+    and the table's memory behind the current stream. A capture cannot wait for
+    work outside it: its graph is replayed behind the build by whoever replays
+    it (torch.cuda.graph waits for all earlier work before it captures)."""
+    with torch.cuda.device(dev):
+        capturing = torch.cuda.is_current_stream_capturing()
+    if tl.captured and not capturing:
+        raise RuntimeError("a list built inside a capture is for calls inside captures: "
+                           "its table is written when the graph is replayed")
+    stream = torch.cuda.current_stream(dev)
+    if tl.built is not None and not capturing:
+        if tl.built.query():
+            tl.built = None
+        else:
+            stream.wait_event(tl.built)
+    tl.mem.record_stream(stream)  # not reused before this stream has read it
+
+
 def _launch(tl: TensorList, name, fn, *args):
     """One call on the list's device (launches go to the current one) and on
     that device's current stream."""
     torch = _torch()
     dev = tl.device.index
     stream = torch._C._cuda_getCurrentRawStream(dev)  # current_stream() builds an object: 2 us
-    if stream != tl.stream:  # the table may not be reused before this stream has read it
-        tl.mem.record_stream(torch.cuda.current_stream(dev))
+    if stream != tl.stream or tl.captured:
+        _behind_build(torch, tl, dev)
     if torch.cuda.current_device() == dev:
         _check(name, fn(*args, stream))
     else:

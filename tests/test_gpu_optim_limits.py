@@ -1,0 +1,58 @@
+"""GPU checks of the tensor lists, the global gradient norm, clipping and the
+AdamW step at the limits of their types and of their launch forms. Tolerances
+as in test_gpu_optim.py, where a test says nothing else: u = 2^-24 and
+u16 = 2^-8 are the half steps of fp32 and bf16."""
+import math
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_optim import HP, MORE, U, U16, Arena, Train, _check_step, _close, _norm64, _normal
+from tests.test_gpu_optim import dev  # noqa: F401 (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ streams --
+DELAY = 20_000_000  # clock ticks of a kernel that only waits: 10 to 200 ms
+
+
+def test_a_list_used_on_another_stream_waits_for_its_build(dev):
+    """The building stream is held up; nothing orders the other one but the call."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    g = [torch.full((3000,), float(k % 5), device=dev) for k in range(100)]
+    ref = _norm64([x.double().cpu().numpy() for x in g])
+    build, side = torch.cuda.Stream(dev), torch.cuda.Stream(dev)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(build):
+        torch.cuda._sleep(DELAY)
+        tl = dstd.make_tensor_list(g)
+    assert not tl.built.query()
+    with torch.cuda.stream(side):
+        norm = dstd.grad_norm(tl)
+    torch.cuda.synchronize()
+    _close([norm.item()], [ref], [U * MORE * ref], "norm")
+    with torch.cuda.stream(side):  # the build is long done
+        assert torch.equal(dstd.grad_norm(tl), norm)
+    assert tl.built is None
+
+
+def test_a_list_built_inside_a_capture_is_for_captures(dev):
+    import torch
+    from paper_2607_14672_amd import dstd
+    g = [torch.ones(500, device=dev) for _ in range(40)]
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tl = dstd.make_tensor_list(g)
+    with pytest.raises(RuntimeError, match="inside a capture"):
+        dstd.grad_norm(tl)
+    with torch.cuda.graph(other):
+        norm = dstd.grad_norm(tl)
+    graph.replay()
+    for _ in range(3):
+        norm.fill_(-1.0)
+        other.replay()
+        torch.cuda.synchronize()
+        _close([norm.item()], [math.sqrt(20_000)], [U * MORE * 200], "norm")
