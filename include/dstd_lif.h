@@ -565,7 +565,8 @@ size_t dstd_tensor_list_size(int64_t n_tensors, const dstd_tensor *tensors);
  * n may be 0; n < 2^35 and fewer than 2^23 chunks of 4096 elements in all (each
  * tensor with 63 elements more). Arrays of one list must not overlap (out = g
  * apart): DSTD_ERR_PARAM. The calls' other arguments (norm, lr, step, ws) lie
- * outside them.
+ * outside them, and none of them in another or in the list's memory unless both
+ * are only read (the calls refuse that with DSTD_ERR_PARAM).
  */
 dstd_status dstd_tensor_list_build(int64_t n_tensors, const dstd_tensor *tensors, void *mem,
                                    size_t mem_bytes, dstd_tensor_list *list, void *stream);

@@ -1166,6 +1166,37 @@ dstd::OptList opt_list(const dstd_tensor_list *l) {
                          l->out_bytes, l->w_bytes, l->g_types};
 }
 
+// Places that a call of a list reads or writes beside the list's arrays: the
+// table, the workspace, and the scalars on the device. None may lie in another
+// if one of them is written: blocks that read the other would see either value
+// (and addresses, where it is the table's).
+struct Place {
+    const void *p;  // null: none
+    size_t bytes, align;
+    bool written;
+    const char *what;
+};
+template <size_t N> dstd_status check_places(const Place (&places)[N]) {
+    for (size_t i = 0; i < N; ++i) {
+        const Place &a = places[i];
+        if (!a.p) continue;
+        const uintptr_t lo = (uintptr_t)a.p;
+        if (lo % a.align != 0) return fail(DSTD_ERR_PARAM, "%s is not aligned to %zu bytes", a.what, a.align);
+        for (size_t k = 0; k < i; ++k) {
+            const Place &b = places[k];
+            const uintptr_t at = (uintptr_t)b.p;
+            if (b.p && (a.written || b.written) && lo < at + b.bytes && at < lo + a.bytes)
+                return fail(DSTD_ERR_PARAM, "%s and %s overlap", b.what, a.what);
+        }
+    }
+    return DSTD_OK;
+}
+Place table_place(const dstd_tensor_list *l) {
+    return Place{l->mem, (size_t)l->n_chunks * sizeof(dstd::OptChunk), kAlign, false, "the list's table"};
+}
+Place ws_place(const void *ws) { return Place{ws, opt_ws_layout().total, kAlign, true, "the workspace"}; }
+Place norm_place(const float *norm, bool given) { return Place{norm, 4, 4, !given, "norm"}; }
+
 dstd_status check_max_norm(double max_norm) {
     if (!(max_norm > 0.0)) return fail(DSTD_ERR_PARAM, "max_norm must be > 0 or +inf (got %g)", max_norm);
     return DSTD_OK;
@@ -1258,6 +1289,7 @@ dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, 
     if (!norm) return fail(DSTD_ERR_NULL, "norm is NULL");
     const OptWs w = opt_ws_layout();
     if ((s = check_ws(ws, ws_bytes, w.total)) != DSTD_OK) return s;
+    if ((s = check_places({table_place(list), ws_place(ws), norm_place(norm, false)})) != DSTD_OK) return s;
     const dstd::OptList L = opt_list(list);
     const dstd::OptNorm nm{at<double>(ws, w.part), dstd::opt_norm_blocks(L.n_chunks), norm, INFINITY};
     return hip_status(dstd::launch_grad_norm(L, nm, static_cast<hipStream_t>(stream)), "grad_norm launch");
@@ -1271,6 +1303,8 @@ dstd_status dstd_grad_clip(const dstd_tensor_list *list, double max_norm, float 
     if ((s = check_norm(norm, norm_given)) != DSTD_OK) return s;
     const OptWs w = opt_ws_layout();
     if ((s = check_ws(ws, ws_bytes, w.total)) != DSTD_OK) return s;
+    if ((s = check_places({table_place(list), ws_place(ws), norm_place(norm, norm_given)})) != DSTD_OK)
+        return s;
     const dstd::OptList L = opt_list(list);
     const dstd::OptNorm nm{at<double>(ws, w.part), norm_given ? -1 : dstd::opt_norm_blocks(L.n_chunks),
                            norm, max_norm};
@@ -1297,6 +1331,9 @@ dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_param
         return fail(DSTD_ERR_NULL, "a tensor of the list has no weights");
     const OptWs w = opt_ws_layout();
     if ((s = check_ws(ws, ws_bytes, w.total)) != DSTD_OK) return s;
+    if ((s = check_places({table_place(list), ws_place(ws), norm_place(norm, norm_given),
+                           Place{lr, 4, 4, false, "lr"}, Place{step, 8, 8, true, "step"}})) != DSTD_OK)
+        return s;
     const dstd::OptList L = opt_list(list);
     const bool sums = !norm_given && (norm || isfinite(p->max_norm));
     const dstd::OptNorm nm{at<double>(ws, w.part), sums ? dstd::opt_norm_blocks(L.n_chunks) : -1,

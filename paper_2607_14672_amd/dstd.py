@@ -815,6 +815,8 @@ def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
         ws = workspace(tl.ws_bytes, tl.device)
     elif ws.device != tl.device:
         raise ValueError(f"ws must be on {tl.device}")
+    elif not ws.is_contiguous():  # an expanded tensor has less memory than elements
+        raise ValueError("ws must be contiguous")
     if norm is None:
         return None, None, ws
     return norm, _scalar(norm, _torch().float32, tl.device, "norm"), ws

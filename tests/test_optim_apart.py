@@ -1,0 +1,64 @@
+"""Places of the tensor lists' calls that must lie apart or be aligned, on the
+CPU: refused on the host, before anything touches a device."""
+import pytest
+
+from paper_2607_14672_amd import dstd
+
+MEM, WS, NORM, STEP, LR = 1 << 40, 1 << 20, 4, 8, 16
+
+
+def _list():
+    """An empty list at MEM, said to hold 3 chunks of 64 bytes."""
+    lst = dstd.dstd_tensor_list()
+    assert dstd.dstd_tensor_list_build(0, None, MEM, 256, lst, None) == dstd.DSTD_OK
+    lst.n_chunks = 3
+    return lst
+
+
+def _call(name, norm=NORM, step=STEP, lr=LR, ws=WS, given=0):
+    lst, hp = _list(), dstd.make_adamw()
+    need = dstd.dstd_tensor_list_workspace_size(lst)
+    if name == "norm":
+        return dstd.dstd_grad_norm(lst, norm, ws, need, None)
+    if name == "clip":
+        return dstd.dstd_grad_clip(lst, 1.0, norm, given, ws, need, None)
+    return dstd.dstd_adamw_step(lst, hp, lr, step, norm, given, ws, need, None)
+
+
+ALL = ("norm", "clip", "step")
+
+
+@pytest.mark.parametrize("names,kw", [
+    (ALL, dict(ws=MEM)),                        # the table itself as workspace
+    (ALL, dict(norm=WS)), (ALL, dict(norm=WS + 4096)), (ALL, dict(norm=MEM)), (ALL, dict(norm=MEM + 188)),
+    (("clip", "step"), dict(norm=WS, given=1)),
+    (("step",), dict(step=WS + 8)), (("step",), dict(lr=WS + 16)), (("step",), dict(step=MEM + 64)),
+    (("step",), dict(norm=LR)), (("step",), dict(norm=STEP)), (("step",), dict(norm=STEP + 4)),
+    (("step",), dict(lr=STEP)), (("step",), dict(lr=STEP + 4)),
+    (("step",), dict(norm=STEP + 4, given=1)),
+], ids=str)
+def test_overlapping_places_are_refused(names, kw):
+    for name in names:
+        assert _call(name, **kw) == dstd.DSTD_ERR_PARAM, name
+        assert "overlap" in dstd.dstd_last_error()
+
+
+@pytest.mark.parametrize("names,kw", [
+    (ALL, dict(norm=6)), (("clip", "step"), dict(norm=5, given=1)), (("step",), dict(step=12)),
+    (("step",), dict(lr=18)),
+], ids=str)
+def test_places_off_their_alignment_are_refused(names, kw):
+    for name in names:
+        assert _call(name, **kw) == dstd.DSTD_ERR_PARAM, name
+        assert "aligned" in dstd.dstd_last_error()
+
+
+def test_expanded_workspaces_are_refused():
+    """One byte seen many times is no workspace."""
+    import torch
+    tl = dstd.TensorList(_list(), None, (), torch.device("cpu"), 0)
+    ws = torch.empty(1, dtype=torch.uint8).expand(2 * tl.ws_bytes)
+    with pytest.raises(ValueError, match="ws must be contiguous"):
+        dstd._optim_args(tl, None, False, ws, False)
+    ok = torch.empty(tl.ws_bytes, dtype=torch.uint8)
+    assert dstd._optim_args(tl, None, False, ok, False) == (None, None, ok)
