@@ -56,3 +56,29 @@ def test_a_list_built_inside_a_capture_is_for_captures(dev):
         other.replay()
         torch.cuda.synchronize()
         _close([norm.item()], [math.sqrt(20_000)], [U * MORE * 200], "norm")
+
+
+def test_the_table_of_a_dropped_list_is_not_reused_while_it_is_read(dev):
+    """The other stream is held up in front of its call: until it is through, an
+    allocation of the table's size on the building stream gets other memory."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    g = [torch.ones(1000, device=dev) for _ in range(5000)]
+    side = torch.cuda.Stream(dev)
+    tl = dstd.make_tensor_list(g)
+    size, at = tl.mem.numel(), tl.mem.data_ptr()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(DELAY)
+        norm = dstd.grad_norm(tl)
+        read = side.record_event()
+    del tl
+    blocks = [torch.empty(size, dtype=torch.uint8, device=dev) for _ in range(3)]
+    assert not read.query()
+    assert at not in [b.data_ptr() for b in blocks]
+    torch.cuda.synchronize()
+    del blocks
+    want = math.sqrt(5e6)
+    _close([norm.item()], [want], [U * MORE * want], "norm")
+    # the delay over, its memory is there for others again
+    assert at in [torch.empty(size, dtype=torch.uint8, device=dev).data_ptr()]
