@@ -599,8 +599,9 @@ dstd_status dstd_grad_clip(const dstd_tensor_list *list, double max_norm, float 
 
 /*
  * AdamW's constants: 0 <= beta < 1, eps > 0, lr and weight_decay >= 0 (the
- * three finite in fp32, and eps not 0 there), max_norm > 0 or +INFINITY
- * (DSTD_ERR_PARAM otherwise).
+ * three finite in fp32, and eps not 0 there; a beta that is 1 in fp32 is one
+ * that moments in fp32 cannot follow), max_norm > 0 or +INFINITY
+ * (DSTD_ERR_PARAM otherwise). Betas are used to 48 bits.
  */
 typedef struct {
     double lr, beta1, beta2, eps, weight_decay, max_norm;

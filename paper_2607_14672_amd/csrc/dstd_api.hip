@@ -1197,6 +1197,13 @@ Place table_place(const dstd_tensor_list *l) {
 Place ws_place(const void *ws) { return Place{ws, opt_ws_layout().total, kAlign, true, "the workspace"}; }
 Place norm_place(const float *norm, bool given) { return Place{norm, 4, 4, !given, "norm"}; }
 
+// beta in two fp32 parts, hi below beta (the kernels' adamw_one needs lo > 0)
+void split_beta(double beta, float *hi, float *lo) {
+    *hi = (float)beta;
+    if ((double)*hi >= beta) *hi = nextafterf(*hi, 0.f);
+    *lo = (float)(beta - (double)*hi);
+}
+
 dstd_status check_max_norm(double max_norm) {
     if (!(max_norm > 0.0)) return fail(DSTD_ERR_PARAM, "max_norm must be > 0 or +inf (got %g)", max_norm);
     return DSTD_OK;
@@ -1318,8 +1325,8 @@ dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_param
     if (s != DSTD_OK) return s;
     if (!p) return fail(DSTD_ERR_NULL, "params is NULL");
     if (!(isfinite((float)p->lr) && p->lr >= 0.0)) return fail(DSTD_ERR_PARAM, "lr must be finite and >= 0");
-    if (!(p->beta1 >= 0.0 && p->beta1 < 1.0 && p->beta2 >= 0.0 && p->beta2 < 1.0))
-        return fail(DSTD_ERR_PARAM, "need 0 <= beta1, beta2 < 1");
+    if (!(p->beta1 >= 0.0 && (float)p->beta1 < 1.f && p->beta2 >= 0.0 && (float)p->beta2 < 1.f))
+        return fail(DSTD_ERR_PARAM, "need 0 <= beta1, beta2 < 1 in fp32");
     if (!(isfinite((float)p->eps) && (float)p->eps > 0.f))
         return fail(DSTD_ERR_PARAM, "eps must be finite and > 0 in fp32");
     if (!(isfinite((float)p->weight_decay) && p->weight_decay >= 0.0))
@@ -1341,8 +1348,8 @@ dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_param
     dstd::OptAdamW hp{};
     hp.beta1 = p->beta1;
     hp.beta2 = p->beta2;
-    hp.b1 = (float)p->beta1;
-    hp.b2 = (float)p->beta2;
+    split_beta(p->beta1, &hp.b1, &hp.b1_lo);
+    split_beta(p->beta2, &hp.b2, &hp.b2_lo);
     hp.a1 = (float)(1.0 - p->beta1);
     hp.a2 = (float)(1.0 - p->beta2);
     hp.eps = (float)p->eps;

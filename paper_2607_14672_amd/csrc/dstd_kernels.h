@@ -302,7 +302,8 @@ struct OptStep {
 };
 struct OptAdamW {
     double beta1, beta2;
-    float b1, b2, a1, a2;  // betas and 1 - beta
+    float b1, b1_lo, b2, b2_lo;  // beta = b + b_lo to 48 bits, 0 < b_lo <= 2^-24 (0 for beta = 0)
+    float a1, a2;                // 1 - beta
     float eps, lr, decay;
 };
 int opt_norm_blocks(int n_chunks);

@@ -82,3 +82,51 @@ def test_the_table_of_a_dropped_list_is_not_reused_while_it_is_read(dev):
     _close([norm.item()], [want], [U * MORE * want], "norm")
     # the delay over, its memory is there for others again
     assert at in [torch.empty(size, dtype=torch.uint8, device=dev).data_ptr()]
+
+
+# ------------------------------------------------------- moments over steps --
+@pytest.mark.parametrize("n", [4000, 20_000])
+@pytest.mark.parametrize("beta1,beta2", [(0.9, 0.999), (0.999, 0.9999), (0.9999, 0.99999)])
+def test_moments_follow_their_betas_over_many_steps(dev, beta1, beta2, n):
+    """4000 steps against a 64-bit recursion that sees the gradients alone. In
+    the mean over all elements only what all of them share is left: 1 - beta
+    rounded (u), and at worst the two roundings of (1 - beta) g^2 (2 u). The
+    roundings of a moment differ in every step and element (at most u each,
+    evenly spread: u / sqrt(3) in the mean square), so that their mean over n
+    elements has a deviation below u sqrt(4000 / (3 n)) = 0.6 u for n = 4000:
+    3 u and six deviations, 7 u. A beta and a 1 - beta that do not add to 1
+    would be off by 2^-25 / (1 - beta) once the moment is settled."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    steps, bank = 4000, 16
+    gen = torch.Generator(device=dev).manual_seed(n)
+    grads = 1.0 + 0.3 * torch.randn(bank, n, generator=gen, device=dev)
+    g, w, m, v = (torch.zeros(n, device=dev) for _ in range(4))
+    tl = dstd.make_tensor_list([g], weights=[w], m=[m], v=[v])
+    hp = dstd.make_adamw(lr=0.0, beta1=beta1, beta2=beta2)
+    step, ws = torch.zeros(1, dtype=torch.int64, device=dev), dstd.workspace(tl.ws_bytes, dev)
+    m64, v64 = torch.zeros(2, n, dtype=torch.float64, device=dev)
+    g64 = grads.double()
+    for k in range(steps):
+        g.copy_(grads[k % bank])
+        dstd.adamw_step(tl, hp, step, ws=ws)
+        m64.mul_(beta1).add_(g64[k % bank], alpha=1.0 - beta1)
+        v64.mul_(beta2).addcmul_(g64[k % bank], g64[k % bank], value=1.0 - beta2)
+    assert step.item() == steps
+    for got, ref, what in ((m, m64, "m"), (v, v64, "v")):
+        off = float(((got.double() - ref) / ref).mean())
+        assert abs(off) <= 7 * U, f"{what} off by {off:.3g} in the mean"
+
+
+@pytest.mark.parametrize("n", [4000, 20_000])
+@pytest.mark.parametrize("beta2", [0.5, 0.999])
+def test_a_second_moment_that_overflowed_stays_infinite(dev, beta2, n):
+    """Its weight only decays then: m / (inf + eps) is 0."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    g, w, m = (torch.full((n,), x, device=dev) for x in (0.5, 1.0, 0.25))
+    v = torch.full((n,), math.inf, device=dev)
+    tl = dstd.make_tensor_list([g], weights=[w], m=[m], v=[v])
+    step = torch.full((1,), 3, dtype=torch.int64, device=dev)
+    dstd.adamw_step(tl, dstd.make_adamw(lr=0.5, beta2=beta2, weight_decay=0.5), step)
+    assert bool((v == math.inf).all()) and bool((w == 0.75).all())

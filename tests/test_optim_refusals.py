@@ -1,5 +1,6 @@
-"""Places of the tensor lists' calls that must lie apart or be aligned, on the
-CPU: refused on the host, before anything touches a device."""
+"""Places of the tensor lists' calls that must lie apart or be aligned, and
+betas that fp32 cannot hold, on the CPU: refused on the host, before anything
+touches a device."""
 import pytest
 
 from paper_2607_14672_amd import dstd
@@ -62,3 +63,12 @@ def test_expanded_workspaces_are_refused():
         dstd._optim_args(tl, None, False, ws, False)
     ok = torch.empty(tl.ws_bytes, dtype=torch.uint8)
     assert dstd._optim_args(tl, None, False, ok, False) == (None, None, ok)
+
+
+@pytest.mark.parametrize("beta", [1.0 - 2.0 ** -26, 1.0 - 1e-9, 1.0 - 2.0 ** -53])
+def test_betas_that_are_one_in_fp32_are_refused(beta):
+    """A moment in fp32 loses less than half a step of itself: it would stand."""
+    need = dstd.dstd_tensor_list_workspace_size(_list())
+    for kw in (dict(beta1=beta), dict(beta2=beta)):
+        assert dstd.dstd_adamw_step(_list(), dstd.make_adamw(**kw), LR, STEP, NORM, 0, WS, need,
+                                    None) == dstd.DSTD_ERR_PARAM
