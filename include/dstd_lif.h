@@ -586,8 +586,8 @@ dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, 
 
 /*
  * Clips the gradients to a norm of at most max_norm (> 0 or +INFINITY):
- * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c and the
- * products in fp32, rounded to bf16 where out is). A norm that is not finite
+ * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c to 24 bits
+ * down to 2^-252, the products in fp32, rounded to bf16 where out is). A norm that is not finite
  * clips nothing (c = 1).
  *  norm [1]   norm_given = 0: out, the norm before clipping, or NULL;
  *             norm_given = 1: in, the norm to clip by, for gradients that are

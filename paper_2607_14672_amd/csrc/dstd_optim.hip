@@ -246,15 +246,27 @@ __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
 
 // The norm and its clipping factor, in every thread of the block: from the
 // partials, or as given. A norm that is not finite clips nothing (factor 1).
+// The factor is c c2: max_norm / norm and 1, or where that is no normal fp32
+// number, 2^126 times it and 2^-126. So it keeps its 24 bits (down to 2^-252),
+// which gradients of 1e35 clipped to a norm of 1e-3 would lose to a factor of
+// 4e-41; x c cannot overflow, and the product with c2 is exact or the one
+// rounding of a subnormal result.
 struct NormFactor {
-    float norm, c;
+    float norm, c, c2;
     bool finite;
+    __device__ bool one() const { return c == 1.f && c2 == 1.f; }
 };
+__device__ __forceinline__ float scaled(float x, const NormFactor &f) { return x * f.c * f.c2; }
 __device__ NormFactor factor_of(double n, double max_norm) {
     NormFactor r;
     r.norm = static_cast<float>(n);
     r.finite = isfinite(r.norm);
     r.c = (r.finite && n > max_norm) ? static_cast<float>(max_norm / n) : 1.f;
+    r.c2 = 1.f;
+    if (__builtin_amdgcn_readfirstlane(r.c < 0x1p-126f)) {  // the same in every lane
+        r.c = static_cast<float>(max_norm / n * 0x1p126);
+        r.c2 = 0x1p-126f;
+    }
     return r;
 }
 template <int kThreads> __device__ NormFactor norm_factor(const OptNorm &nm, double *sh) {
@@ -285,17 +297,17 @@ __device__ __forceinline__ void clip_values(const TI *g, TO *out, const Span &p,
     for (int i = 0; i < kOptGroups; ++i)
         if (i * kOptThreads + tid < p.n4) x[i] = load4<NT>(g + p.lead + (i * kOptThreads + tid) * 4);
     const float x1 = p.one < p.count ? load1(g + p.one) : 0.f;
-    const float c = factor().c;
+    const NormFactor f = factor();
 #pragma unroll
     for (int i = 0; i < kOptGroups; ++i)
         if (i * kOptThreads + tid < p.n4)
-            store4<NT>(out + p.lead + (i * kOptThreads + tid) * 4, widen(x[i]) * c);
-    if (p.one < p.count) store1(out + p.one, x1 * c);
+            store4<NT>(out + p.lead + (i * kOptThreads + tid) * 4, widen(x[i]) * f.c * f.c2);
+    if (p.one < p.count) store1(out + p.one, scaled(x1, f));
 }
 
 template <bool NT, typename F>
 __device__ __forceinline__ void clip_chunk(const OptChunk &t, int tid, const F &factor) {
-    if (t.g == t.out && factor().c == 1.f) return;  // in place, nothing to clip
+    if (t.g == t.out && factor().one()) return;  // in place, nothing to clip
     const bool gb = t.types & kOptGradBf16, ob = t.types & kOptOutBf16;
     gu16 *gh = (gu16 *)t.g, *oh = (gu16 *)t.out;
     gf32 *gf = (gf32 *)t.g, *of = (gf32 *)t.out;
@@ -322,7 +334,7 @@ __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
     if (kInPlace) {
         const NormFactor f = factor();
         if (write_norm && threadIdx.x == 0) *nm.norm = f.norm;
-        if (f.c == 1.f) return;
+        if (f.one()) return;
         for (; k >= 0; k -= gridDim.x) clip_chunk<NT>(chunks[k], threadIdx.x, [&] { return f; });
         return;
     }
@@ -337,7 +349,8 @@ __global__ __launch_bounds__(kOptThreads) void grad_clip_kernel(
 // update is added to the widened weight and rounded once), 2 = bf16 weights
 // with an fp32 copy, which the update works on.
 struct StepConst {
-    float c, b1, b1_lo, b2, b2_lo, a1, a2, inv_c1, inv_c2, eps, lr, decay;
+    NormFactor f;
+    float b1, b1_lo, b2, b2_lo, a1, a2, inv_c1, inv_c2, eps, lr, decay;
 };
 // A moment settles where what it loses in a step is what it takes in, so beta
 // and 1 - beta have to add to 1: with beta rounded to fp32 (off by up to 2^-25)
@@ -345,7 +358,7 @@ struct StepConst {
 // 0.99999. So beta comes in two parts. The low one is above zero, for an
 // overflowed v (inf) has to stay one and not become inf - inf.
 __device__ __forceinline__ void adamw_one(const StepConst &q, float g, float &w, float &m, float &v) {
-    g *= q.c;
+    g = scaled(g, q.f);
     m = fmaf(q.b1, m, fmaf(q.a1, g, q.b1_lo * m));
     v = fmaf(q.b2, v, fmaf(q.a2 * g, g, q.b2_lo * v));
     const float u = (m * q.inv_c1) / (sqrtf(v * q.inv_c2) + q.eps);
@@ -394,7 +407,7 @@ __device__ __forceinline__ void adamw_values(const OptChunk &t, const Span &p, c
     const StepIn si = in();
     if (!si.f.finite) return;  // the step is skipped
     const float rate = a.lr ? *a.lr : a.hp.lr;
-    const StepConst q{si.f.c, a.hp.b1, a.hp.b1_lo, a.hp.b2, a.hp.b2_lo, a.hp.a1, a.hp.a2, si.at.inv_c1,
+    const StepConst q{si.f, a.hp.b1, a.hp.b1_lo, a.hp.b2, a.hp.b2_lo, a.hp.a1, a.hp.a2, si.at.inv_c1,
                       si.at.inv_c2, a.hp.eps, rate * t.lr_scale, a.hp.decay * t.decay_scale};
 #pragma unroll
     for (int i = 0; i < kVecs<kThreads>; ++i) {

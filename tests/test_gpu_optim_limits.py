@@ -130,3 +130,59 @@ def test_a_second_moment_that_overflowed_stays_infinite(dev, beta2, n):
     step = torch.full((1,), 3, dtype=torch.int64, device=dev)
     dstd.adamw_step(tl, dstd.make_adamw(lr=0.5, beta2=beta2, weight_decay=0.5), step)
     assert bool((v == math.inf).all()) and bool((w == 0.75).all())
+
+
+# ---------------------------------------------------------- extreme factors --
+# of chunks for one launch of one block, and for many
+@pytest.mark.parametrize("sizes", [[5000, 3], [60_001, 7]])
+@pytest.mark.parametrize("g_type,o_type", [("f32", None), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-6, 1e-12])
+def test_clip_of_huge_gradients_keeps_its_bits(dev, max_norm, g_type, o_type, sizes):
+    """max_norm / norm lies below the normal range of fp32 here, or below all of
+    it; the results do not. Bounds as for other factors, and half of the least
+    fp32 or bf16 number for results that go there."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    vals = _normal(np.random.default_rng(21), sizes, 1e35)
+    g = Arena(vals, g_type, 1, dev)
+    o = Arena([0 * v for v in vals], o_type, 2, dev) if o_type else None
+    before = g.get()
+    ref = _norm64(before)
+    assert ref < 3e38 and max_norm / ref < 2.0 ** -126
+    norm = dstd.grad_clip(dstd.make_tensor_list(g.t, out=o.t if o else None), max_norm)
+    torch.cuda.synchronize()
+    _close(norm.cpu().numpy(), [ref], [U * MORE * ref], "norm")
+    c = max_norm / ref
+    half, least = (U16, 2.0 ** -133) if o_type == "bf16" else (0.0, 2.0 ** -149)
+    for x, b in zip((o or g).get(), before):
+        _close(x, b * c, np.abs(b * c) * MORE * (2 * U + half) + least, "clipped")
+    assert g.gaps_kept() and (o is None or o.gaps_kept())
+
+
+@pytest.mark.parametrize("sizes", [[5000, 3], [60_001, 7]])
+@pytest.mark.parametrize("g_type", ["f32", "bf16"])
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-6])
+def test_adamw_of_huge_gradients(dev, max_norm, g_type, sizes):
+    import torch
+    from paper_2607_14672_amd import dstd
+    tr = Train(dev, sizes, g_type, seed=22, g_scale=1e35)
+    before = tr.g.get(), tr.w.get(), tr.m.get(), tr.v.get()
+    ref = _norm64(before[0])
+    step = torch.full((1,), 9, dtype=torch.int64, device=dev)
+    norm = dstd.adamw_step(tr.tl, dstd.make_adamw(lr=2e-3, max_norm=max_norm, **HP), step)
+    torch.cuda.synchronize()
+    _close(norm.cpu().numpy(), [ref], [U * MORE * ref], "norm")
+    _check_step(tr, before, 10, HP, max_norm / ref, 2e-3)
+
+
+@pytest.mark.parametrize("n", [5000, 60_001])
+@pytest.mark.parametrize("outside", [False, True])
+def test_a_tiny_factor_whose_mantissa_rounds_to_one_still_clips(dev, outside, n):
+    import torch
+    from paper_2607_14672_amd import dstd
+    g = torch.full((n,), 2.0 ** 100, device=dev)
+    out = [torch.zeros(n, device=dev)] if outside else None
+    norm = torch.full((1,), 2.0 ** 120, device=dev)
+    dstd.grad_clip(dstd.make_tensor_list([g], out=out), 2.0 ** -10 * (1 - 2.0 ** -30), norm=norm,
+                   norm_given=True)
+    assert bool(((out[0] if outside else g) == 2.0 ** -30).all())
