@@ -578,8 +578,8 @@ size_t dstd_tensor_list_workspace_size(const dstd_tensor_list *list);
 /*
  * norm [1] out: the L2 norm of all gradients of the list together, the sum of
  * squares in 64 bits (no overflow or underflow for any fp32 gradients), the
- * norm rounded to fp32. 0 for an empty list; NaN or inf as the gradients have
- * them.
+ * norm rounded to fp32 (inf where it is larger than that). 0 for an empty list;
+ * NaN or inf as the gradients have them.
  */
 dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, size_t ws_bytes,
                            void *stream);
@@ -588,7 +588,8 @@ dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, 
  * Clips the gradients to a norm of at most max_norm (> 0 or +INFINITY):
  * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c to 24 bits
  * down to 2^-252, the products in fp32, rounded to bf16 where out is). A norm that is not finite
- * clips nothing (c = 1).
+ * clips nothing (c = 1). Finite gradients whose norm leaves fp32 (*norm reads
+ * inf) are clipped by its 64-bit value, unless max_norm leaves fp32 too.
  *  norm [1]   norm_given = 0: out, the norm before clipping, or NULL;
  *             norm_given = 1: in, the norm to clip by, for gradients that are
  *             spread over several lists or ranks (their squared norms added);
@@ -619,8 +620,11 @@ typedef struct {
  *  step [1]   in/out, on the device: steps done (>= 0); every list has its own.
  *  norm [1]   as in dstd_grad_clip. The norm is summed if norm is not NULL or
  *             max_norm is finite; a step whose norm is then not finite leaves
- *             w, w32, m, v and step as they were. With norm = NULL and
- *             max_norm = +INFINITY no norm is formed and every step is made.
+ *             w, w32, m, v and step as they were. A norm of finite gradients
+ *             that leaves fp32 counts as not finite only if max_norm leaves it
+ *             too; otherwise the gradients are clipped and the step is made.
+ *             With norm = NULL and max_norm = +INFINITY no norm is formed and
+ *             every step is made.
  */
 dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_params *p,
                             const float *lr, int64_t *step, float *norm, int32_t norm_given,

@@ -20,6 +20,8 @@
 // launch that follows adds the partials again in every block, in a fixed
 // order, while the block's chunk is on its way. A launch of its own for that
 // gains nothing (201 M weights: 1075 us with it, 1065 without, at that step).
+#include <float.h>
+
 #include "dstd_internal.h"
 #include "dstd_kernels.h"
 #include "dstd_profile.h"
@@ -246,6 +248,8 @@ __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
 
 // The norm and its clipping factor, in every thread of the block: from the
 // partials, or as given. A norm that is not finite clips nothing (factor 1).
+// The norm of finite gradients is finite in 64 bits; where it leaves fp32 it
+// counts as finite if max_norm is a bound in fp32, which it is then clipped to.
 // The factor is c c2: max_norm / norm and 1, or where that is no normal fp32
 // number, 2^126 times it and 2^-126. So it keeps its 24 bits (down to 2^-252),
 // which gradients of 1e35 clipped to a norm of 1e-3 would lose to a factor of
@@ -261,9 +265,12 @@ __device__ NormFactor factor_of(double n, double max_norm) {
     NormFactor r;
     r.norm = static_cast<float>(n);
     r.finite = isfinite(r.norm);
+    // what is rare goes by branches that are the same in every lane
+    if (__builtin_amdgcn_readfirstlane(!r.finite))
+        r.finite = isfinite(n) && max_norm <= FLT_MAX;
     r.c = (r.finite && n > max_norm) ? static_cast<float>(max_norm / n) : 1.f;
     r.c2 = 1.f;
-    if (__builtin_amdgcn_readfirstlane(r.c < 0x1p-126f)) {  // the same in every lane
+    if (__builtin_amdgcn_readfirstlane(r.c < 0x1p-126f)) {
         r.c = static_cast<float>(max_norm / n * 0x1p126);
         r.c2 = 0x1p-126f;
     }

@@ -886,7 +886,8 @@ def adamw_step(tl: TensorList, hp: dstd_adamw_params, step, lr=None, norm=None,
     hp.max_norm on the way. `step` [1] int64: steps done, on the device, counted
     up (one for each list); `lr` [1] f32 on the device replaces hp.lr. Returns the norm before
     clipping (None where none is formed: no `norm` given and hp.max_norm infinite);
-    a step whose norm is not finite changes nothing."""
+    a step whose norm is not finite changes nothing. (Finite gradients whose norm
+    leaves fp32 are clipped and the step is made, though the norm reads inf.)"""
     norm, ptr, ws = _optim_args(tl, norm, norm_given, ws, math.isfinite(hp.max_norm))
     torch = _torch()
     _launch(tl, "dstd_adamw_step", dstd_adamw_step, tl.c, hp,

@@ -186,3 +186,44 @@ def test_a_tiny_factor_whose_mantissa_rounds_to_one_still_clips(dev, outside, n)
     dstd.grad_clip(dstd.make_tensor_list([g], out=out), 2.0 ** -10 * (1 - 2.0 ** -30), norm=norm,
                    norm_given=True)
     assert bool(((out[0] if outside else g) == 2.0 ** -30).all())
+
+
+@pytest.mark.parametrize("sizes", [[5000, 3], [60_001, 7]])
+@pytest.mark.parametrize("o_type", [None, "f32"])
+def test_clip_of_finite_gradients_whose_norm_leaves_fp32(dev, o_type, sizes):
+    import torch
+    from paper_2607_14672_amd import dstd
+    with np.errstate(over="ignore"):
+        vals = [np.clip(v, -3.3e38, 3.3e38) for v in _normal(np.random.default_rng(23), sizes, 1.5e38)]
+    g = Arena(vals, "f32", 1, dev)
+    o = Arena([0 * v for v in vals], o_type, 2, dev) if o_type else None
+    before = g.get()
+    ref = _norm64(before)
+    assert ref > 1e39
+    tl = dstd.make_tensor_list(g.t, out=o.t if o else None)
+    assert dstd.grad_clip(tl, 0.5).item() == math.inf
+    for x, b in zip((o or g).get(), before):
+        _close(x, b * (0.5 / ref), np.abs(b) * (0.5 / ref) * MORE * 2 * U, "clipped")
+    assert g.gaps_kept() and (o is None or o.gaps_kept())
+
+
+@pytest.mark.parametrize("sizes", [[5000, 3], [60_001, 7]])
+def test_adamw_of_finite_gradients_whose_norm_leaves_fp32(dev, sizes):
+    """Clipped, the step is made; without a bound in fp32 it is skipped."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    tr = Train(dev, sizes, seed=24, g_scale=3e37)
+    for a, n in tr.g.slots:  # a norm beyond fp32 in the short list, too
+        tr.g.buf[a:a + 2] = 3e38
+    before = tr.g.get(), tr.w.get(), tr.m.get(), tr.v.get()
+    ref = _norm64(before[0])
+    assert ref > 3.5e38
+    kept, step = tr.bits(), torch.full((1,), 9, dtype=torch.int64, device=dev)
+    for max_norm in (math.inf, 1e300):  # asked for by the norm; with a bound that is none
+        norm = dstd.adamw_step(tr.tl, dstd.make_adamw(max_norm=max_norm), step,
+                               norm=torch.zeros(1, device=dev))
+        assert norm.item() == math.inf and step.item() == 9
+        assert all(torch.equal(a, b) for a, b in zip(tr.bits(), kept))
+    norm = dstd.adamw_step(tr.tl, dstd.make_adamw(lr=2e-3, max_norm=0.5, **HP), step)
+    assert norm.item() == math.inf and step.item() == 10
+    _check_step(tr, before, 10, HP, 0.5 / ref, 2e-3)
