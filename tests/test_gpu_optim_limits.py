@@ -227,3 +227,130 @@ def test_adamw_of_finite_gradients_whose_norm_leaves_fp32(dev, sizes):
     norm = dstd.adamw_step(tr.tl, dstd.make_adamw(lr=2e-3, max_norm=0.5, **HP), step)
     assert norm.item() == math.inf and step.item() == 10
     _check_step(tr, before, 10, HP, 0.5 / ref, 2e-3)
+
+
+# ------------------------------------------------- both forms of each launch --
+# 4 chunks, 124 and 2199: one launch of one block for a clip, one block per
+# chunk, and more chunks than a list that is clipped in place has blocks. A step
+# takes one block for at most 3: the first list without its last tensor.
+FORMS = {"block": [9000, 5], "blocks": [500_001, 7], "strided": [9_000_001, 20]}
+
+
+def _places(sizes):
+    """The first element, one in the middle, the last (of the last tensor)."""
+    return [(0, 0), (0, sizes[0] // 2), (len(sizes) - 1, sizes[-1] - 1)]
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_norm_of_what_is_not_finite_in_every_form(dev, form, dtype, value):
+    from paper_2607_14672_amd import dstd
+    sizes = FORMS[form]
+    for k, i in _places(sizes):
+        g = Arena([np.ones(n, dtype=np.float32) for n in sizes], dtype, 1, dev)
+        g.t[k][i] = value
+        got = dstd.grad_norm(dstd.make_tensor_list(g.t)).item()
+        assert math.isnan(got) if math.isnan(value) else got == math.inf, (k, i, got)
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+@pytest.mark.parametrize("outs", ["in place", "outside", "mixed"])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_clip_with_a_norm_that_is_not_finite_in_every_form(dev, form, outs, value):
+    """In place nothing changes; elsewhere the gradients are copied, bit for bit.
+    Measured by the call itself, and given."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    sizes = FORMS[form]
+    vals = _normal(np.random.default_rng(31), sizes)
+    for k, i in _places(sizes):
+        for given in (False, True):
+            g, o = Arena(vals, "f32", 1, dev), Arena([0 * v for v in vals], "f32", 3, dev)
+            if not given:
+                g.t[k][i] = value
+            kept = g.buf.clone()
+            out = {"in place": None, "outside": o.t, "mixed": [None] + o.t[1:]}[outs]
+            norm = torch.tensor([value], device=dev) if given else None
+            got = dstd.grad_clip(dstd.make_tensor_list(g.t, out=out), 1e-3, norm=norm, norm_given=given)
+            assert not math.isfinite(got.item())
+            assert torch.equal(g.buf.view(torch.int32), kept.view(torch.int32))
+            for a, b, into in zip(o.t, g.t, out or [None] * len(sizes)):
+                if into is None:
+                    assert not bool(a.any())
+                else:
+                    assert torch.equal(a.view(torch.int32), b.view(torch.int32))
+            assert o.gaps_kept()
+
+
+@pytest.mark.parametrize("outs", ["in place", "outside", "mixed"])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_clip_by_a_given_norm_in_every_form(dev, form, outs):
+    """Clipped, and with nothing to clip, where the gradients stay or are copied."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    sizes = FORMS[form]
+    vals = _normal(np.random.default_rng(32), sizes)
+    for given, max_norm in ((8.0, 2.0), (8.0, 8.0), (0.0, 1.0)):
+        g, o = Arena(vals, "f32", 2, dev), Arena([0 * v for v in vals], "f32", 0, dev)
+        out = {"in place": None, "outside": o.t, "mixed": [None] + o.t[1:]}[outs]
+        norm = torch.tensor([given], device=dev)
+        dstd.grad_clip(dstd.make_tensor_list(g.t, out=out), max_norm, norm=norm, norm_given=True)
+        assert norm.item() == given
+        c = 0.25 if max_norm < given else 1.0  # a power of two: exact
+        for a, b, v, into in zip(o.get(), g.get(), vals, out or [None] * len(sizes)):
+            want = v.astype(np.float64)
+            assert np.array_equal(b, want * (c if into is None else 1.0))
+            assert np.array_equal(a, want * c) if into is not None else not a.any()
+        assert g.gaps_kept() and o.gaps_kept()
+
+
+STEP_FORMS = {"block": [9000], "blocks": [500_001, 7], "far": [9_000_001, 20]}
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("g_type,w_type,master", [("f32", "f32", False), ("bf16", "bf16", True),
+                                                  ("f32", "bf16", False)])
+@pytest.mark.parametrize("form", sorted(STEP_FORMS))
+def test_a_skipped_step_changes_nothing_in_every_form(dev, form, g_type, w_type, master, value):
+    """A norm that is not finite: asked for by max_norm, by a place for it alone,
+    and given. Weights, copies, moments, gaps and step number keep their bits."""
+    import torch
+    from paper_2607_14672_amd import dstd
+    sizes = STEP_FORMS[form]
+    tr = Train(dev, sizes, g_type, w_type, master, shift=1, seed=33)
+    step = torch.full((1,), 3, dtype=torch.int64, device=dev)
+    for k, i in _places(sizes):
+        old = tr.g.t[k][i].clone()
+        tr.g.t[k][i] = value
+        kept = tr.bits()
+        calls = [(1.0, None, False), (math.inf, torch.zeros(1, device=dev), False),
+                 (1.0, torch.tensor([value], device=dev), True),
+                 (math.inf, torch.tensor([value], device=dev), True)]
+        for max_norm, norm, given in calls:
+            norm = dstd.adamw_step(tr.tl, dstd.make_adamw(max_norm=max_norm), step, norm=norm,
+                                   norm_given=given)
+            got = norm.item()
+            assert math.isnan(got) if math.isnan(value) else abs(got) == math.inf
+            assert step.item() == 3
+            for a, b in zip(tr.bits(), kept):
+                bits = torch.int16 if a.dtype == torch.bfloat16 else torch.int32
+                assert torch.equal(a.view(bits), b.view(bits))
+        tr.g.t[k][i] = old
+    # no norm asked for: the step is made
+    assert dstd.adamw_step(tr.tl, dstd.make_adamw(), step) is None and step.item() == 4
+    assert all(a.gaps_kept() for a in tr.arenas)
+
+
+@pytest.mark.parametrize("form", sorted(STEP_FORMS))
+def test_adamw_by_a_given_norm_in_every_form(dev, form):
+    import torch
+    from paper_2607_14672_amd import dstd
+    tr = Train(dev, STEP_FORMS[form], seed=34)
+    before = tr.g.get(), tr.w.get(), tr.m.get(), tr.v.get()
+    norm = torch.tensor([8.0], device=dev)
+    step = torch.full((1,), 6, dtype=torch.int64, device=dev)
+    dstd.adamw_step(tr.tl, dstd.make_adamw(lr=1e-3, max_norm=2.0, **HP), step, norm=norm, norm_given=True)
+    torch.cuda.synchronize()
+    assert norm.item() == 8.0 and step.item() == 7
+    _check_step(tr, before, 7, HP, 0.25, 1e-3)
