@@ -412,6 +412,26 @@ def workspace(nbytes: int, device):
     return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
 
 
+def _grad_dest(torch, grad_W, W, shape, dev, need_W):
+    """Where a backward writes dL/dW (f32): `grad_W`, checked, a new tensor, or
+    None where it is not wanted."""
+    if grad_W is None:
+        return torch.empty(shape, dtype=torch.float32, device=dev) if need_W else None
+    if not need_W:
+        raise ValueError("grad_W is given, but need_W is False")
+    if not isinstance(grad_W, torch.Tensor) or grad_W.dtype != torch.float32:
+        raise TypeError("grad_W must be a float32 tensor")
+    if grad_W.device != dev:
+        raise ValueError(f"grad_W must be on {dev}")
+    if grad_W.shape != torch.Size(shape):
+        raise ValueError(f"grad_W has shape {tuple(grad_W.shape)}, not {tuple(shape)}")
+    if not grad_W.is_contiguous():
+        raise ValueError("grad_W must be contiguous")
+    if grad_W.data_ptr() == W.data_ptr() and W.numel() > 0:
+        raise ValueError("grad_W and W are the same memory")
+    return grad_W
+
+
 def forward(p: dstd_lif_params, t_in, W, ws=None):
     """Dense layer forward. t_in [B, N_in] f32, W [N_out, N_in] f32|bf16 (CUDA tensors)."""
     torch = _torch()
@@ -455,17 +475,19 @@ def forward_noalloc(p: dstd_lif_params, t_in, W, outputs=None):
 
 
 def backward(p: dstd_lif_params, t_in, W, t_out, slope, q, grad_t_out, need_W=True,
-             need_t_in=True, ws=None, synfire: Optional[dstd_synfire_params] = None):
+             need_t_in=True, ws=None, synfire: Optional[dstd_synfire_params] = None, grad_W=None):
     """Dense layer backward; returns (grad_W or None, grad_t_in or None). With
     `synfire`, the layer's temporal-penalty and dead-neuron gradients are
-    included."""
+    included. dL/dW is written to `grad_W` if given (f32, as all four
+    backward helpers take it), else to a new tensor at each call: a tensor list
+    needs the former."""
     torch = _torch()
     t_in = _cont(t_in, torch.float32)
     W = _cont(W)
     B, N_in = t_in.shape
     N_out = W.shape[0]
     dev = t_in.device
-    gW = torch.empty((N_out, N_in), dtype=torch.float32, device=dev) if need_W else None
+    gW = _grad_dest(torch, grad_W, W, (N_out, N_in), dev, need_W)
     gt = torch.empty((B, N_in), dtype=torch.float32, device=dev) if need_t_in else None
     need = dstd_lif_backward_workspace_size(p, B, N_in, N_out)
     if ws is None or ws.numel() < need:
@@ -506,7 +528,7 @@ def multispike_forward(p: dstd_lif_params, t_in, W, F_out: int, ws=None):
 
 
 def multispike_backward(p: dstd_lif_params, t_in, W, t_out, slope, q, cur, grad_t_out,
-                        need_W=True, need_t_in=True, ws=None):
+                        need_W=True, need_t_in=True, ws=None, grad_W=None):
     """Multi-spike dense backward; returns (grad_W or None, grad_t_in [B, N_in, F_in] or None)."""
     torch = _torch()
     t_in = _cont(t_in, torch.float32)
@@ -515,7 +537,7 @@ def multispike_backward(p: dstd_lif_params, t_in, W, t_out, slope, q, cur, grad_
     N_out = W.shape[0]
     F_out = t_out.shape[2]
     dev = t_in.device
-    gW = torch.empty((N_out, N_in), dtype=torch.float32, device=dev) if need_W else None
+    gW = _grad_dest(torch, grad_W, W, (N_out, N_in), dev, need_W)
     gt = torch.empty((B, N_in, F_in), dtype=torch.float32, device=dev) if need_t_in else None
     need = dstd_lif_multispike_backward_workspace_size(p, B, N_in, F_in, N_out, F_out)
     if ws is None or ws.numel() < need:
@@ -590,7 +612,7 @@ def exact_forward(p: dstd_lif_params, t_in, W, ws=None):
 
 
 def exact_backward(p: dstd_lif_params, t_in, W, t_out, slope, k, grad_t_out, need_W=True,
-                   need_t_in=True, ws=None):
+                   need_t_in=True, ws=None, grad_W=None):
     """Exact backward of a dense layer; returns (grad_W or None, grad_t_in or None)."""
     torch = _torch()
     t_in = _cont(t_in, torch.float32)
@@ -598,7 +620,7 @@ def exact_backward(p: dstd_lif_params, t_in, W, t_out, slope, k, grad_t_out, nee
     B, N_in = t_in.shape
     N_out = W.shape[0]
     dev = t_in.device
-    gW = torch.empty((N_out, N_in), dtype=torch.float32, device=dev) if need_W else None
+    gW = _grad_dest(torch, grad_W, W, (N_out, N_in), dev, need_W)
     gt = torch.empty((B, N_in), dtype=torch.float32, device=dev) if need_t_in else None
     need = dstd_exact_backward_workspace_size(p, B, N_in, N_out)
     if ws is None or ws.numel() < need:
@@ -632,13 +654,15 @@ def conv_forward(p: dstd_lif_params, cs: dstd_conv_shape, t_in, W, ws=None):
 
 
 def conv_backward(p, cs, t_in, W, t_out, slope, q, grad_t_out, need_W=True, need_t_in=True,
-                  ws=None, synfire: Optional[dstd_synfire_params] = None):
+                  ws=None, synfire: Optional[dstd_synfire_params] = None, grad_W=None):
+    """Conv layer backward; returns (grad_W or None, grad_t_in or None), as
+    `backward`."""
     torch = _torch()
     t_in = _cont(t_in, torch.float32)
     W = _cont(W)
     B = t_in.shape[0]
     dev = t_in.device
-    gW = torch.empty(W.shape, dtype=torch.float32, device=dev) if need_W else None
+    gW = _grad_dest(torch, grad_W, W, W.shape, dev, need_W)
     gt = torch.empty(t_in.shape, dtype=torch.float32, device=dev) if need_t_in else None
     need = dstd_lif_conv_backward_workspace_size(p, cs, B)
     if ws is None or ws.numel() < need:
@@ -750,7 +774,8 @@ def _per_tensor(x, n, what):
 def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None, lr_scale=None,
                      decay_scale=None) -> TensorList:
     """List of tensors for grad_norm, grad_clip and adamw_step. `grads` f32 or
-    bf16; `weights` f32 or bf16 with their moments `m`, `v` (f32), and for bf16
+    bf16 (the tensors that every backward writes: `grad_W` of the backward
+    helpers); `weights` f32 or bf16 with their moments `m`, `v` (f32), and for bf16
     weights optionally their f32 copies `master`; `out` the tensors grad_clip
     writes (default: the gradients themselves); `lr_scale`, `decay_scale`
     factors per tensor (default 1). All contiguous, on one GPU; entries of

@@ -72,3 +72,23 @@ def test_betas_that_are_one_in_fp32_are_refused(beta):
     for kw in (dict(beta1=beta), dict(beta2=beta)):
         assert dstd.dstd_adamw_step(_list(), dstd.make_adamw(**kw), LR, STEP, NORM, 0, WS, need,
                                     None) == dstd.DSTD_ERR_PARAM
+
+
+def test_gradient_places_are_checked():
+    """The backward helpers' `grad_W`."""
+    import torch
+    W, cpu = torch.ones(4, 6), torch.device("cpu")
+
+    def dest(g, need=True):
+        return dstd._grad_dest(torch, g, W, (4, 6), cpu, need)
+
+    g = torch.zeros(4, 6)
+    assert dest(g) is g and dest(None, False) is None
+    assert dest(None).shape == (4, 6) and dest(None).dtype == torch.float32
+    for bad, err in ((g.double(), TypeError), (0.0, TypeError), (g.t(), ValueError),
+                     (torch.zeros(6, 4).t(), ValueError), (torch.zeros(24), ValueError),
+                     (g.to("meta"), ValueError), (W, ValueError)):
+        with pytest.raises(err, match="grad_W"):
+            dest(bad)
+    with pytest.raises(ValueError, match="need_W"):
+        dest(g, False)
