@@ -749,6 +749,11 @@ class TensorList:
         self.ws_bytes = dstd_tensor_list_workspace_size(c)
 
 
+def _tensor(x, what):
+    if not isinstance(x, _torch().Tensor):
+        raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
+
+
 def _list_array(torch, x, like, dev, dtypes, what, k):
     """Address of one array of tensor k of a list, checked."""
     if not isinstance(x, torch.Tensor):
@@ -823,6 +828,7 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
 
 
 def _scalar(x, dtype, dev, what):
+    _tensor(x, what)
     if x.dtype != dtype or x.numel() != 1 or x.device != dev:
         raise ValueError(f"{what} must hold one {dtype} on {dev}")
     return x.data_ptr()
@@ -836,6 +842,8 @@ def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
         if want_norm:
             torch = _torch()
             norm = torch.empty(1, dtype=torch.float32, device=tl.device)
+    if ws is not None:
+        _tensor(ws, "ws")
     if ws is None or ws.numel() < tl.ws_bytes:
         ws = workspace(tl.ws_bytes, tl.device)
     elif ws.device != tl.device:

@@ -92,3 +92,21 @@ def test_gradient_places_are_checked():
             dest(bad)
     with pytest.raises(ValueError, match="need_W"):
         dest(g, False)
+
+
+def test_scalars_that_are_no_tensors_are_refused():
+    """A number in place of the tensor that holds it, in every place for one."""
+    import torch
+    tl = dstd.TensorList(_list(), None, (), torch.device("cpu"), 0)
+    hp, step = dstd.make_adamw(max_norm=1.0), torch.zeros(1, dtype=torch.int64)
+    norm, ws = torch.zeros(1), torch.empty(tl.ws_bytes, dtype=torch.uint8)
+    for kw in (dict(lr=1e-3), dict(lr=torch.zeros(1, dtype=torch.float64).numpy()), dict(norm=2.0),
+               dict(norm=2.0, norm_given=True), dict(step=3), dict(ws=bytearray(tl.ws_bytes))):
+        args = dict(step=step, norm=norm, ws=ws)
+        args.update(kw)
+        with pytest.raises(TypeError, match=f"{next(iter(kw))} must be a tensor"):
+            dstd.adamw_step(tl, hp, **args)
+    with pytest.raises(TypeError, match="norm must be a tensor"):
+        dstd.grad_norm(tl, norm=2.0, ws=ws)
+    with pytest.raises(TypeError, match="norm must be a tensor"):
+        dstd.grad_clip(tl, 1.0, norm=2.0, norm_given=True, ws=ws)
