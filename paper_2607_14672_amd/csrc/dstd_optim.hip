@@ -18,8 +18,13 @@
 // sizes. The norm needs every gradient before the first is scaled: one launch
 // sums the squares of a fixed set of chunks per block (partials), and the
 // launch that follows adds the partials again in every block, in a fixed
-// order, while the block's chunk is on its way. A launch of its own for that
-// gains nothing (201 M weights: 1075 us with it, 1065 without, at that step).
+// order. A thread's first partial is read while the block's chunk is on its
+// way; the others (four a thread at most in a clip, two in a step), the step's
+// constants and the learning rate are read one after the other behind it, which
+// is what launches of a few us wait for (grad_norm_kernel, which does nothing
+// else: 1.7 us for 106 partials, 4.4 for 1024). A launch of its own for the
+// partials gains nothing (201 M weights: 1075 us with it, 1065 without, at that
+// step).
 #include <float.h>
 
 #include "dstd_internal.h"
@@ -225,8 +230,9 @@ __device__ OptStep step_at(const int64_t *step, double beta1, double beta2) {
 // 1 / (1 - beta^t): the update writes the number, so its other blocks must
 // not read it.
 __global__ __launch_bounds__(kOptThreads) void grad_squares_kernel(
-    const OptChunk *__restrict__ chunks, int n_chunks, int n_stream, uint32_t types, double *__restrict__ part, const int64_t *step, double beta1,
-    double beta2, OptStep *__restrict__ at) {
+    const OptChunk *__restrict__ chunks, int n_chunks, int n_stream, uint32_t types,
+    double *__restrict__ part, const int64_t *step, double beta1, double beta2,
+    OptStep *__restrict__ at) {
     __shared__ double sh[kOptThreads / kWave];
     double s = 0.0;
     const int b = blockIdx.x, by = gridDim.x, tid = threadIdx.x;
@@ -560,8 +566,10 @@ hipError_t launch_squares(const OptList &L, const OptNorm &nm, bool scaled, cons
                           double beta1, double beta2, OptStep *at, hipStream_t st) {
     const bool sums = nm.n_part >= 0;
     int n_stream = 0;
-    if (L.g_bytes > kOptCached)
-        n_stream = L.n_chunks - (scaled ? static_cast<int>(static_cast<double>(L.n_chunks) * kOptCached / L.g_bytes) : 0);
+    if (L.g_bytes > kOptCached) {
+        const double kept = static_cast<double>(L.n_chunks) * kOptCached / L.g_bytes;
+        n_stream = L.n_chunks - (scaled ? static_cast<int>(kept) : 0);
+    }
     ProfScope prof(sums ? "grad_squares" : "adamw_count", st);
     hipLaunchKernelGGL(grad_squares_kernel, dim3(sums ? nm.n_part : 1), dim3(kOptThreads), 0, st,
                        L.chunks, sums ? L.n_chunks : 0, n_stream, sums ? L.g_types : 0u, nm.part,
