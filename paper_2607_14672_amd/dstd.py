@@ -828,8 +828,8 @@ def make_tensor_list(grads, weights=None, m=None, v=None, master=None, out=None,
 
 
 def _scalar(x, dtype, dev, what):
-    _tensor(x, what)
-    if x.dtype != dtype or x.numel() != 1 or x.device != dev:
+    if getattr(x, "dtype", None) != dtype or x.numel() != 1 or x.device != dev:
+        _tensor(x, what)
         raise ValueError(f"{what} must hold one {dtype} on {dev}")
     return x.data_ptr()
 
@@ -842,9 +842,9 @@ def _optim_args(tl: TensorList, norm, norm_given, ws, want_norm):
         if want_norm:
             torch = _torch()
             norm = torch.empty(1, dtype=torch.float32, device=tl.device)
-    if ws is not None:
-        _tensor(ws, "ws")
-    if ws is None or ws.numel() < tl.ws_bytes:
+    if ws is None or getattr(ws, "numel", int)() < tl.ws_bytes:
+        if ws is not None:
+            _tensor(ws, "ws")
         ws = workspace(tl.ws_bytes, tl.device)
     elif ws.device != tl.device:
         raise ValueError(f"ws must be on {tl.device}")
