@@ -587,9 +587,10 @@ dstd_status dstd_grad_norm(const dstd_tensor_list *list, float *norm, void *ws, 
 /*
  * Clips the gradients to a norm of at most max_norm (> 0 or +INFINITY):
  * out = c g with c = max_norm / norm where norm > max_norm, else 1 (c to 24 bits
- * down to 2^-252, the products in fp32, rounded to bf16 where out is). A norm that is not finite
- * clips nothing (c = 1). Finite gradients whose norm leaves fp32 (*norm reads
- * inf) are clipped by its 64-bit value, unless max_norm leaves fp32 too.
+ * down to 2^-252, the products in fp32, rounded to bf16 where out is). A norm
+ * that is not finite clips nothing (c = 1). Finite gradients whose norm leaves
+ * fp32 (*norm reads inf) are clipped by its 64-bit value, unless max_norm leaves
+ * fp32 too.
  *  norm [1]   norm_given = 0: out, the norm before clipping, or NULL;
  *             norm_given = 1: in, the norm to clip by, for gradients that are
  *             spread over several lists or ranks (their squared norms added);

@@ -427,8 +427,9 @@ def _grad_dest(torch, grad_W, W, shape, dev, need_W):
         raise ValueError(f"grad_W has shape {tuple(grad_W.shape)}, not {tuple(shape)}")
     if not grad_W.is_contiguous():
         raise ValueError("grad_W must be contiguous")
-    if grad_W.data_ptr() == W.data_ptr() and W.numel() > 0:
-        raise ValueError("grad_W and W are the same memory")
+    a, b = grad_W.data_ptr(), W.data_ptr()
+    if a < b + W.numel() * W.element_size() and b < a + grad_W.numel() * 4:
+        raise ValueError("grad_W and W share the same memory")
     return grad_W
 
 
@@ -741,7 +742,9 @@ class TensorList:
     The table is written on the stream that is current when the list is built
     (``stream``; ``built``: the event behind it). Calls on another stream wait
     for it. A list built inside a capture (``captured``) has its table once the
-    graph is replayed, and is for calls inside captures alone."""
+    graph is replayed, and is for calls inside captures alone, whose graphs are
+    replayed behind that one; streams that a capture forks are ordered by
+    whoever forks them."""
 
     def __init__(self, c, mem, tensors, device, stream, built=None, captured=False):
         self.c, self.mem, self.tensors, self.device, self.stream = c, mem, tensors, device, stream

@@ -92,6 +92,13 @@ def test_gradient_places_are_checked():
             dest(bad)
     with pytest.raises(ValueError, match="need_W"):
         dest(g, False)
+    # a part of the weights' memory, in whichever order
+    buf = torch.zeros(100)
+    lo, hi, off = buf[:24].view(4, 6), buf[23:47].view(4, 6), buf[24:48].view(4, 6)
+    for w, place in ((lo, hi), (hi, lo)):
+        with pytest.raises(ValueError, match="share"):
+            dstd._grad_dest(torch, place, w, (4, 6), cpu, True)
+    assert dstd._grad_dest(torch, off, lo, (4, 6), cpu, True) is off
 
 
 def test_scalars_that_are_no_tensors_are_refused():
