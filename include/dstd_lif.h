@@ -281,6 +281,96 @@ dstd_status dstd_softmax_ce_grad(int64_t B, int64_t N, const float *t_out, const
 dstd_status dstd_mse_grad(int64_t B, int64_t N, const float *t_out, const float *target,
                           float *grad_t, float *loss, void *stream);
 
+/* --------------------------------------------------------------- answers -- */
+
+/*
+ * Scores whose softmax is a network's answer: x, B rows of N, `ld` elements
+ * apart, fp32 or bf16 (dtype); the logits are z = scale x. A network's output
+ * spike times have scale = -1 / tau_soft (App. C.1), the scores of another
+ * network 1 / temperature.
+ *  cap   what an entry that is not finite (a neuron that did not fire, a class
+ *        that is masked) counts as, as t_cap above; a cap that is not finite
+ *        leaves such entries out.
+ * 1 <= N < 2^24, 0 <= B <= 65535, ld >= N; scale finite and not 0 in fp32. No
+ * output or workspace of a call may overlap another or an input
+ * (DSTD_ERR_PARAM).
+ */
+typedef struct {
+    const void *x;
+    int64_t B, N, ld;
+    int32_t dtype;
+    float cap;
+    double scale;
+} dstd_scores;
+
+#define DSTD_MAX_TOP 256
+
+/*
+ * The K largest logits of every row, falling, equal scores by index, and the
+ * rest of the softmax: what is kept of a teacher for dstd_distill_grad.
+ *  idx   [B][K] out: their classes; -1 where a row has fewer entries.
+ *  logit [B][K] out: their logits, rounded to fp32; -inf there.
+ *  rest  [B]    out: ln of the sum of e^z over all others, -inf without any; or
+ *               NULL to skip.
+ * 1 <= K <= min(N, DSTD_MAX_TOP). Rows are ordered by their scores, exactly.
+ */
+size_t dstd_top_logits_workspace_size(const dstd_scores *s, int64_t K);
+dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float *logit,
+                            float *rest, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Distillation from a teacher's top logits: the Kullback-Leibler divergence of
+ * the softmax of a student's output spike times (logits -t/tau_soft, neurons
+ * that did not fire at t_cap and without gradient, as in dstd_softmax_ce_grad)
+ * from what the teacher says of the classes it names, S:
+ *   p = softmax(logit[0 .. K), rest), q_k the student's probability of class k,
+ *   L_b = weight [ sum_k p_k (ln p_k - ln q_k) + p_rest (ln p_rest - ln q_rest) ]
+ * with q_rest the student's probability of all classes outside S. With rest =
+ * NULL the teacher's probabilities add to 1 over S, and q is not renormalised.
+ *  t_out [B] rows of N, ld_t apart.
+ *  idx   [B][K] int32, logit [B][K] fp32 or bf16: an entry whose index is not in
+ *               [0, N), or whose logit is not finite, is none; a class that is
+ *               named twice has both probabilities. A row without entries (a
+ *               padded one) has no loss and no gradient.
+ *  rest  [B]    logits of the rest; one that is not finite says p_rest = 0.
+ *  weight       factor of loss and gradient, finite and >= 0 (1/B: batch mean).
+ *  grad_t       out, B rows of N, ld_g apart: dL/dt, added to what is there
+ *               with accumulate = 1 (another loss's gradient), written with 0;
+ *               NULL: the loss alone.
+ *  loss  [B + 1] out: loss[0] = L, loss[1 + b] = L_b, as in dstd_softmax_ce_grad.
+ * 1 <= K <= min(N, DSTD_MAX_TOP); other sizes, and overlaps, as for dstd_scores.
+ */
+size_t dstd_distill_workspace_size(int64_t B, int64_t N, int64_t K);
+dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_out, int64_t ld_t,
+                              const int32_t *idx, const void *logit, dstd_dtype logit_dtype,
+                              const float *rest, float tau_soft, float t_cap, float weight,
+                              int32_t accumulate, float *grad_t, int64_t ld_g, float *loss,
+                              void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * One class for every row, drawn from its softmax by the random number u. With
+ * w_i = e^(z_i - max z), kept are
+ *   the top_k largest (0: all),
+ *   of these, falling, the shortest run whose w add to top_p of theirs or more
+ *   (1: all), equal scores by index in both,
+ *   of these, those with w_i >= min_p (0: all);
+ * the choice is the first class, by index, where the sum of the kept w up to it
+ * exceeds u times the sum of all kept. Weights are held to 2^-s of the largest,
+ * s = min(52, 62 - ceil(log2 N)), and their sums are exact.
+ *  u      [B]     fp32 in [0, 1); others are drawn in to it, NaN counts as 0.
+ *  choice [B] out int32; -1 for a row without entries.
+ *  logp   [B] out: ln of the choice's probability among the kept, -inf for a row
+ *                 without entries; or NULL to skip.
+ * top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1 (DSTD_ERR_PARAM otherwise).
+ */
+typedef struct {
+    int64_t top_k;
+    double top_p, min_p;
+} dstd_sample_params;
+size_t dstd_sample_workspace_size(const dstd_scores *s, const dstd_sample_params *p);
+dstd_status dstd_sample(const dstd_scores *s, const dstd_sample_params *p, const float *u,
+                        int32_t *choice, float *logp, void *ws, size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------ synfire terms -- */
 
 /*

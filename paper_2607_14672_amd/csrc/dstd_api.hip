@@ -1360,3 +1360,171 @@ dstd_status dstd_adamw_step(const dstd_tensor_list *list, const dstd_adamw_param
 }
 
 }  // extern "C"
+
+// --------------------------------------------------------------- answers --
+namespace {
+
+dstd_status check_rows(int64_t B, int64_t N, int64_t ld, const char *what) {
+    if (B < 0 || B > 65535 || N < 1 || N >= (1 << 24))
+        return fail(DSTD_ERR_SHAPE, "need 0 <= B <= 65535 and 1 <= N < 2^24");
+    if (ld < N || ld > (int64_t)1 << 40)
+        return fail(DSTD_ERR_SHAPE, "rows of %s lie %lld elements apart, need N to 2^40", what, (long long)ld);
+    return DSTD_OK;
+}
+size_t rows_bytes(int64_t B, int64_t N, int64_t ld, size_t elem) {
+    return B > 0 ? ((size_t)(B - 1) * (size_t)ld + (size_t)N) * elem : 0;
+}
+dstd_status check_top(int64_t K, int64_t N) {
+    if (K < 1 || K > N) return fail(DSTD_ERR_SHAPE, "need 1 <= K <= N");
+    if (K > DSTD_MAX_TOP) return fail(DSTD_ERR_UNSUPPORTED, "K = %lld exceeds DSTD_MAX_TOP = %d", (long long)K, DSTD_MAX_TOP);
+    return DSTD_OK;
+}
+
+dstd_status check_scores(const dstd_scores *s) {
+    if (!s) return fail(DSTD_ERR_NULL, "scores are NULL");
+    dstd_status st = check_rows(s->B, s->N, s->ld, "the scores");
+    if (st != DSTD_OK) return st;
+    if (s->dtype != DSTD_F32 && s->dtype != DSTD_BF16) return fail(DSTD_ERR_PARAM, "unknown dtype %d", s->dtype);
+    if (!isfinite((float)s->scale) || (float)s->scale == 0.f)
+        return fail(DSTD_ERR_PARAM, "scale must be finite and not 0 in fp32 (got %g)", s->scale);
+    return DSTD_OK;
+}
+
+dstd::ScoreRows score_rows(const dstd_scores *s) {
+    const bool neg = s->scale < 0.0;
+    dstd::ScoreRows r{};
+    r.x = s->x;
+    r.B = s->B;
+    r.N = s->N;
+    r.ld = s->ld;
+    r.bf16 = s->dtype == DSTD_BF16;
+    r.cap = isfinite(s->cap) ? s->cap : neg ? INFINITY : -INFINITY;
+    r.flip = neg ? 0x80000000u : 0u;
+    r.scale = fabs(s->scale);
+    return r;
+}
+Place scores_place(const dstd_scores *s) {
+    const size_t elem = s->dtype == DSTD_BF16 ? 2 : 4;
+    return Place{s->x, rows_bytes(s->B, s->N, s->ld, elem), elem, false, "the scores"};
+}
+
+dstd_status check_sample(const dstd_sample_params *p) {
+    if (!p) return fail(DSTD_ERR_NULL, "params is NULL");
+    if (p->top_k < 0) return fail(DSTD_ERR_PARAM, "top_k must be >= 0");
+    if (!(p->top_p > 0.0 && p->top_p <= 1.0)) return fail(DSTD_ERR_PARAM, "need 0 < top_p <= 1 (got %g)", p->top_p);
+    if (!(p->min_p >= 0.0 && p->min_p <= 1.0)) return fail(DSTD_ERR_PARAM, "need 0 <= min_p <= 1 (got %g)", p->min_p);
+    return DSTD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dstd_top_logits_workspace_size(const dstd_scores *s, int64_t K) {
+    if (check_scores(s) != DSTD_OK || check_top(K, s->N) != DSTD_OK) return 0;
+    return kAlign;
+}
+
+dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float *logit, float *rest,
+                            void *ws, size_t ws_bytes, void *stream) {
+    dstd_status st = check_scores(s);
+    if (st != DSTD_OK) return st;
+    if ((st = check_top(K, s->N)) != DSTD_OK) return st;
+    if (s->B > 0 && (!s->x || !idx || !logit)) return fail(DSTD_ERR_NULL, "x, idx and logit are required");
+    const size_t need = dstd_top_logits_workspace_size(s, K);
+    if ((st = check_ws(ws, ws_bytes, need)) != DSTD_OK) return st;
+    const size_t bk = (size_t)(s->B * K) * 4;
+    if ((st = check_places({scores_place(s), Place{idx, bk, 4, true, "idx"}, Place{logit, bk, 4, true, "logit"},
+                            Place{rest, (size_t)s->B * 4, 4, true, "rest"},
+                            Place{ws, need, kAlign, true, "the workspace"}})) != DSTD_OK)
+        return st;
+    const dstd::TopJob j{score_rows(s), (int)K, idx, logit, rest};
+    return hip_status(dstd::launch_top_logits(j, static_cast<hipStream_t>(stream)), "top_logits launch");
+}
+
+size_t dstd_distill_workspace_size(int64_t B, int64_t N, int64_t K) {
+    if (check_rows(B, N, N, "t_out") != DSTD_OK || check_top(K, N) != DSTD_OK) return 0;
+    return align_up(std::max<size_t>((size_t)(B * dstd::distill_parts(N)) * sizeof(float2), 1));
+}
+
+dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_out, int64_t ld_t,
+                              const int32_t *idx, const void *logit, dstd_dtype logit_dtype,
+                              const float *rest, float tau_soft, float t_cap, float weight,
+                              int32_t accumulate, float *grad_t, int64_t ld_g, float *loss, void *ws,
+                              size_t ws_bytes, void *stream) {
+    dstd_status st = check_rows(B, N, ld_t, "t_out");
+    if (st != DSTD_OK) return st;
+    if (grad_t && (st = check_rows(B, N, ld_g, "grad_t")) != DSTD_OK) return st;
+    if ((st = check_top(K, N)) != DSTD_OK) return st;
+    if (logit_dtype != DSTD_F32 && logit_dtype != DSTD_BF16)
+        return fail(DSTD_ERR_PARAM, "unknown dtype %d", (int)logit_dtype);
+    if (!(isfinite(tau_soft) && tau_soft > 0.f && isfinite(1.f / tau_soft)))
+        return fail(DSTD_ERR_PARAM, "tau_soft must be > 0, and 1 / tau_soft finite");
+    if (!isfinite(t_cap)) return fail(DSTD_ERR_PARAM, "t_cap must be finite");
+    if (!(isfinite(weight) && weight >= 0.f)) return fail(DSTD_ERR_PARAM, "weight must be finite and >= 0");
+    if (accumulate != 0 && accumulate != 1) return fail(DSTD_ERR_PARAM, "accumulate must be 0 or 1");
+    if (!loss || (B > 0 && (!t_out || !idx || !logit)))
+        return fail(DSTD_ERR_NULL, "t_out, idx, logit and loss are required");
+    const size_t need = dstd_distill_workspace_size(B, N, K);
+    if ((st = check_ws(ws, ws_bytes, need)) != DSTD_OK) return st;
+    const size_t le = dtype_bytes(logit_dtype), bk = (size_t)(B * K);
+    if ((st = check_places({Place{t_out, rows_bytes(B, N, ld_t, 4), 4, false, "t_out"},
+                            Place{idx, bk * 4, 4, false, "idx"}, Place{logit, bk * le, le, false, "logit"},
+                            Place{rest, (size_t)B * 4, 4, false, "rest"},
+                            Place{grad_t, rows_bytes(B, N, ld_g, 4), 4, true, "grad_t"},
+                            Place{loss, (size_t)(B + 1) * 4, 4, true, "loss"},
+                            Place{ws, need, kAlign, true, "the workspace"}})) != DSTD_OK)
+        return st;
+    dstd::KdArgs a{};
+    a.N = (int)N;
+    a.K = (int)K;
+    a.t = t_out;
+    a.ld_t = ld_t;
+    a.idx = idx;
+    a.rest = rest;
+    a.inv = 1.f / tau_soft;
+    a.c2 = (float)(1.4426950408889634 / (double)tau_soft);
+    a.t_cap = t_cap;
+    a.weight = weight;
+    a.accumulate = accumulate;
+    a.grad = grad_t;
+    a.ld_g = ld_g;
+    a.loss = loss;
+    a.part = static_cast<float2 *>(ws);
+    return hip_status(dstd::launch_distill(a, B, logit, logit_dtype == DSTD_BF16, static_cast<hipStream_t>(stream)),
+                      "distill launch");
+}
+
+size_t dstd_sample_workspace_size(const dstd_scores *s, const dstd_sample_params *p) {
+    if (check_scores(s) != DSTD_OK || check_sample(p) != DSTD_OK) return 0;
+    return kAlign;
+}
+
+dstd_status dstd_sample(const dstd_scores *s, const dstd_sample_params *p, const float *u, int32_t *choice,
+                        float *logp, void *ws, size_t ws_bytes, void *stream) {
+    dstd_status st = check_scores(s);
+    if (st != DSTD_OK) return st;
+    if ((st = check_sample(p)) != DSTD_OK) return st;
+    if (s->B > 0 && (!s->x || !u || !choice)) return fail(DSTD_ERR_NULL, "x, u and choice are required");
+    const size_t need = dstd_sample_workspace_size(s, p);
+    if ((st = check_ws(ws, ws_bytes, need)) != DSTD_OK) return st;
+    const size_t b4 = (size_t)s->B * 4;
+    if ((st = check_places({scores_place(s), Place{u, b4, 4, false, "u"}, Place{choice, b4, 4, true, "choice"},
+                            Place{logp, b4, 4, true, "logp"},
+                            Place{ws, need, kAlign, true, "the workspace"}})) != DSTD_OK)
+        return st;
+    dstd::SampleJob j{};
+    j.in = score_rows(s);
+    int bits = 0;  // ceil(log2 N)
+    while (((int64_t)1 << bits) < s->N) ++bits;
+    j.shift = std::min(52, 62 - bits);
+    j.top_k = (int)std::min<int64_t>(p->top_k, s->N);
+    j.top_p = p->top_p;
+    j.min_p = p->min_p;
+    j.u = u;
+    j.choice = choice;
+    j.logp = logp;
+    return hip_status(dstd::launch_sample(j, static_cast<hipStream_t>(stream)), "sample launch");
+}
+
+}  // extern "C"

@@ -446,6 +446,12 @@ hipError_t launch_backward(const LifConst &C, int64_t B, int64_t N_in, int64_t N
                                   dq, grad_W, grad_t_in}, st);
 }
 
+hipError_t launch_loss_total(int64_t B, float *loss, hipStream_t st) {
+    hipLaunchKernelGGL(loss_total_kernel, dim3(1), dim3(kLossThreads), 0, st, static_cast<int>(B),
+                       loss);
+    return hipGetLastError();
+}
+
 hipError_t launch_softmax_ce(int64_t B, int64_t N, const float *t, const int *labels,
                              float tau_soft, float t_cap, float *grad, float *loss,
                              hipStream_t st) {

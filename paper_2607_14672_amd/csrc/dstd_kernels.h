@@ -82,6 +82,58 @@ hipError_t launch_softmax_ce(int64_t B, int64_t N, const float *t, const int *la
 hipError_t launch_mse(int64_t B, int64_t N, const float *t, const float *y, float *grad,
                       float *loss, hipStream_t st);
 
+// loss[0] = sum of loss[1 .. B], in a fixed order
+hipError_t launch_loss_total(int64_t B, float *loss, hipStream_t st);
+
+// --------------------------------------------------------------- answers --
+// Rows of scores: an entry that is not finite counts as cap (-+inf where it is
+// left out); flip: the sign bit where smaller scores are likelier; scale > 0.
+struct ScoreRows {
+    const void *x;
+    int64_t B, N, ld;
+    bool bf16;
+    float cap;
+    uint32_t flip;
+    double scale;
+};
+struct TopJob {
+    ScoreRows in;
+    int K;
+    int32_t *idx;
+    float *logit, *rest;
+};
+hipError_t launch_top_logits(const TopJob &j, hipStream_t st);
+
+// shift: weights are integers, the largest 2^shift, and a row of them adds up to
+// 2^62 at most.
+struct SampleJob {
+    ScoreRows in;
+    int shift, top_k;
+    double top_p, min_p;
+    const float *u;
+    int32_t *choice;
+    float *logp;
+};
+hipError_t launch_sample(const SampleJob &j, hipStream_t st);
+
+// inv = 1 / tau_soft, c2 = log2(e) / tau_soft; part: distill_parts(N) for each row.
+constexpr int kKdMaxK = 256;
+struct KdArgs {
+    int N, K;
+    const float *t;
+    int64_t ld_t;
+    const int32_t *idx;
+    const float *rest;
+    float inv, c2, t_cap, weight;
+    int accumulate;
+    float *grad;
+    int64_t ld_g;
+    float *loss;
+    float2 *part;
+};
+int64_t distill_parts(int64_t N);
+hipError_t launch_distill(const KdArgs &a, int64_t B, const void *logit, bool bf16, hipStream_t st);
+
 // ------------------------------------------------------------------ conv --
 // Geometry of a conv layer, derived on the host. The (pooled) input map has
 // Hp x Wp cells of P raw pixels; PC = P * C_in raw inputs per cell.

@@ -27,6 +27,7 @@ DSTD_ERR_HIP = -6
 DSTD_F32 = 0
 DSTD_BF16 = 1
 DSTD_MAX_M = 256
+DSTD_MAX_TOP = 256
 DSTD_NOALLOC_SCRATCH_BYTES = 32 << 20
 DSTD_FLAG_CONTRACT_SPARSE = 0x2
 DSTD_FLAG_CONTRACT_MFMA = 0x4
@@ -64,6 +65,15 @@ class dstd_tensor_list(C.Structure):
 
 class dstd_adamw_params(C.Structure):
     _fields_ = [(k, C.c_double) for k in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")]
+
+
+class dstd_scores(C.Structure):
+    _fields_ = ([("x", C.c_void_p)] + [(k, C.c_int64) for k in ("B", "N", "ld")] +
+                [("dtype", C.c_int32), ("cap", C.c_float), ("scale", C.c_double)])
+
+
+class dstd_sample_params(C.Structure):
+    _fields_ = [("top_k", C.c_int64), ("top_p", C.c_double), ("min_p", C.c_double)]
 
 
 class DSTDError(RuntimeError):
@@ -114,6 +124,13 @@ _SIGS = {
     "dstd_skip_delay_concat_backward": (_I, [_L, _L, _L, _L, _P, _P, C.c_int32, _P, _P]),
     "dstd_softmax_ce_grad": (_I, [_L, _L, _P, _P, _F, _F, _P, _P, _P]),
     "dstd_mse_grad": (_I, [_L, _L, _P, _P, _P, _P, _P]),
+    "dstd_top_logits_workspace_size": (_S, [_P, _L]),
+    "dstd_top_logits": (_I, [_P, _L, _P, _P, _P, _P, _S, _P]),
+    "dstd_distill_workspace_size": (_S, [_L, _L, _L]),
+    "dstd_distill_grad": (_I, [_L, _L, _L, _P, _L, _P, _P, _I, _P, _F, _F, _F, C.c_int32, _P, _L, _P,
+                               _P, _S, _P]),
+    "dstd_sample_workspace_size": (_S, [_P, _P]),
+    "dstd_sample": (_I, [_P, _P, _P, _P, _P, _P, _S, _P]),
     "dstd_tensor_list_size": (_S, [_L, _P]),
     "dstd_tensor_list_build": (_I, [_L, _P, _P, _S, _P, _P]),
     "dstd_tensor_list_workspace_size": (_S, [_P]),
@@ -278,6 +295,33 @@ def dstd_softmax_ce_grad(B, N, t_out, labels, tau_soft, t_cap, grad_t, loss, str
 
 def dstd_mse_grad(B, N, t_out, target, grad_t, loss, stream):
     return _load().dstd_mse_grad(B, N, t_out, target, grad_t, loss, stream)
+
+
+def dstd_top_logits_workspace_size(s, K):
+    return _load().dstd_top_logits_workspace_size(_ref(s), K)
+
+
+def dstd_top_logits(s, K, idx, logit, rest, ws, ws_bytes, stream):
+    return _load().dstd_top_logits(_ref(s), K, idx, logit, rest, ws, ws_bytes, stream)
+
+
+def dstd_distill_workspace_size(B, N, K):
+    return _load().dstd_distill_workspace_size(B, N, K)
+
+
+def dstd_distill_grad(B, N, K, t_out, ld_t, idx, logit, logit_dtype, rest, tau_soft, t_cap, weight,
+                      accumulate, grad_t, ld_g, loss, ws, ws_bytes, stream):
+    return _load().dstd_distill_grad(B, N, K, t_out, ld_t, idx, logit, logit_dtype, rest, tau_soft,
+                                     t_cap, weight, accumulate, grad_t, ld_g, loss, ws, ws_bytes,
+                                     stream)
+
+
+def dstd_sample_workspace_size(s, p):
+    return _load().dstd_sample_workspace_size(_ref(s), _ref(p))
+
+
+def dstd_sample(s, p, u, choice, logp, ws, ws_bytes, stream):
+    return _load().dstd_sample(_ref(s), _ref(p), u, choice, logp, ws, ws_bytes, stream)
 
 
 def dstd_tensor_list_size(n_tensors, tensors):
@@ -730,6 +774,170 @@ def mse_grad(t_out, target):
     _check("dstd_mse_grad", dstd_mse_grad(B, N, _ptr(t_out), _ptr(target), _ptr(grad), _ptr(loss),
                                           _stream(t_out.device)))
     return grad, loss
+
+
+def _rows(x, dtypes, what):
+    """A matrix on the GPU whose rows lie whole in memory, copied only if they do not."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
+    if x.dtype not in dtypes:
+        raise TypeError(f"{what} must be one of {list(dtypes)}, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{what} must live on the GPU")
+    if x.dim() != 2:
+        raise ValueError(f"{what} must have two dimensions, got {x.dim()}")
+    if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        x = x.contiguous()
+    return x
+
+
+def _ld(x):
+    """Elements from one row of `_rows` to the next (a single row has any stride)."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _given(x, shape, dtype, dev, what, rows=False):
+    """A tensor that the caller hands in or wants written, checked: contiguous, or
+    with `rows` of whole rows."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
+    if x.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {x.dtype}")
+    if x.device != dev:
+        raise ValueError(f"{what} must be on {dev}")
+    if x.shape != torch.Size(shape):
+        raise ValueError(f"{what} has shape {tuple(x.shape)}, not {tuple(shape)}")
+    if rows:
+        if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+            raise ValueError(f"{what} must have rows that lie whole in memory, one behind the other")
+    elif not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return x
+
+
+def _out(x, shape, dtype, dev, what):
+    """The caller's tensor for an output, or a new one."""
+    if x is None:
+        return _torch().empty(shape, dtype=dtype, device=dev)
+    return _given(x, shape, dtype, dev, what)
+
+
+def _ws_for(ws, need, dev):
+    """The caller's workspace if it is large enough, or a new one."""
+    torch = _torch()
+    if ws is None:
+        return workspace(need, dev)
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8:
+        raise TypeError("ws must be a uint8 tensor")
+    if ws.device != dev:
+        raise ValueError(f"ws must be on {dev}")
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws if ws.numel() >= need else workspace(need, dev)
+
+
+def _on(dev, name, fn, *args):
+    """One call on a device (launches go to the current one) and its current stream."""
+    torch = _torch()
+    stream = torch._C._cuda_getCurrentRawStream(dev.index)
+    if torch.cuda.current_device() == dev.index:
+        _check(name, fn(*args, stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(name, fn(*args, stream))
+
+
+def make_scores(x, scale: float = 1.0, cap: Optional[float] = None) -> dstd_scores:
+    """Rows of scores x [B, N], f32 or bf16, as top_logits and sample read them: logits
+    scale * x. Entries that are not finite count as `cap`, or are left out (None).
+    It holds x's address, so x has to stay while it is used."""
+    torch = _torch()
+    code = {torch.float32: DSTD_F32, torch.bfloat16: DSTD_BF16}
+    return dstd_scores(x.data_ptr(), x.shape[0], x.shape[1], _ld(x), code[x.dtype],
+                       math.nan if cap is None else float(cap), float(scale))
+
+
+def top_logits(x, K: int, scale: float = 1.0, cap: Optional[float] = None, idx=None, logit=None,
+               rest=None, ws=None):
+    """The K largest logits of every row of scores x [B, N] (f32 or bf16; logits scale * x,
+    for spike times scale = -1 / tau_soft), falling, equal ones by index. Entries that are
+    not finite count as `cap`, or are left out (None). Returns (idx [B, K] int32, logit
+    [B, K] f32, rest [B] f32): classes, logits, and the log of the sum of all others'
+    exponentials; -1 and -inf where there is none."""
+    torch = _torch()
+    x = _rows(x, (torch.float32, torch.bfloat16), "x")
+    dev, B = x.device, x.shape[0]
+    s = make_scores(x, scale, cap)
+    need = dstd_top_logits_workspace_size(s, K)
+    idx = _out(idx, (B, max(K, 0)), torch.int32, dev, "idx")
+    logit = _out(logit, (B, max(K, 0)), torch.float32, dev, "logit")
+    rest = _out(rest, (B,), torch.float32, dev, "rest")
+    ws = _ws_for(ws, need, dev)
+    _on(dev, "dstd_top_logits", dstd_top_logits, s, K, _ptr(idx), _ptr(logit), _ptr(rest), _ptr(ws),
+        ws.numel())
+    return idx, logit, rest
+
+
+def distill_grad(t_out, idx, logit, rest=None, tau_soft: float = 1.0, t_cap: Optional[float] = None,
+                 weight: Optional[float] = None, grad=None, accumulate: bool = False,
+                 need_grad: bool = True, loss=None, ws=None):
+    """Distillation of output spike times t_out [B, N] from a teacher's top logits (idx,
+    logit [B, K] and rest [B], as top_logits gives them). Returns (dL/dt [B, N], loss
+    [B + 1]): loss[0] = L, loss[1 + b] = sample b's term. `weight`: factor of both (default
+    1 / B). dL/dt is written to `grad` if given, with `accumulate` added to it (another loss's
+    gradient); need_grad=False: the loss alone."""
+    torch = _torch()
+    t_out = _rows(t_out, (torch.float32,), "t_out")
+    if t_cap is None:
+        raise ValueError("t_cap is required (time used for outputs that did not fire)")
+    if accumulate and grad is None:
+        raise ValueError("accumulate needs the gradient to add to")
+    if grad is not None and not need_grad:
+        raise ValueError("grad is given, but need_grad is False")
+    dev, (B, N) = t_out.device, t_out.shape
+    idx = _rows(idx, (torch.int32,), "idx").contiguous()
+    logit = _rows(logit, (torch.float32, torch.bfloat16), "logit").contiguous()
+    K = idx.shape[1]
+    _given(idx, (B, K), torch.int32, dev, "idx")
+    _given(logit, (B, K), logit.dtype, dev, "logit")
+    if rest is not None:
+        _given(rest, (B,), torch.float32, dev, "rest")
+    if need_grad:
+        grad = (torch.empty((B, N), dtype=torch.float32, device=dev) if grad is None else
+                _given(grad, (B, N), torch.float32, dev, "grad", rows=True))
+    loss = _out(loss, (B + 1,), torch.float32, dev, "loss")
+    if weight is None:
+        weight = 1.0 / max(B, 1)
+    need = dstd_distill_workspace_size(B, N, K)
+    ws = _ws_for(ws, need, dev)
+    _on(dev, "dstd_distill_grad", dstd_distill_grad, B, N, K, _ptr(t_out), _ld(t_out), _ptr(idx),
+        _ptr(logit), DSTD_F32 if logit.dtype == torch.float32 else DSTD_BF16, _ptr(rest),
+        float(tau_soft), float(t_cap), float(weight), 1 if accumulate else 0, _ptr(grad),
+        _ld(grad) if need_grad else 0, _ptr(loss), _ptr(ws), ws.numel())
+    return grad, loss
+
+
+def sample(x, u, scale: float = 1.0, cap: Optional[float] = None, top_k: int = 0, top_p: float = 1.0,
+           min_p: float = 0.0, choice=None, logp=None, ws=None):
+    """One class for every row of scores x [B, N] (as in top_logits), drawn from its
+    softmax by the random numbers u [B] f32 in [0, 1): of the top_k largest logits (0:
+    all) the shortest run of probability top_p or more, and of these those with at least
+    min_p times the largest's probability. Returns (choice [B] int32, logp [B] f32: the
+    log of its probability among what is kept); -1 and -inf for a row without entries."""
+    torch = _torch()
+    x = _rows(x, (torch.float32, torch.bfloat16), "x")
+    dev, B = x.device, x.shape[0]
+    _given(u, (B,), torch.float32, dev, "u")
+    s = make_scores(x, scale, cap)
+    p = dstd_sample_params(int(top_k), float(top_p), float(min_p))
+    need = dstd_sample_workspace_size(s, p)
+    choice = _out(choice, (B,), torch.int32, dev, "choice")
+    logp = _out(logp, (B,), torch.float32, dev, "logp")
+    ws = _ws_for(ws, need, dev)
+    _on(dev, "dstd_sample", dstd_sample, s, p, _ptr(u), _ptr(choice), _ptr(logp), _ptr(ws), ws.numel())
+    return choice, logp
 
 
 class TensorList:
