@@ -84,6 +84,28 @@ __device__ __forceinline__ void row_each(const E *p, int lo, int hi, int tid, in
     for (int i = nv * V::n + tid; i < hi - lo; i += count) f(lo + i, widen1(p[i]));
 }
 
+// As row_each over [0, n), f(group, index, score): the entries of a thread fall into
+// kRowAhead groups.
+template <typename E, typename F>
+__device__ __forceinline__ void row_groups(const E *p, int n, int tid, int count, F f) {
+    using V = RowVec<E>;
+    const int nv = n / V::n;
+    for (int v0 = tid; v0 < nv; v0 += kRowAhead * count) {
+        typename V::type r[kRowAhead] = {};
+#pragma unroll
+        for (int a = 0; a < kRowAhead; ++a)
+            if (v0 + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v0 + a * count) * V::n);
+#pragma unroll
+        for (int a = 0; a < kRowAhead; ++a) {
+            if (v0 + a * count >= nv) break;
+#pragma unroll
+            for (int k = 0; k < V::n; ++k)
+                f(a, (v0 + a * count) * V::n + k, widen1(static_cast<E>(r[a][k])));
+        }
+    }
+    for (int i = nv * V::n + tid; i < n; i += count) f(0, i, widen1(p[i]));
+}
+
 // ------------------------------------------------------ sums over a block --
 // Every result goes to every thread; `red` holds a u64 per wave and one more.
 // The order of each is fixed.

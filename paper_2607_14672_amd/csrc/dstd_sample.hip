@@ -9,6 +9,8 @@
 //            w up to i exceeds u times the sum of all kept.
 //
 // Both order by the score itself, not by its product with the scale.
+#include <float.h>
+
 #include "dstd_answer.h"
 #include "dstd_kernels.h"
 #include "dstd_profile.h"
@@ -18,12 +20,15 @@ namespace dstd {
 namespace {
 
 constexpr int kBins = 2048;  // of a histogram over a row
-// Candidates that are put in order in one go: each is compared with all others.
+// Candidates of a row that are held at once, and so the largest top_k that is
+// chosen from candidates.
 template <int T> constexpr int kList = T >= 1024 ? 2048 : 1024;
+constexpr int kMaxPicked = 1024;
+constexpr int kGroups = kRowAhead;  // of a thread's share of the row, a maximum each
 
 template <int T> struct RowShared {
     u64 red[T / kWave + 1];
-    u64 list[kList<T>], sorted[kList<T>];
+    u64 list[kList<T>];
     u64 hist[kBins];
     u64 found[2];
     int count;
@@ -51,15 +56,38 @@ struct One {
     __device__ u64 operator()(u32) const { return 1; }
 };
 
-// The list in falling order, each entry placed by how many are larger.
+// The first n entries of the list in falling order, in place. Few are placed by how
+// many are larger, each against all (written back from the histogram's memory); more by
+// a bitonic network over the next power of two.
 template <int T> __device__ void sort_list(RowShared<T> &sh, int n) {
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += T) {
-        const u64 mine = sh.list[i];
-        int at = 0;
-        for (int k = 0; k < n; ++k) at += sh.list[k] > mine;
-        sh.sorted[at] = mine;
+    if (n <= 128) {
+        for (int i = threadIdx.x; i < n; i += T) {
+            const u64 mine = sh.list[i];
+            int at = 0;
+            for (int k = 0; k < n; ++k) at += sh.list[k] > mine;
+            sh.hist[at] = mine;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += T) sh.list[i] = sh.hist[i];
+        __syncthreads();
+        return;
     }
+    int p = 256;
+    while (p < n) p *= 2;
+    for (int i = n + threadIdx.x; i < p; i += T) sh.list[i] = 0;
+    for (int k = 2; k <= p; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            __syncthreads();
+            for (int t = threadIdx.x; t < p / 2; t += T) {
+                const int i = 2 * t - (t & (j - 1)), o = i + j;
+                const u64 x = sh.list[i], y = sh.list[o];
+                if ((x < y) == ((i & k) == 0)) {
+                    sh.list[i] = y;
+                    sh.list[o] = x;
+                }
+            }
+        }
     __syncthreads();
 }
 
@@ -228,7 +256,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
 #pragma unroll
         for (int k = 0; k < each; ++k) {
             const int i = threadIdx.x * each + k;
-            w[k] = i < count ? weight(rank_key(sh.sorted[i])) : 0;
+            w[k] = i < count ? weight(rank_key(sh.list[i])) : 0;
             mine += w[k];
         }
         u64 all;
@@ -238,7 +266,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
 #pragma unroll
             for (int k = 0; k < each; ++k) {
                 if (static_cast<double>(at) < target && static_cast<double>(at + w[k]) >= target)
-                    sh.found[0] = sh.sorted[threadIdx.x * each + k];
+                    sh.found[0] = sh.list[threadIdx.x * each + k];
                 at += w[k];
             }
         __syncthreads();
@@ -309,47 +337,115 @@ __global__ __launch_bounds__(T) void sample_kernel(int n, int64_t ld, const E *_
     }
 }
 
+// Candidates for the K first entries of a row's order: all that reach a bound which K
+// entries reach at least. The bound is the K-th largest of the groups' largest values, or
+// a little less: few others reach it unless the largest lie close together in the row.
+// Goodness y without a look at entries that do not count: y < INF is false for these, and
+// they are no candidates.
 template <int T, typename E>
-__global__ __launch_bounds__(T) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
-                                                       double scale, float c2, int K, int32_t *__restrict__ idx,
-                                                       float *__restrict__ logit, float *__restrict__ rest) {
-    __shared__ RowShared<T> sh;
-    const int64_t b = blockIdx.x;
-    const E *row = x + b * ld;
-    // Of the threads' largest keys the K-th largest bounds the row's K-th largest
-    // from below; few other keys reach it.
-    u32 best = 0;
-    row_each<E>(row, 0, n, threadIdx.x, T,
-                [&](int, float v) { best = max(best, key_of(goodness(v, m))); });
-    u32 *bests = reinterpret_cast<u32 *>(sh.hist);
-    bests[threadIdx.x] = best;
-    if (threadIdx.x == 0) sh.found[0] = 0;
-    __syncthreads();
-    int above = 0;
-    for (int k = 0; k < T; ++k) {
-        const u32 other = bests[k];
-        above += other > best || (other == best && k < static_cast<int>(threadIdx.x));
+__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, bool caps, int K) {
+    float best[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) best[g] = -INFINITY;
+    row_groups<E>(row, n, threadIdx.x, T, [&](int g, int, float x) {
+        // med3 passes NaN over; +inf gives FLT_MAX, which is looked at below
+        const float y = caps ? goodness(x, m) : __uint_as_float(__float_as_uint(x) ^ m.flip);
+        best[g] = __builtin_amdgcn_fmed3f(y, best[g], FLT_MAX);
+    });
+    float lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        if (best[g] > -INFINITY) lo = fminf(lo, best[g]);
+        hi = best[g] == best[g] ? fmaxf(hi, best[g]) : FLT_MAX;
     }
-    if (above == K - 1) sh.found[0] = best;
+    hi = value_of(static_cast<u32>(block_max<T>(key_of(hi), sh.red)));
+    lo = value_of(static_cast<u32>(block_min<T>(key_of(lo), sh.red)));
+    if (hi >= FLT_MAX || K > kGroups * T) return -FLT_MAX;
+    if (!(hi > -INFINITY)) return INFINITY;  // nothing counts
+    // bins of the range of the maxima
+    const float per = static_cast<float>(kBins / (static_cast<double>(hi) - static_cast<double>(lo)));
+    u32 *hist = reinterpret_cast<u32 *>(sh.hist);
+    for (int k = threadIdx.x; k < kBins; k += T) hist[k] = 0;
+    if (threadIdx.x == 0) sh.count = -1;
     __syncthreads();
-    const u32 bound = static_cast<u32>(sh.found[0]);
-    int count = collect<T>(sh, row, n, m, [&](u32 key, int) { return key >= bound; });
+    int bin[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        bin[g] = kBins;  // a group without an entry
+        if (best[g] > -INFINITY) {
+            bin[g] = static_cast<int>(fminf((hi - best[g]) * per, kBins - 1.f));
+            atomicAdd(&hist[bin[g]], 1u);
+        }
+    }
+    __syncthreads();
+    constexpr int each = kBins / T;
+    u64 mine = 0;
+#pragma unroll
+    for (int k = 0; k < each; ++k) mine += hist[threadIdx.x * each + k];
+    u64 all;
+    u64 at = block_before<T>(mine, sh.red, &all);
+    if (at < static_cast<u64>(K) && at + mine >= static_cast<u64>(K))
+        for (int k = 0; k < each; ++k) {
+            at += hist[threadIdx.x * each + k];
+            if (at >= static_cast<u64>(K)) {
+                sh.count = threadIdx.x * each + k;
+                break;
+            }
+        }
+    __syncthreads();
+    const int last = sh.count;
+    float bound = INFINITY;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+        if (bin[g] <= last) bound = fminf(bound, best[g]);
+    bound = value_of(static_cast<u32>(block_min<T>(key_of(bound), sh.red)));
+    return last < 0 ? -FLT_MAX : bound;
+}
+
+// The K first entries of a row's order and at most a few more, sorted, in the list;
+// returns how many there are (fewer than K where the row has fewer). kSum: *others is the
+// sum over the entries behind the K-th.
+template <int T, bool kSum, typename E>
+__device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, bool caps, int K, float c2,
+                          ExpSum *others) {
+    float bound = -FLT_MAX;
+    if (n > kList<T>) bound = candidate_bound<T>(sh, row, n, m, caps, K);
+    if (kSum) *others = ExpSum{-INFINITY, 0.f};
+    if (bound == INFINITY) return 0;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    float sum = 0.f;  // of what is below the bound, relative to it
+    row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float x) {
+        const float y = caps ? goodness(x, m) : __uint_as_float(__float_as_uint(x) ^ m.flip);
+        const float d = y - bound;
+        if (d >= 0.f && y < INFINITY) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kList<T>) sh.list[at] = rank_of(key_of(y), i);
+        }
+        if (kSum && d < 0.f) sum += exp_of(d, c2);
+    });
+    __syncthreads();
+    int count = sh.count;
+    bool listed = bound == -FLT_MAX;  // the sum is that of the list's others alone
     if (count > kList<T>) {
         const Extremes ex = row_extremes<T>(sh, row, n, m);
         const Border kept = by_order<T>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
         count = collect<T>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+        sum = 0.f;
+        listed = false;
     }
     sort_list<T>(sh, count);
-    for (int k = threadIdx.x; k < K; k += T) {
-        const bool some = k < count;
-        const u64 r = some ? sh.sorted[k] : 0;
-        idx[b * K + k] = some ? rank_index(r) : -1;
-        logit[b * K + k] = some ? static_cast<float>(static_cast<double>(value_of(rank_key(r))) * scale) : -INFINITY;
-    }
-    if (!rest) return;
+    if (!kSum || count < K) return count;
     ExpSum s{-INFINITY, 0.f};
-    if (count >= K) {
-        const u64 last = sh.sorted[K - 1];
+    const bool some = __syncthreads_or(sum > 0.f);
+    if (some || listed) {
+        if (sum > 0.f) s = ExpSum{bound, sum};
+        for (int k = K + threadIdx.x; k < count; k += T)
+            s = exp_join(s, ExpSum{value_of(rank_key(sh.list[k])), 1.f}, c2);
+    } else {
+        // all others far below the bound (their sum there is 0), or no bound was found
+        const u64 last = sh.list[K - 1];
         row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float v) {
             const float y = goodness(v, m);
             const u32 key = key_of(y);
@@ -362,19 +458,119 @@ __global__ __launch_bounds__(T) void top_logits_kernel(int n, int64_t ld, const 
             }
         });
     }
-    s = block_exp_sum<T>(s, c2, sh.red);
-    if (threadIdx.x == 0)
+    *others = block_exp_sum<T>(s, c2, sh.red);
+    return count;
+}
+
+template <int T, typename E>
+__global__ __launch_bounds__(T) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
+                                                       bool caps, double scale, float c2, int K,
+                                                       int32_t *__restrict__ idx, float *__restrict__ logit,
+                                                       float *__restrict__ rest) {
+    __shared__ RowShared<T> sh;
+    const int64_t b = blockIdx.x;
+    const E *row = x + b * ld;
+    ExpSum s;
+    const int count = candidates<T, true>(sh, row, n, m, caps, K, c2, &s);
+    for (int k = threadIdx.x; k < K; k += T) {
+        const bool some = k < count;
+        const u64 r = some ? sh.list[k] : 0;
+        idx[b * K + k] = some ? rank_index(r) : -1;
+        logit[b * K + k] = some ? static_cast<float>(static_cast<double>(value_of(rank_key(r))) * scale) : -INFINITY;
+    }
+    if (threadIdx.x == 0 && rest)
         rest[b] = s.s > 0.f ? static_cast<float>(static_cast<double>(s.m) * scale + log(static_cast<double>(s.s)))
                             : -INFINITY;
 }
 
+// One class from the top_k <= kMaxPicked first entries of each row.
+template <int T, typename E>
+__global__ __launch_bounds__(T) void sample_picked_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
+                                                          bool caps, double scale, int shift, int top_k,
+                                                          double top_p, double min_p, const float *__restrict__ u,
+                                                          int32_t *__restrict__ choice, float *__restrict__ logp) {
+    __shared__ RowShared<T> sh;
+    const int64_t b = blockIdx.x;
+    const E *row = x + b * ld;
+    int count = candidates<T, false>(sh, row, n, m, caps, top_k, 0.f, nullptr);
+    if (count == 0) {
+        if (threadIdx.x == 0) {
+            choice[b] = -1;
+            if (logp) logp[b] = -INFINITY;
+        }
+        return;
+    }
+    count = min(count, top_k);
+    const Mass mass{value_of(rank_key(sh.list[0])), scale, ldexp(1.0, shift)};
+    constexpr int each = kMaxPicked / T > 1 ? kMaxPicked / T : 1;
+    u64 w[each], mine = 0;
+    const int first = threadIdx.x * each;
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        w[k] = first + k < count ? mass(rank_key(sh.list[first + k])) : 0;
+        mine += w[k];
+    }
+    u64 all;
+    u64 at = block_before<T>(mine, sh.red, &all);
+    const double target = top_p < 1.0 ? top_p * static_cast<double>(all) : INFINITY;
+    u64 keeps = 0;
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        if (first + k < count && static_cast<double>(at) < target &&
+            (min_p == 0.0 || exp(-mass.distance(rank_key(sh.list[first + k]))) >= min_p))
+            ++keeps;
+        at += w[k];
+    }
+    count = static_cast<int>(block_add<T>(keeps, sh.red));
+    // what is kept, by index
+    u64 back[each];
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        const u64 r = first + k < count ? sh.list[first + k] : 0;
+        back[k] = (r << 32) | (r >> 32);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < each; ++k)
+        if (first + k < count) sh.list[first + k] = back[k];
+    sort_list<T>(sh, count);
+    mine = 0;
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        w[k] = first + k < count ? mass(static_cast<u32>(sh.list[first + k])) : 0;
+        mine += w[k];
+    }
+    at = block_before<T>(mine, sh.red, &all);
+    const double share = fmin(fmax(static_cast<double>(u[b]), 0.0), 1.0 - 0x1p-24);
+    const double goal = share * static_cast<double>(all);
+    if (static_cast<double>(at) <= goal && static_cast<double>(at + mine) > goal)
+#pragma unroll
+        for (int k = 0; k < each; ++k) {
+            if (static_cast<double>(at) <= goal && static_cast<double>(at + w[k]) > goal) {
+                const u64 r = sh.list[first + k];
+                choice[b] = static_cast<int>(~static_cast<u32>(r >> 32));
+                if (logp)
+                    logp[b] = static_cast<float>(-mass.distance(static_cast<u32>(r)) -
+                                                 log(static_cast<double>(all) / mass.one));
+            }
+            at += w[k];
+        }
+}
+
 template <typename E>
 hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
-#define SAMPLE(T)                                                                                          \
-    hipLaunchKernelGGL((sample_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,         \
-                       static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                  \
-                       ScoreMap{j.in.cap, j.in.flip}, j.in.scale, j.shift, j.top_k, j.top_p, j.min_p, j.u, \
-                       j.choice, j.logp)
+    const bool caps = isfinite(j.in.cap);
+#define SAMPLE(T)                                                                                              \
+    if (j.top_k > 0 && j.top_k <= kMaxPicked)                                                                  \
+        hipLaunchKernelGGL((sample_picked_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,  \
+                           static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                  \
+                           ScoreMap{j.in.cap, j.in.flip}, caps, j.in.scale, j.shift, j.top_k, j.top_p, j.min_p, \
+                           j.u, j.choice, j.logp);                                                             \
+    else                                                                                                       \
+        hipLaunchKernelGGL((sample_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,         \
+                           static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                  \
+                           ScoreMap{j.in.cap, j.in.flip}, j.in.scale, j.shift, j.top_k, j.top_p, j.min_p, j.u, \
+                           j.choice, j.logp)
     if (j.in.N <= 512) SAMPLE(64);
     else if (j.in.N <= 4096) SAMPLE(256);
     else SAMPLE(1024);
@@ -385,10 +581,11 @@ hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
 template <typename E>
 hipError_t launch_top_t(const TopJob &j, hipStream_t st) {
     const float c2 = static_cast<float>(j.in.scale * 1.4426950408889634);
-#define TOP(T)                                                                                            \
-    hipLaunchKernelGGL((top_logits_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,    \
-                       static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                 \
-                       ScoreMap{j.in.cap, j.in.flip}, j.in.scale, c2, j.K, j.idx, j.logit, j.rest)
+#define TOP(T)                                                                                              \
+    hipLaunchKernelGGL((top_logits_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,      \
+                       static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                   \
+                       ScoreMap{j.in.cap, j.in.flip}, isfinite(j.in.cap), j.in.scale, c2, j.K, j.idx,       \
+                       j.logit, j.rest)
     if (j.in.N <= 512) TOP(64);
     else if (j.in.N <= 4096) TOP(256);
     else TOP(1024);

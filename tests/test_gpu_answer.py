@@ -61,6 +61,9 @@ def _scores(kind, B, N, seed):
         x[~np.isfinite(x)] = 0
     elif kind == "near":  # distinct, all within a few steps
         x = (1.0 + rng.integers(0, 50, (B, N)) * 2.0 ** -23).astype(np.float32)
+    elif kind == "signalling":  # NaN of the other kind, and +inf
+        x[rng.random((B, N)) < 0.3] = np.inf
+        x.view(np.uint32)[rng.random((B, N)) < 0.3] = 0x7f810000
     elif kind == "sorted":  # one thread's share holds many of the largest
         x = np.sort(x, axis=1)
     elif kind == "outlier":
@@ -69,7 +72,7 @@ def _scores(kind, B, N, seed):
     return x
 
 
-KINDS = ["plain", "masked", "ties", "equal", "zeros", "huge", "near", "sorted", "outlier"]
+KINDS = ["plain", "masked", "ties", "equal", "zeros", "huge", "near", "sorted", "outlier", "signalling"]
 SIZES = [1, 2, 63, 64, 65, 511, 512, 513, 1000, 4096, 4097, 20011]
 
 
