@@ -292,8 +292,8 @@ dstd_status dstd_mse_grad(int64_t B, int64_t N, const float *t_out, const float 
  *        that is masked) counts as, as t_cap above; a cap that is not finite
  *        leaves such entries out.
  * 1 <= N < 2^24, 0 <= B <= 65535, ld >= N; scale finite and not 0 in fp32. No
- * output or workspace of a call may overlap another or an input
- * (DSTD_ERR_PARAM).
+ * output of a call may overlap another or an input (DSTD_ERR_PARAM; rows with
+ * room between them count as a whole, the room too).
  */
 typedef struct {
     const void *x;
@@ -314,9 +314,8 @@ typedef struct {
  *               NULL to skip.
  * 1 <= K <= min(N, DSTD_MAX_TOP). Rows are ordered by their scores, exactly.
  */
-size_t dstd_top_logits_workspace_size(const dstd_scores *s, int64_t K);
 dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float *logit,
-                            float *rest, void *ws, size_t ws_bytes, void *stream);
+                            float *rest, void *stream);
 
 /*
  * Distillation from a teacher's top logits: the Kullback-Leibler divergence of
@@ -367,9 +366,8 @@ typedef struct {
     int64_t top_k;
     double top_p, min_p;
 } dstd_sample_params;
-size_t dstd_sample_workspace_size(const dstd_scores *s, const dstd_sample_params *p);
 dstd_status dstd_sample(const dstd_scores *s, const dstd_sample_params *p, const float *u,
-                        int32_t *choice, float *logp, void *ws, size_t ws_bytes, void *stream);
+                        int32_t *choice, float *logp, void *stream);
 
 /* ------------------------------------------------------ synfire terms -- */
 

@@ -59,29 +59,34 @@ template <typename E> __device__ __forceinline__ typename RowVec<E>::type load_v
     return *reinterpret_cast<const typename RowVec<E>::any *>(p);
 }
 
-// f(index, score) for the elements [lo, hi) of a row by `count` threads, of which
-// this is number `tid`; kRowAhead vectors a thread on the way at once. lo is a
-// multiple of a vector's elements.
+// f(index, score) for the first n elements of a row by `count` threads, of which
+// this is number `tid`; kAhead vectors a thread on the way at once, or (0) element by
+// element in a loop of few registers, for what rows in earnest do not reach.
 constexpr int kRowAhead = 4;
-template <typename E, typename F>
-__device__ __forceinline__ void row_each(const E *p, int lo, int hi, int tid, int count, F f) {
+template <int kAhead, typename E, typename F>
+__device__ __forceinline__ void row_each(const E *p, int n, int tid, int count, F f) {
     using V = RowVec<E>;
-    const int nv = (hi - lo) / V::n;
-    p += lo;
-    for (int v0 = tid; v0 < nv; v0 += kRowAhead * count) {
-        typename V::type r[kRowAhead] = {};
+    if constexpr (kAhead == 0) {
+#pragma unroll 1
+        for (int i = tid; i < n; i += count) f(i, widen1(p[i]));
+    } else {
+        const int nv = n / V::n;
+#pragma unroll 1
+        for (int v0 = tid; v0 < nv; v0 += kAhead * count) {
+            typename V::type r[kAhead] = {};
 #pragma unroll
-        for (int a = 0; a < kRowAhead; ++a)
-            if (v0 + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v0 + a * count) * V::n);
+            for (int a = 0; a < kAhead; ++a)
+                if (v0 + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v0 + a * count) * V::n);
 #pragma unroll
-        for (int a = 0; a < kRowAhead; ++a) {
-            if (v0 + a * count >= nv) break;
+            for (int a = 0; a < kAhead; ++a) {
+                if (v0 + a * count >= nv) break;
 #pragma unroll
-            for (int k = 0; k < V::n; ++k)
-                f(lo + (v0 + a * count) * V::n + k, widen1(static_cast<E>(r[a][k])));
+                for (int k = 0; k < V::n; ++k)
+                    f((v0 + a * count) * V::n + k, widen1(static_cast<E>(r[a][k])));
+            }
         }
+        for (int i = nv * V::n + tid; i < n; i += count) f(i, widen1(p[i]));
     }
-    for (int i = nv * V::n + tid; i < hi - lo; i += count) f(lo + i, widen1(p[i]));
 }
 
 // As row_each over [0, n), f(group, index, score): the entries of a thread fall into
@@ -116,9 +121,9 @@ template <int T, typename F> __device__ u64 block_fold(u64 v, u64 *red, F f) {
     __syncthreads();
     if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
     __syncthreads();
-    v = red[0];
+    v = red[threadIdx.x % (T / kWave)];
 #pragma unroll
-    for (int k = 1; k < T / kWave; ++k) v = f(v, red[k]);
+    for (int o = T / kWave / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
     return v;
 }
 template <int T> __device__ u64 block_max(u64 v, u64 *red) {
@@ -142,15 +147,18 @@ template <int T> __device__ u64 block_before(u64 v, u64 *red, u64 *total) {
     __syncthreads();
     if (lane == kWave - 1) red[threadIdx.x / kWave] = s;
     __syncthreads();
-    u64 base = 0, all = 0;
+    // every wave forms the sums over the waves for itself
+    constexpr int waves = T / kWave;
+    u64 x = red[lane % waves];
 #pragma unroll
-    for (int k = 0; k < T / kWave; ++k) {
-        const u64 x = red[k];
-        if (k < static_cast<int>(threadIdx.x / kWave)) base += x;
-        all += x;
+    for (int o = 1; o < waves; o <<= 1) {
+        const u64 up = __shfl_up(x, o);
+        if (lane % waves >= o) x += up;
     }
-    *total = all;
-    return base + s - v;
+    *total = __shfl(x, waves - 1);
+    const int wave = threadIdx.x / kWave;
+    const u64 base = __shfl(x, wave > 0 ? wave - 1 : 0);
+    return (wave > 0 ? base : 0) + s - v;
 }
 
 // A sum of exponentials e^(scale y): the largest y, and the sum relative to it.
@@ -175,13 +183,11 @@ template <int T> __device__ ExpSum block_exp_sum(ExpSum v, float c2, u64 *red) {
     if (threadIdx.x % kWave == 0)
         red[threadIdx.x / kWave] = (static_cast<u64>(__float_as_uint(v.m)) << 32) | __float_as_uint(v.s);
     __syncthreads();
-    v = ExpSum{-INFINITY, 0.f};
+    const u64 x = red[threadIdx.x % (T / kWave)];
+    v = ExpSum{__uint_as_float(static_cast<u32>(x >> 32)), __uint_as_float(static_cast<u32>(x))};
 #pragma unroll
-    for (int k = 0; k < T / kWave; ++k) {
-        const u64 x = red[k];
-        v = exp_join(v, ExpSum{__uint_as_float(static_cast<u32>(x >> 32)), __uint_as_float(static_cast<u32>(x))},
-                     c2);
-    }
+    for (int o = T / kWave / 2; o > 0; o >>= 1)
+        v = exp_join(v, ExpSum{__shfl_xor(v.m, o), __shfl_xor(v.s, o)}, c2);
     return v;
 }
 

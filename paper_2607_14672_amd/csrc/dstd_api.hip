@@ -1420,23 +1420,15 @@ dstd_status check_sample(const dstd_sample_params *p) {
 
 extern "C" {
 
-size_t dstd_top_logits_workspace_size(const dstd_scores *s, int64_t K) {
-    if (check_scores(s) != DSTD_OK || check_top(K, s->N) != DSTD_OK) return 0;
-    return kAlign;
-}
-
 dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float *logit, float *rest,
-                            void *ws, size_t ws_bytes, void *stream) {
+                            void *stream) {
     dstd_status st = check_scores(s);
     if (st != DSTD_OK) return st;
     if ((st = check_top(K, s->N)) != DSTD_OK) return st;
     if (s->B > 0 && (!s->x || !idx || !logit)) return fail(DSTD_ERR_NULL, "x, idx and logit are required");
-    const size_t need = dstd_top_logits_workspace_size(s, K);
-    if ((st = check_ws(ws, ws_bytes, need)) != DSTD_OK) return st;
     const size_t bk = (size_t)(s->B * K) * 4;
     if ((st = check_places({scores_place(s), Place{idx, bk, 4, true, "idx"}, Place{logit, bk, 4, true, "logit"},
-                            Place{rest, (size_t)s->B * 4, 4, true, "rest"},
-                            Place{ws, need, kAlign, true, "the workspace"}})) != DSTD_OK)
+                            Place{rest, (size_t)s->B * 4, 4, true, "rest"}})) != DSTD_OK)
         return st;
     const dstd::TopJob j{score_rows(s), (int)K, idx, logit, rest};
     return hip_status(dstd::launch_top_logits(j, static_cast<hipStream_t>(stream)), "top_logits launch");
@@ -1495,23 +1487,15 @@ dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_ou
                       "distill launch");
 }
 
-size_t dstd_sample_workspace_size(const dstd_scores *s, const dstd_sample_params *p) {
-    if (check_scores(s) != DSTD_OK || check_sample(p) != DSTD_OK) return 0;
-    return kAlign;
-}
-
 dstd_status dstd_sample(const dstd_scores *s, const dstd_sample_params *p, const float *u, int32_t *choice,
-                        float *logp, void *ws, size_t ws_bytes, void *stream) {
+                        float *logp, void *stream) {
     dstd_status st = check_scores(s);
     if (st != DSTD_OK) return st;
     if ((st = check_sample(p)) != DSTD_OK) return st;
     if (s->B > 0 && (!s->x || !u || !choice)) return fail(DSTD_ERR_NULL, "x, u and choice are required");
-    const size_t need = dstd_sample_workspace_size(s, p);
-    if ((st = check_ws(ws, ws_bytes, need)) != DSTD_OK) return st;
     const size_t b4 = (size_t)s->B * 4;
     if ((st = check_places({scores_place(s), Place{u, b4, 4, false, "u"}, Place{choice, b4, 4, true, "choice"},
-                            Place{logp, b4, 4, true, "logp"},
-                            Place{ws, need, kAlign, true, "the workspace"}})) != DSTD_OK)
+                            Place{logp, b4, 4, true, "logp"}})) != DSTD_OK)
         return st;
     dstd::SampleJob j{};
     j.in = score_rows(s);

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kKdThreads) void distill_rest_kernel(KdArgs a, cons
     const float *row = a.t + b * a.ld_t + lo;
     mark(bits, lo, count, a.idx + b * a.K, logit + b * a.K, a.K, a.N);
     ExpSum s{-INFINITY, 0.f};
-    row_each<float>(row, 0, count, threadIdx.x, kKdThreads, [&](int i, float x) {
+    row_each<kRowAhead>(row, count, threadIdx.x, kKdThreads, [&](int i, float x) {
         if (marked(bits, i)) return;
         const float y = -(isfinite(x) ? x : a.t_cap);
         if (y > s.m) {
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kKdThreads) void distill_grad_kernel(KdArgs a, cons
     const float qr = r.s * exp_of(r.m - z.m, a.c2) * one_z;
     const float other = r.s > 0.f ? (qr - pr) / r.s : 0.f;
     __syncthreads();
-    row_each<float>(row + lo, 0, count, threadIdx.x, kKdThreads, [&](int i, float x) {
+    row_each<kRowAhead>(row + lo, count, threadIdx.x, kKdThreads, [&](int i, float x) {
         float g = 0.f;
         if (isfinite(x) && any) {
             if (!marked(bits, i)) {

@@ -93,12 +93,12 @@ template <int T> __device__ void sort_list(RowShared<T> &sh, int n) {
 
 // Entries of a row that `want` (key, index) holds for, into the list, as many as
 // fit; returns how many there are.
-template <int T, typename E, typename F>
+template <int T, int kAhead, typename E, typename F>
 __device__ int collect(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, F want) {
     __syncthreads();
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
-    row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float x) {
+    row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
         const u32 key = key_of(goodness(x, m));
         if (key > kAbsentKey && want(key, i)) {
             const int at = atomicAdd(&sh.count, 1);
@@ -112,7 +112,7 @@ __device__ int collect(RowShared<T> &sh, const E *row, int n, const ScoreMap &m,
 // First index where the sum of weight(key, index) up to it exceeds share times
 // the whole sum (returned in *all), -1 where that is 0. The waves sum a part of
 // the row each; the part that holds the place is read again.
-template <int T, typename E, typename F>
+template <int T, int kAhead, typename E, typename F>
 __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, double share, u64 *all,
                         F weight) {
     constexpr int waves = T / kWave, unit = kWave * RowVec<E>::n;
@@ -120,7 +120,7 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m
     const int part = (n + waves * unit - 1) / (waves * unit) * unit;
     const int lo = min(n, wave * part), hi = min(n, lo + part);
     u64 s = 0;
-    row_each<E>(row + lo, 0, hi - lo, lane, kWave,
+    row_each<kAhead>(row + lo, hi - lo, lane, kWave,
                 [&](int i, float x) { s += weight(key_of(goodness(x, m)), lo + i); });
     u64 total;
     u64 before = block_before<T>(s, sh.red, &total);
@@ -167,7 +167,7 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m
 // finds a smaller bin, down to a single key; entries of one key go by index.
 // ymin, ymax: the range of the finite values of the row; span: how far below ymax
 // weights are not 0. The largest weight is not 0.
-template <int T, typename E, typename W>
+template <int T, int kAhead, typename E, typename W>
 __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, Border kept, float ymin,
                            float ymax, double span, W weight, u64 target_n, double share) {
     u32 lo = 0, hi = 0;   // keys of the bin
@@ -187,7 +187,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
             __syncthreads();
             for (int k = threadIdx.x; k < kBins; k += T) sh.hist[k] = 0;
             __syncthreads();
-            row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float x) {
+            row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
                 const u32 key = key_of(goodness(x, m));
                 if (!in_range(key, i)) return;
                 const u64 w = weight(key);
@@ -214,12 +214,12 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
             __syncthreads();
             base = sh.found[0];
             bin = static_cast<int>(sh.found[1]);
-            const int count = collect<T>(sh, row, n, m, [&](u32 key, int i) {
+            const int count = collect<T, kAhead>(sh, row, n, m, [&](u32 key, int i) {
                 return in_range(key, i) && bin_of(key) == bin;
             });
             if (count > kList<T>) {
                 u32 a = 0xffffffffu, b = 0;
-                row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float x) {
+                row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
                     const u32 key = key_of(goodness(x, m));
                     if (in_range(key, i) && bin_of(key) == bin) {
                         a = min(a, key);
@@ -238,7 +238,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                     u64 all_ties;
                     const u32 tie = lo;
                     auto is_tie = [&](u32 key, int i) -> u64 { return key == tie && kept.has(key, i); };
-                    const int i = by_index<T>(sh, row, n, m, (static_cast<double>(k) + 0.5) / count, &all_ties, is_tie);
+                    const int i = by_index<T, kAhead>(sh, row, n, m, (static_cast<double>(k) + 0.5) / count, &all_ties, is_tie);
                     return Border{rank_of(lo, i)};
                 }
                 shift = 0;
@@ -246,7 +246,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                 continue;
             }
         } else {
-            collect<T>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+            collect<T, kAhead>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
         }
         // the list in order, and the sums of its weights
         const int count = sh.count;
@@ -281,10 +281,10 @@ struct Extremes {
     float ymin, ymax;
     int count;
 };
-template <int T, typename E>
+template <int T, int kAhead, typename E>
 __device__ Extremes row_extremes(RowShared<T> &sh, const E *row, int n, const ScoreMap &m) {
     u32 a = 0xffffffffu, b = 0, c = 0;
-    row_each<E>(row, 0, n, threadIdx.x, T, [&](int, float x) {
+    row_each<kAhead>(row, n, threadIdx.x, T, [&](int, float x) {
         const u32 key = key_of(goodness(x, m));
         if (key > kAbsentKey) {
             a = min(a, key);
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(T) void sample_kernel(int n, int64_t ld, const E *_
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
     const E *row = x + b * ld;
-    const Extremes ex = row_extremes<T>(sh, row, n, m);
+    const Extremes ex = row_extremes<T, kRowAhead>(sh, row, n, m);
     if (ex.count == 0) {
         if (threadIdx.x == 0) {
             choice[b] = -1;
@@ -316,14 +316,14 @@ __global__ __launch_bounds__(T) void sample_kernel(int n, int64_t ld, const E *_
     const Mass mass{ex.ymax, scale, ldexp(1.0, shift)};
     Border kept{0};
     if (top_k > 0 && top_k < ex.count)
-        kept = by_order<T>(sh, row, n, m, kept, ex.ymin, ex.ymax, INFINITY, One{}, top_k, 0.0);
+        kept = by_order<T, kRowAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax, INFINITY, One{}, top_k, 0.0);
     if (top_p < 1.0)
-        kept = by_order<T>(sh, row, n, m, kept, ex.ymin, ex.ymax, 0.6931471805599453 * (shift + 1) / scale, mass,
+        kept = by_order<T, kRowAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax, 0.6931471805599453 * (shift + 1) / scale, mass,
                            0, top_p);
     // u outside [0, 1) is drawn in, NaN to 0
     const double share = fmin(fmax(static_cast<double>(u[b]), 0.0), 1.0 - 0x1p-24);
     u64 all;
-    const int i = by_index<T>(sh, row, n, m, share, &all, [&](u32 key, int k) -> u64 {
+    const int i = by_index<T, kRowAhead>(sh, row, n, m, share, &all, [&](u32 key, int k) -> u64 {
         if (!kept.has(key, k)) return 0;
         if (min_p > 0.0 && !(exp(-mass.distance(key)) >= min_p)) return 0;
         return mass(key);
@@ -416,7 +416,7 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     float sum = 0.f;  // of what is below the bound, relative to it
-    row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float x) {
+    row_each<kRowAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
         const float y = caps ? goodness(x, m) : __uint_as_float(__float_as_uint(x) ^ m.flip);
         const float d = y - bound;
         if (d >= 0.f && y < INFINITY) {
@@ -429,9 +429,9 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     int count = sh.count;
     bool listed = bound == -FLT_MAX;  // the sum is that of the list's others alone
     if (count > kList<T>) {
-        const Extremes ex = row_extremes<T>(sh, row, n, m);
-        const Border kept = by_order<T>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
-        count = collect<T>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+        const Extremes ex = row_extremes<T, 0>(sh, row, n, m);
+        const Border kept = by_order<T, 0>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
+        count = collect<T, 0>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
         sum = 0.f;
         listed = false;
     }
@@ -446,7 +446,7 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     } else {
         // all others far below the bound (their sum there is 0), or no bound was found
         const u64 last = sh.list[K - 1];
-        row_each<E>(row, 0, n, threadIdx.x, T, [&](int i, float v) {
+        row_each<0>(row, n, threadIdx.x, T, [&](int i, float v) {
             const float y = goodness(v, m);
             const u32 key = key_of(y);
             if (key > kAbsentKey && rank_of(key, i) < last) {
@@ -463,7 +463,7 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
 }
 
 template <int T, typename E>
-__global__ __launch_bounds__(T) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
                                                        bool caps, double scale, float c2, int K,
                                                        int32_t *__restrict__ idx, float *__restrict__ logit,
                                                        float *__restrict__ rest) {
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(T) void top_logits_kernel(int n, int64_t ld, const 
 
 // One class from the top_k <= kMaxPicked first entries of each row.
 template <int T, typename E>
-__global__ __launch_bounds__(T) void sample_picked_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
                                                           bool caps, double scale, int shift, int top_k,
                                                           double top_p, double min_p, const float *__restrict__ u,
                                                           int32_t *__restrict__ choice, float *__restrict__ logp) {

@@ -124,13 +124,11 @@ _SIGS = {
     "dstd_skip_delay_concat_backward": (_I, [_L, _L, _L, _L, _P, _P, C.c_int32, _P, _P]),
     "dstd_softmax_ce_grad": (_I, [_L, _L, _P, _P, _F, _F, _P, _P, _P]),
     "dstd_mse_grad": (_I, [_L, _L, _P, _P, _P, _P, _P]),
-    "dstd_top_logits_workspace_size": (_S, [_P, _L]),
-    "dstd_top_logits": (_I, [_P, _L, _P, _P, _P, _P, _S, _P]),
+    "dstd_top_logits": (_I, [_P, _L, _P, _P, _P, _P]),
     "dstd_distill_workspace_size": (_S, [_L, _L, _L]),
     "dstd_distill_grad": (_I, [_L, _L, _L, _P, _L, _P, _P, _I, _P, _F, _F, _F, C.c_int32, _P, _L, _P,
                                _P, _S, _P]),
-    "dstd_sample_workspace_size": (_S, [_P, _P]),
-    "dstd_sample": (_I, [_P, _P, _P, _P, _P, _P, _S, _P]),
+    "dstd_sample": (_I, [_P, _P, _P, _P, _P, _P]),
     "dstd_tensor_list_size": (_S, [_L, _P]),
     "dstd_tensor_list_build": (_I, [_L, _P, _P, _S, _P, _P]),
     "dstd_tensor_list_workspace_size": (_S, [_P]),
@@ -297,12 +295,8 @@ def dstd_mse_grad(B, N, t_out, target, grad_t, loss, stream):
     return _load().dstd_mse_grad(B, N, t_out, target, grad_t, loss, stream)
 
 
-def dstd_top_logits_workspace_size(s, K):
-    return _load().dstd_top_logits_workspace_size(_ref(s), K)
-
-
-def dstd_top_logits(s, K, idx, logit, rest, ws, ws_bytes, stream):
-    return _load().dstd_top_logits(_ref(s), K, idx, logit, rest, ws, ws_bytes, stream)
+def dstd_top_logits(s, K, idx, logit, rest, stream):
+    return _load().dstd_top_logits(_ref(s), K, idx, logit, rest, stream)
 
 
 def dstd_distill_workspace_size(B, N, K):
@@ -316,12 +310,8 @@ def dstd_distill_grad(B, N, K, t_out, ld_t, idx, logit, logit_dtype, rest, tau_s
                                      stream)
 
 
-def dstd_sample_workspace_size(s, p):
-    return _load().dstd_sample_workspace_size(_ref(s), _ref(p))
-
-
-def dstd_sample(s, p, u, choice, logp, ws, ws_bytes, stream):
-    return _load().dstd_sample(_ref(s), _ref(p), u, choice, logp, ws, ws_bytes, stream)
+def dstd_sample(s, p, u, choice, logp, stream):
+    return _load().dstd_sample(_ref(s), _ref(p), u, choice, logp, stream)
 
 
 def dstd_tensor_list_size(n_tensors, tensors):
@@ -776,10 +766,14 @@ def mse_grad(t_out, target):
     return grad, loss
 
 
+def _whole_rows(x):
+    """Whether the rows of a matrix lie whole in memory, one behind the other."""
+    return (x.shape[1] <= 1 or x.stride(1) == 1) and (x.shape[0] <= 1 or x.stride(0) >= x.shape[1])
+
+
 def _rows(x, dtypes, what):
-    """A matrix on the GPU whose rows lie whole in memory, copied only if they do not."""
-    torch = _torch()
-    if not isinstance(x, torch.Tensor):
+    """A matrix on the GPU, copied only if its rows do not lie whole in memory."""
+    if not isinstance(x, _torch().Tensor):
         raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
     if x.dtype not in dtypes:
         raise TypeError(f"{what} must be one of {list(dtypes)}, got {x.dtype}")
@@ -787,9 +781,7 @@ def _rows(x, dtypes, what):
         raise ValueError(f"{what} must live on the GPU")
     if x.dim() != 2:
         raise ValueError(f"{what} must have two dimensions, got {x.dim()}")
-    if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
-        x = x.contiguous()
-    return x
+    return x if x.is_contiguous() or _whole_rows(x) else x.contiguous()
 
 
 def _ld(x):
@@ -800,49 +792,45 @@ def _ld(x):
 def _given(x, shape, dtype, dev, what, rows=False):
     """A tensor that the caller hands in or wants written, checked: contiguous, or
     with `rows` of whole rows."""
-    torch = _torch()
-    if not isinstance(x, torch.Tensor):
+    if not isinstance(x, _torch().Tensor):
         raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
     if x.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, got {x.dtype}")
     if x.device != dev:
         raise ValueError(f"{what} must be on {dev}")
-    if x.shape != torch.Size(shape):
+    if x.shape != shape:
         raise ValueError(f"{what} has shape {tuple(x.shape)}, not {tuple(shape)}")
-    if rows:
-        if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
-            raise ValueError(f"{what} must have rows that lie whole in memory, one behind the other")
-    elif not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
+    if not x.is_contiguous() and not (rows and _whole_rows(x)):
+        raise ValueError(f"{what} must be contiguous" +
+                         (", or of rows that lie whole in memory, one behind the other" if rows else ""))
     return x
 
 
-def _out(x, shape, dtype, dev, what):
+def _out(torch, x, shape, dtype, dev, what):
     """The caller's tensor for an output, or a new one."""
     if x is None:
-        return _torch().empty(shape, dtype=dtype, device=dev)
+        return torch.empty(shape, dtype=dtype, device=dev)
     return _given(x, shape, dtype, dev, what)
 
 
-def _ws_for(ws, need, dev):
+def _ws_for(torch, ws, need, dev):
     """The caller's workspace if it is large enough, or a new one."""
-    torch = _torch()
     if ws is None:
-        return workspace(need, dev)
+        return torch.empty(need, dtype=torch.uint8, device=dev)
     if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8:
         raise TypeError("ws must be a uint8 tensor")
     if ws.device != dev:
         raise ValueError(f"ws must be on {dev}")
     if not ws.is_contiguous():
         raise ValueError("ws must be contiguous")
-    return ws if ws.numel() >= need else workspace(need, dev)
+    return ws if ws.numel() >= need else torch.empty(need, dtype=torch.uint8, device=dev)
 
 
-def _on(dev, name, fn, *args):
+def _on(torch, dev, name, fn, *args):
     """One call on a device (launches go to the current one) and its current stream."""
-    torch = _torch()
-    stream = torch._C._cuda_getCurrentRawStream(dev.index)
-    if torch.cuda.current_device() == dev.index:
+    at = dev.index
+    stream = torch._C._cuda_getCurrentRawStream(at)
+    if torch.cuda.current_device() == at:
         _check(name, fn(*args, stream))
     else:
         with torch.cuda.device(dev):
@@ -853,14 +841,13 @@ def make_scores(x, scale: float = 1.0, cap: Optional[float] = None) -> dstd_scor
     """Rows of scores x [B, N], f32 or bf16, as top_logits and sample read them: logits
     scale * x. Entries that are not finite count as `cap`, or are left out (None).
     It holds x's address, so x has to stay while it is used."""
-    torch = _torch()
-    code = {torch.float32: DSTD_F32, torch.bfloat16: DSTD_BF16}
-    return dstd_scores(x.data_ptr(), x.shape[0], x.shape[1], _ld(x), code[x.dtype],
-                       math.nan if cap is None else float(cap), float(scale))
+    B, N = x.shape
+    return dstd_scores(x.data_ptr(), B, N, _ld(x), DSTD_F32 if x.dtype == _torch().float32 else DSTD_BF16,
+                       math.nan if cap is None else cap, scale)
 
 
 def top_logits(x, K: int, scale: float = 1.0, cap: Optional[float] = None, idx=None, logit=None,
-               rest=None, ws=None):
+               rest=None):
     """The K largest logits of every row of scores x [B, N] (f32 or bf16; logits scale * x,
     for spike times scale = -1 / tau_soft), falling, equal ones by index. Entries that are
     not finite count as `cap`, or are left out (None). Returns (idx [B, K] int32, logit
@@ -869,14 +856,11 @@ def top_logits(x, K: int, scale: float = 1.0, cap: Optional[float] = None, idx=N
     torch = _torch()
     x = _rows(x, (torch.float32, torch.bfloat16), "x")
     dev, B = x.device, x.shape[0]
-    s = make_scores(x, scale, cap)
-    need = dstd_top_logits_workspace_size(s, K)
-    idx = _out(idx, (B, max(K, 0)), torch.int32, dev, "idx")
-    logit = _out(logit, (B, max(K, 0)), torch.float32, dev, "logit")
-    rest = _out(rest, (B,), torch.float32, dev, "rest")
-    ws = _ws_for(ws, need, dev)
-    _on(dev, "dstd_top_logits", dstd_top_logits, s, K, _ptr(idx), _ptr(logit), _ptr(rest), _ptr(ws),
-        ws.numel())
+    idx = _out(torch, idx, (B, max(K, 0)), torch.int32, dev, "idx")
+    logit = _out(torch, logit, (B, max(K, 0)), torch.float32, dev, "logit")
+    rest = _out(torch, rest, (B,), torch.float32, dev, "rest")
+    _on(torch, dev, "dstd_top_logits", dstd_top_logits, make_scores(x, scale, cap), K, idx.data_ptr(),
+        logit.data_ptr(), rest.data_ptr())
     return idx, logit, rest
 
 
@@ -897,30 +881,29 @@ def distill_grad(t_out, idx, logit, rest=None, tau_soft: float = 1.0, t_cap: Opt
     if grad is not None and not need_grad:
         raise ValueError("grad is given, but need_grad is False")
     dev, (B, N) = t_out.device, t_out.shape
-    idx = _rows(idx, (torch.int32,), "idx").contiguous()
-    logit = _rows(logit, (torch.float32, torch.bfloat16), "logit").contiguous()
-    K = idx.shape[1]
+    bf16 = getattr(logit, "dtype", None) == torch.bfloat16
+    K = idx.shape[1] if getattr(idx, "ndim", 0) == 2 else 0
     _given(idx, (B, K), torch.int32, dev, "idx")
-    _given(logit, (B, K), logit.dtype, dev, "logit")
+    _given(logit, (B, K), torch.bfloat16 if bf16 else torch.float32, dev, "logit")
     if rest is not None:
         _given(rest, (B,), torch.float32, dev, "rest")
-    if need_grad:
-        grad = (torch.empty((B, N), dtype=torch.float32, device=dev) if grad is None else
-                _given(grad, (B, N), torch.float32, dev, "grad", rows=True))
-    loss = _out(loss, (B + 1,), torch.float32, dev, "loss")
+    if grad is not None:
+        _given(grad, (B, N), torch.float32, dev, "grad", rows=True)
+    elif need_grad:
+        grad = torch.empty((B, N), dtype=torch.float32, device=dev)
+    loss = _out(torch, loss, (B + 1,), torch.float32, dev, "loss")
     if weight is None:
         weight = 1.0 / max(B, 1)
-    need = dstd_distill_workspace_size(B, N, K)
-    ws = _ws_for(ws, need, dev)
-    _on(dev, "dstd_distill_grad", dstd_distill_grad, B, N, K, _ptr(t_out), _ld(t_out), _ptr(idx),
-        _ptr(logit), DSTD_F32 if logit.dtype == torch.float32 else DSTD_BF16, _ptr(rest),
-        float(tau_soft), float(t_cap), float(weight), 1 if accumulate else 0, _ptr(grad),
-        _ld(grad) if need_grad else 0, _ptr(loss), _ptr(ws), ws.numel())
+    ws = _ws_for(torch, ws, dstd_distill_workspace_size(B, N, K), dev)
+    _on(torch, dev, "dstd_distill_grad", dstd_distill_grad, B, N, K, t_out.data_ptr(), _ld(t_out),
+        idx.data_ptr(), logit.data_ptr(), DSTD_BF16 if bf16 else DSTD_F32, _ptr(rest), tau_soft, t_cap,
+        weight, 1 if accumulate else 0, _ptr(grad), _ld(grad) if need_grad else 0, loss.data_ptr(),
+        ws.data_ptr(), ws.numel())
     return grad, loss
 
 
 def sample(x, u, scale: float = 1.0, cap: Optional[float] = None, top_k: int = 0, top_p: float = 1.0,
-           min_p: float = 0.0, choice=None, logp=None, ws=None):
+           min_p: float = 0.0, choice=None, logp=None):
     """One class for every row of scores x [B, N] (as in top_logits), drawn from its
     softmax by the random numbers u [B] f32 in [0, 1): of the top_k largest logits (0:
     all) the shortest run of probability top_p or more, and of these those with at least
@@ -930,13 +913,11 @@ def sample(x, u, scale: float = 1.0, cap: Optional[float] = None, top_k: int = 0
     x = _rows(x, (torch.float32, torch.bfloat16), "x")
     dev, B = x.device, x.shape[0]
     _given(u, (B,), torch.float32, dev, "u")
-    s = make_scores(x, scale, cap)
-    p = dstd_sample_params(int(top_k), float(top_p), float(min_p))
-    need = dstd_sample_workspace_size(s, p)
-    choice = _out(choice, (B,), torch.int32, dev, "choice")
-    logp = _out(logp, (B,), torch.float32, dev, "logp")
-    ws = _ws_for(ws, need, dev)
-    _on(dev, "dstd_sample", dstd_sample, s, p, _ptr(u), _ptr(choice), _ptr(logp), _ptr(ws), ws.numel())
+    choice = _out(torch, choice, (B,), torch.int32, dev, "choice")
+    logp = _out(torch, logp, (B,), torch.float32, dev, "logp")
+    _on(torch, dev, "dstd_sample", dstd_sample, make_scores(x, scale, cap),
+        dstd_sample_params(int(top_k), float(top_p), float(min_p)), u.data_ptr(), choice.data_ptr(),
+        logp.data_ptr())
     return choice, logp
 
 

@@ -26,13 +26,12 @@ def _s(**kw):
     return dstd.dstd_scores(*(f[k] for k in ("x", "B", "N", "ld", "dtype", "cap", "scale")))
 
 
-def _top(s, K=5, idx=IDX, logit=LOGIT, rest=REST, ws=WSP, size=BIG):
-    return dstd.dstd_top_logits(s, K, idx, logit, rest, ws, size, None)
+def _top(s, K=5, idx=IDX, logit=LOGIT, rest=REST):
+    return dstd.dstd_top_logits(s, K, idx, logit, rest, None)
 
 
-def _sample(s, top_k=0, top_p=1.0, min_p=0.0, u=U, choice=IDX, logp=LOGIT, ws=WSP, size=BIG):
-    return dstd.dstd_sample(s, dstd.dstd_sample_params(top_k, top_p, min_p), u, choice, logp, ws,
-                            size, None)
+def _sample(s, top_k=0, top_p=1.0, min_p=0.0, u=U, choice=IDX, logp=LOGIT):
+    return dstd.dstd_sample(s, dstd.dstd_sample_params(top_k, top_p, min_p), u, choice, logp, None)
 
 
 SCORES = [(dict(B=-1), SHAPE), (dict(B=65536), SHAPE), (dict(N=0), SHAPE), (dict(N=1 << 24), SHAPE),
@@ -46,9 +45,6 @@ SCORES = [(dict(B=-1), SHAPE), (dict(B=65536), SHAPE), (dict(N=0), SHAPE), (dict
 def test_scores_are_checked(kw, status):
     assert _top(_s(**kw)) == status, dstd.dstd_last_error()
     assert _sample(_s(**kw)) == status, dstd.dstd_last_error()
-    if "x" not in kw:  # the sizes do not go by addresses
-        assert dstd.dstd_top_logits_workspace_size(_s(**kw), 5) == 0
-        assert dstd.dstd_sample_workspace_size(_s(**kw), dstd.dstd_sample_params(0, 1.0, 0.0)) == 0
 
 
 def test_top_logits_arguments():
@@ -59,41 +55,27 @@ def test_top_logits_arguments():
     assert _top(_s(N=1000, ld=1000), K=dstd.DSTD_MAX_TOP + 1) == UNSUP
     assert _top(_s(), idx=None) == NULL
     assert _top(_s(), logit=None) == NULL
-    assert _top(_s(), ws=None) == NULL
-    assert _top(_s(), ws=WSP + 128) == WS
-    need = dstd.dstd_top_logits_workspace_size(_s(), 5)
-    assert need > 0 and _top(_s(), size=need - 1) == WS
     assert _top(_s(), idx=IDX + 2) == PARAM
-    # overlaps: outputs with the scores (their last row too), each other, the workspace
+    # overlaps: outputs with the scores (their last row too) and each other
     assert _top(_s(), idx=X + 4 * 399) == PARAM
     assert _top(_s(ld=1000), rest=X + 4 * 3099) == PARAM
     assert _top(_s(), logit=IDX + 4 * 19) == PARAM
     assert _top(_s(), rest=LOGIT) == PARAM
-    assert _top(_s(), rest=WSP) == PARAM
-    assert _top(_s(), ws=X) == PARAM
 
 
 def test_sample_arguments():
     p = dstd.dstd_sample_params(0, 1.0, 0.0)
-    assert dstd.dstd_sample(_s(), None, U, IDX, LOGIT, WSP, BIG, None) == NULL
-    assert dstd.dstd_sample(None, p, U, IDX, LOGIT, WSP, BIG, None) == NULL
+    assert dstd.dstd_sample(_s(), None, U, IDX, LOGIT, None) == NULL
+    assert dstd.dstd_sample(None, p, U, IDX, LOGIT, None) == NULL
     for bad in (dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.0000001), dict(top_p=-0.5),
                 dict(top_p=math.nan), dict(min_p=-1e-9), dict(min_p=1.1), dict(min_p=math.nan)):
         assert _sample(_s(), **bad) == PARAM, bad
-        full = dict(top_k=0, top_p=1.0, min_p=0.0)
-        full.update(bad)
-        assert dstd.dstd_sample_workspace_size(_s(), dstd.dstd_sample_params(*full.values())) == 0
     assert _sample(_s(), u=None) == NULL
     assert _sample(_s(), choice=None) == NULL
-    assert _sample(_s(), ws=None) == NULL
-    assert _sample(_s(), ws=WSP + 4) == WS
-    need = dstd.dstd_sample_workspace_size(_s(), p)
-    assert need > 0 and _sample(_s(), size=need - 1) == WS
     assert _sample(_s(), choice=U) == PARAM
     assert _sample(_s(), logp=U + 12) == PARAM
     assert _sample(_s(), choice=X) == PARAM
     assert _sample(_s(), choice=IDX, logp=IDX) == PARAM
-    assert _sample(_s(), u=WSP) == PARAM
 
 
 def _distill(B=4, N=100, K=5, t=X, ld_t=None, idx=IDX, logit=LOGIT, dtype=dstd.DSTD_F32, rest=REST, tau=0.1,
