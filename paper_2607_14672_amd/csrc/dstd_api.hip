@@ -1501,7 +1501,7 @@ dstd_status dstd_sample(const dstd_scores *s, const dstd_sample_params *p, const
     j.in = score_rows(s);
     int bits = 0;  // ceil(log2 N)
     while (((int64_t)1 << bits) < s->N) ++bits;
-    j.shift = std::min(52, 62 - bits);
+    j.shift = std::min(51, 62 - bits);
     j.top_k = (int)std::min<int64_t>(p->top_k, s->N);
     j.top_p = p->top_p;
     j.min_p = p->min_p;

@@ -10,6 +10,7 @@
 //
 // Both order by the score itself, not by its product with the scale.
 #include <float.h>
+#include <string.h>
 
 #include "dstd_answer.h"
 #include "dstd_kernels.h"
@@ -40,17 +41,39 @@ struct Border {
     __device__ bool has(u32 key, int i) const { return key > kAbsentKey && rank_of(key, i) >= last; }
 };
 
-// Weights of the exponentials in 64-bit integers, the largest 2^shift: their sums
-// do not depend on the order, and what is lost of a weight, 2^-(shift+1) of the
-// largest, is below what sums in 64-bit floats lose over long rows.
+// Weights of the exponentials in 64-bit integers, the largest 2^shift (shift <= 51):
+// their sums do not depend on the order, and what is lost of a weight, 2^-(shift+1) of
+// the largest, is below what sums in 64-bit floats lose over long rows.
 struct Mass {
     double top, scale;  // the largest goodness; |scale|
-    double one;         // 2^shift
-    __device__ double distance(u32 key) const { return (top - static_cast<double>(value_of(key))) * scale; }
-    __device__ u64 operator()(u32 key) const {
-        const double d = distance(key);
-        return d < 64.0 ? static_cast<u64>(rint(exp(-d) * one)) : 0;
+    int shift;
+    __device__ double distance(float y) const { return (top - static_cast<double>(y)) * scale; }
+    __device__ double distance(u32 key) const { return distance(value_of(key)); }
+    // rint(e^-d 2^shift): d = n ln 2 + r, e^-r by its series to r^12 / 12! (|r| <= ln 2 / 2:
+    // 2^-52 relative). Adding 2^52 leaves the integer in the low bits.
+    static __device__ __forceinline__ u64 fixed_exp(double d, int shift) {
+        const double big = 0x1.8p52;
+        const double t = fma(fmin(d, 128.0), 1.4426950408889634, big);
+        const double n = t - big;
+        const double r = fma(n, -0x1.abc9e3b39803fp-56, fma(n, -0x1.62e42fefa39efp-1, fmin(d, 128.0)));
+        double p = 1.0 / 479001600;
+        p = fma(p, -r, 1.0 / 39916800);
+        p = fma(p, -r, 1.0 / 3628800);
+        p = fma(p, -r, 1.0 / 362880);
+        p = fma(p, -r, 1.0 / 40320);
+        p = fma(p, -r, 1.0 / 5040);
+        p = fma(p, -r, 1.0 / 720);
+        p = fma(p, -r, 1.0 / 120);
+        p = fma(p, -r, 1.0 / 24);
+        p = fma(p, -r, 1.0 / 6);
+        p = fma(p, -r, 0.5);
+        p = fma(p, -r, 1.0);
+        p = fma(p, -r, 1.0);
+        const double v = ldexp(p, shift - static_cast<int>(__double2loint(t))) + 0x1p52;
+        return __double_as_longlong(v) & 0xfffffffffffffull;
     }
+    __device__ u64 of(float y) const { return fixed_exp(distance(y), shift); }
+    __device__ u64 operator()(u32 key) const { return fixed_exp(distance(key), shift); }
 };
 struct One {
     __device__ u64 operator()(u32) const { return 1; }
@@ -297,44 +320,54 @@ __device__ Extremes row_extremes(RowShared<T> &sh, const E *row, int n, const Sc
     return Extremes{value_of(lo), value_of(hi), count};
 }
 
-template <int T, typename E>
-__global__ __launch_bounds__(T) void sample_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
-                                                   double scale, int shift, int top_k, double top_p,
-                                                   double min_p, const float *__restrict__ u,
-                                                   int32_t *__restrict__ choice, float *__restrict__ logp) {
-    __shared__ RowShared<T> sh;
-    const int64_t b = blockIdx.x;
-    const E *row = x + b * ld;
-    const Extremes ex = row_extremes<T, kRowAhead>(sh, row, n, m);
+// What a draw goes by, and where it is written.
+struct DrawArgs {
+    double scale, top_p, dmax;  // dmax: -ln min_p, the largest distance that is kept
+    int shift, top_k;
+    const float *u;
+    int32_t *choice;
+    float *logp;
+};
+__device__ __forceinline__ void put_draw(const DrawArgs &a, int64_t b, int i, double distance, u64 all) {
+    a.choice[b] = i;
+    if (!a.logp) return;
+    a.logp[b] = i < 0 ? -INFINITY
+                      : static_cast<float>(-distance - log(ldexp(static_cast<double>(all), -a.shift)));
+}
+// u outside [0, 1) is drawn in, NaN to 0
+__device__ __forceinline__ double share_of(const DrawArgs &a, int64_t b) {
+    return fmin(fmax(static_cast<double>(a.u[b]), 0.0), 1.0 - 0x1p-24);
+}
+
+// One class of a row by its definition, whatever the values.
+template <int T, int kAhead, typename E>
+__device__ void sample_row(RowShared<T> &sh, const E *row, int64_t b, int n, const ScoreMap &m, const DrawArgs &a) {
+    const Extremes ex = row_extremes<T, kAhead>(sh, row, n, m);
     if (ex.count == 0) {
-        if (threadIdx.x == 0) {
-            choice[b] = -1;
-            if (logp) logp[b] = -INFINITY;
-        }
+        if (threadIdx.x == 0) put_draw(a, b, -1, 0.0, 0);
         return;
     }
-    const Mass mass{ex.ymax, scale, ldexp(1.0, shift)};
+    const Mass mass{ex.ymax, a.scale, a.shift};
     Border kept{0};
-    if (top_k > 0 && top_k < ex.count)
-        kept = by_order<T, kRowAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax, INFINITY, One{}, top_k, 0.0);
-    if (top_p < 1.0)
-        kept = by_order<T, kRowAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax, 0.6931471805599453 * (shift + 1) / scale, mass,
-                           0, top_p);
-    // u outside [0, 1) is drawn in, NaN to 0
-    const double share = fmin(fmax(static_cast<double>(u[b]), 0.0), 1.0 - 0x1p-24);
+    if (a.top_k > 0 && a.top_k < ex.count)
+        kept = by_order<T, kAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax, INFINITY, One{}, a.top_k, 0.0);
+    if (a.top_p < 1.0)
+        kept = by_order<T, kAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax,
+                                   0.6931471805599453 * (a.shift + 1) / a.scale, mass, 0, a.top_p);
     u64 all;
-    const int i = by_index<T, kRowAhead>(sh, row, n, m, share, &all, [&](u32 key, int k) -> u64 {
-        if (!kept.has(key, k)) return 0;
-        if (min_p > 0.0 && !(exp(-mass.distance(key)) >= min_p)) return 0;
-        return mass(key);
+    const int i = by_index<T, kAhead>(sh, row, n, m, share_of(a, b), &all, [&](u32 key, int k) -> u64 {
+        return kept.has(key, k) && mass.distance(key) <= a.dmax ? mass(key) : 0;
     });
-    if (threadIdx.x == 0) {
-        choice[b] = i;
-        if (logp) {
-            const double d = mass.distance(key_of(goodness(widen1(row[i]), m)));
-            logp[b] = static_cast<float>(-d - log(static_cast<double>(all) / mass.one));
-        }
-    }
+    if (threadIdx.x == 0) put_draw(a, b, i, mass.distance(key_of(goodness(widen1(row[i]), m))), all);
+}
+
+template <int T, typename E>
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
+                                                                      ScoreMap m, DrawArgs a) {
+    __shared__ RowShared<T> sh;
+    const int64_t b = blockIdx.x;
+    // bf16 rows come here by a cap that no bf16 value equals, or by their size
+    sample_row<T, sizeof(E) == 4 ? 1 : 0>(sh, x + b * ld, b, n, m, a);
 }
 
 // Candidates for the K first entries of a row's order: all that reach a bound which K
@@ -485,23 +518,19 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n,
 
 // One class from the top_k <= kMaxPicked first entries of each row.
 template <int T, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
-                                                          bool caps, double scale, int shift, int top_k,
-                                                          double top_p, double min_p, const float *__restrict__ u,
-                                                          int32_t *__restrict__ choice, float *__restrict__ logp) {
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int n, int64_t ld,
+                                                                             const E *__restrict__ x, ScoreMap m,
+                                                                             bool caps, DrawArgs a) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
     const E *row = x + b * ld;
-    int count = candidates<T, false>(sh, row, n, m, caps, top_k, 0.f, nullptr);
+    int count = candidates<T, false>(sh, row, n, m, caps, a.top_k, 0.f, nullptr);
     if (count == 0) {
-        if (threadIdx.x == 0) {
-            choice[b] = -1;
-            if (logp) logp[b] = -INFINITY;
-        }
+        if (threadIdx.x == 0) put_draw(a, b, -1, 0.0, 0);
         return;
     }
-    count = min(count, top_k);
-    const Mass mass{value_of(rank_key(sh.list[0])), scale, ldexp(1.0, shift)};
+    count = min(count, a.top_k);
+    const Mass mass{value_of(rank_key(sh.list[0])), a.scale, a.shift};
     constexpr int each = kMaxPicked / T > 1 ? kMaxPicked / T : 1;
     u64 w[each], mine = 0;
     const int first = threadIdx.x * each;
@@ -512,12 +541,12 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int
     }
     u64 all;
     u64 at = block_before<T>(mine, sh.red, &all);
-    const double target = top_p < 1.0 ? top_p * static_cast<double>(all) : INFINITY;
+    const double target = a.top_p < 1.0 ? a.top_p * static_cast<double>(all) : INFINITY;
     u64 keeps = 0;
 #pragma unroll
     for (int k = 0; k < each; ++k) {
         if (first + k < count && static_cast<double>(at) < target &&
-            (min_p == 0.0 || exp(-mass.distance(rank_key(sh.list[first + k]))) >= min_p))
+            mass.distance(rank_key(sh.list[first + k])) <= a.dmax)
             ++keeps;
         at += w[k];
     }
@@ -541,38 +570,276 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int
         mine += w[k];
     }
     at = block_before<T>(mine, sh.red, &all);
-    const double share = fmin(fmax(static_cast<double>(u[b]), 0.0), 1.0 - 0x1p-24);
-    const double goal = share * static_cast<double>(all);
+    const double goal = share_of(a, b) * static_cast<double>(all);
     if (static_cast<double>(at) <= goal && static_cast<double>(at + mine) > goal)
 #pragma unroll
         for (int k = 0; k < each; ++k) {
             if (static_cast<double>(at) <= goal && static_cast<double>(at + w[k]) > goal) {
                 const u64 r = sh.list[first + k];
-                choice[b] = static_cast<int>(~static_cast<u32>(r >> 32));
-                if (logp)
-                    logp[b] = static_cast<float>(-mass.distance(static_cast<u32>(r)) -
-                                                 log(static_cast<double>(all) / mass.one));
+                put_draw(a, b, static_cast<int>(~static_cast<u32>(r >> 32)), mass.distance(static_cast<u32>(r)), all);
             }
             at += w[k];
         }
 }
 
+// ---------------------------------------------- rows of few distinct values --
+// bf16 scores of a magnitude in [2^-24, 2^8) take 2 * 4095 values, and 0; how often each
+// occurs says which are kept and what they weigh, with an exponential a value instead of
+// one an entry. Bins fall from the largest value: kHalf - t for the t-th magnitude,
+// kHalf for 0, kHalf + t for its negative, and the last for all that is smaller (of
+// weight 0, or the row is not drawn from here).
+constexpr int kHalf = 4095, kValues = 2 * kHalf + 2, kFirstMag = 0x3381;
+constexpr int kNoBin = -1, kOddBin = -2;
+struct BinMap {
+    u32 flip;  // as of ScoreMap, for 16 bits
+    u32 cap;   // bits of what an entry that is not finite counts as; 0x8000 more: left out
+};
+__device__ __forceinline__ int value_bin(u32 bits, const BinMap &m) {
+    const int t = static_cast<int>(bits & 0x7fff) - kFirstMag + 1;
+    const int neg = static_cast<int>((bits ^ m.flip) << 16) >> 31;  // 0 or -1
+    if (static_cast<u32>(t - 1) < static_cast<u32>(kHalf)) return kHalf + ((t ^ ~neg) - ~neg);
+    if ((bits & 0x7fff) >= 0x7f80) {
+        if (m.cap > 0xffff) return kNoBin;
+        const int tc = static_cast<int>(m.cap & 0x7fff) - kFirstMag + 1;
+        const int nc = static_cast<int>((m.cap ^ m.flip) << 16) >> 31;
+        return (m.cap & 0x7fff) == 0 ? kHalf : kHalf + ((tc ^ ~nc) - ~nc);
+    }
+    if ((bits & 0x7fff) == 0) return kHalf;
+    return neg && t > kHalf ? kValues - 1 : kOddBin;
+}
+__device__ __forceinline__ float bin_value(int bin) {
+    const int t = bin - kHalf;
+    if (t == 0) return 0.f;
+    const u32 mag = (t < 0 ? -t : t) + kFirstMag - 1;
+    return bf16_to_f32(static_cast<uint16_t>(mag | (t > 0 ? 0x8000u : 0u)));
+}
+
+template <int T> struct ValueShared {
+    u64 red[T / kWave + 1];
+    union {
+        RowShared<T> row;
+        u64 weight[kValues];
+        u32 count[kValues];
+    };
+    u64 part[T / kWave];
+    u32 ties[T / kWave];
+    u64 found, tie_weight;
+    int tie_bin, tie_keep, at;
+};
+
+// f(index, bits) as row_each
+template <typename F>
+__device__ __forceinline__ void bits_each(const uint16_t *p, int n, int tid, int count, F f) {
+    const int nv = n / 8;
+#pragma unroll 1
+    for (int v0 = tid; v0 < nv; v0 += 2 * count) {
+        RowVec<uint16_t>::type r[2] = {};
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+            if (v0 + a * count < nv) r[a] = load_vec<uint16_t>(p + static_cast<int64_t>(v0 + a * count) * 8);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            if (v0 + a * count >= nv) break;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f((v0 + a * count) * 8 + k, static_cast<u32>(r[a][k]));
+        }
+    }
+    for (int i = nv * 8 + tid; i < n; i += count) f(i, static_cast<u32>(p[i]));
+}
+
+template <int T>
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_values_kernel(int n, int64_t ld,
+                                                                             const uint16_t *__restrict__ x,
+                                                                             ScoreMap m, BinMap bm, DrawArgs a) {
+    __shared__ ValueShared<T> sh;
+    constexpr int each = kValues / T, waves = T / kWave;
+    static_assert(kValues % T == 0, "");
+    const int64_t b = blockIdx.x;
+    const uint16_t *row = x + b * ld;
+    const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+    for (int k = tid; k < kValues; k += T) sh.count[k] = 0;
+    __syncthreads();
+    bool odd = false;
+    bits_each(row, n, tid, T, [&](int, u32 bits) {
+        const int bin = value_bin(bits, bm);
+        if (bin >= 0) atomicAdd(&sh.count[bin], 1u);
+        odd |= bin == kOddBin;
+    });
+    odd = __syncthreads_or(odd);
+    // each thread's bins
+    u32 count[each];
+    u64 first = kValues;
+    u64 counted = 0;
+#pragma unroll
+    for (int k = each - 1; k >= 0; --k) {
+        count[k] = sh.count[tid * each + k];
+        counted += count[k];
+        if (count[k]) first = tid * each + k;
+    }
+    const u32 below = sh.count[kValues - 1];
+    first = block_min<T>(first, sh.red);
+    if (first == kValues && !odd) {
+        if (tid == 0) put_draw(a, b, -1, 0.0, 0);
+        return;
+    }
+    const Mass mass{bin_value(static_cast<int>(first)), a.scale, a.shift};
+    if (odd || (below > 0 && (first == kValues - 1 || mass.of(bin_value(kValues - 2)) != 0))) {
+        __syncthreads();
+        sample_row<T, 0>(sh.row, row, b, n, m, a);
+        return;
+    }
+    u64 unused, w[each], sum = 0;
+    u64 before = block_before<T>(counted, sh.red, &unused);
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        u64 keep = count[k];
+        if (a.top_k > 0) keep = before >= static_cast<u64>(a.top_k) ? 0 : min(keep, a.top_k - before);
+        before += count[k];
+        const int bin = tid * each + k;
+        w[k] = keep && bin < kValues - 1 ? mass.of(bin_value(bin)) : 0;
+        count[k] = static_cast<u32>(keep);
+        sum += keep * w[k];
+    }
+    u64 all;
+    u64 at = block_before<T>(sum, sh.red, &all);
+    // the counts are in registers: their place takes the weights
+    if (tid == 0) {
+        sh.tie_bin = -1;
+        sh.tie_keep = 0;
+        sh.tie_weight = 0;
+    }
+    __syncthreads();
+    u64 in_bin[each];
+#pragma unroll
+    for (int k = 0; k < each; ++k) in_bin[k] = sh.count[tid * each + k];
+    __syncthreads();
+    const double target = a.top_p < 1.0 ? a.top_p * static_cast<double>(all) : INFINITY;
+    u64 last = 0;
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        const int bin = tid * each + k;
+        u64 keep = w[k] ? count[k] : 0;
+        if (keep) {
+            if (static_cast<double>(at) >= target || mass.distance(bin_value(bin)) > a.dmax) {
+                keep = 0;
+            } else if (static_cast<double>(at + keep * w[k]) >= target) {
+                // the fewest that reach the target
+                u64 c = static_cast<u64>((target - static_cast<double>(at)) / static_cast<double>(w[k]));
+                while (c > 0 && static_cast<double>(at + (c - 1) * w[k]) >= target) --c;
+                while (static_cast<double>(at + c * w[k]) < target) ++c;
+                at += keep * w[k];
+                keep = min(keep, c);
+            } else {
+                at += keep * w[k];
+            }
+            if (keep) last = bin;
+            if (keep && keep < in_bin[k]) {
+                sh.tie_bin = bin;
+                sh.tie_keep = static_cast<int>(keep);
+                sh.tie_weight = w[k];
+                keep = 0;
+            }
+        }
+        sh.weight[bin] = keep ? w[k] : 0;
+    }
+    last = block_max<T>(last, sh.red);
+    const int tie_bin = sh.tie_bin;
+    const u64 tie_keep = sh.tie_keep, tie_weight = sh.tie_weight;
+    // the kept weights of each wave's part of the row; of the bin that is kept in part, the
+    // entries, of which the first tie_keep count
+    constexpr int unit = kWave * 8;
+    const int part = (n + waves * unit - 1) / (waves * unit) * unit;
+    const int lo = min(n, wave * part), hi = min(n, lo + part);
+    u64 s = 0, ties = 0;
+    auto add = [&](u32 bits) {
+        const int bin = value_bin(bits, bm);
+        if (static_cast<u32>(bin) <= static_cast<u32>(last)) {
+            if (bin == tie_bin) ++ties;
+            else s += sh.weight[bin];
+        }
+    };
+    bits_each(row + lo, hi - lo, lane, kWave, [&](int, u32 bits) { add(bits); });
+    auto plus = [](u64 p, u64 q) { return p + q; };
+    s = block_fold<kWave>(s, nullptr, plus);
+    ties = block_fold<kWave>(ties, nullptr, plus);
+    if (lane == 0) {
+        sh.part[wave] = s;
+        sh.ties[wave] = static_cast<u32>(ties);
+    }
+    __syncthreads();
+    u64 t = 0;
+    all = 0;
+    for (int k = 0; k < waves; ++k) {
+        all += sh.part[k] + tie_weight * min<u64>(sh.ties[k], tie_keep - min(t, tie_keep));
+        t += sh.ties[k];
+    }
+    const double goal = share_of(a, b) * static_cast<double>(all);
+    u64 base = 0;
+    t = 0;
+    int from = 0;
+    for (; from < waves - 1; ++from) {
+        const u64 next = base + sh.part[from] + tie_weight * min<u64>(sh.ties[from], tie_keep - min(t, tie_keep));
+        if (static_cast<double>(next) > goal) break;
+        base = next;
+        t += sh.ties[from];
+    }
+    // the place in that part, runs of `len` entries a thread
+    const int start = from * part, end = min(n, start + part);
+    const int len = (end - start + T - 1) / T;
+    const int p0 = min(end, start + tid * len), p1 = min(end, p0 + len);
+    s = ties = 0;
+    for (int i = p0; i < p1; ++i) add(row[i]);
+    t += block_before<T>(ties, sh.red, &unused);
+    const u64 mine = s + tie_weight * min(ties, tie_keep - min(t, tie_keep));
+    base += block_before<T>(mine, sh.red, &unused);
+    if (static_cast<double>(base) <= goal && static_cast<double>(base + mine) > goal)
+        for (int i = p0; i < p1; ++i) {
+            const int bin = value_bin(row[i], bm);
+            if (static_cast<u32>(bin) > static_cast<u32>(last)) continue;
+            if (bin == tie_bin) base += t++ < tie_keep ? tie_weight : 0;
+            else base += sh.weight[bin];
+            if (static_cast<double>(base) > goal) {
+                put_draw(a, b, i, mass.distance(bin_value(bin)), all);
+                break;
+            }
+        }
+}
+
+// Whether a cap is one of the values that have a bin, or is none.
+bool cap_has_bin(float cap, u32 *bits) {
+    *bits = 0x10000u;
+    if (!isfinite(cap)) return true;
+    u32 f;
+    memcpy(&f, &cap, 4);
+    *bits = f >> 16;
+    const int t = static_cast<int>(*bits & 0x7fff) - kFirstMag;
+    return (f & 0xffff) == 0 && ((*bits & 0x7fff) == 0 || (t >= 0 && t < kHalf));
+}
+
 template <typename E>
 hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
-    const bool caps = isfinite(j.in.cap);
-#define SAMPLE(T)                                                                                              \
-    if (j.top_k > 0 && j.top_k <= kMaxPicked)                                                                  \
-        hipLaunchKernelGGL((sample_picked_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,  \
-                           static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                  \
-                           ScoreMap{j.in.cap, j.in.flip}, caps, j.in.scale, j.shift, j.top_k, j.top_p, j.min_p, \
-                           j.u, j.choice, j.logp);                                                             \
-    else                                                                                                       \
-        hipLaunchKernelGGL((sample_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,         \
-                           static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                  \
-                           ScoreMap{j.in.cap, j.in.flip}, j.in.scale, j.shift, j.top_k, j.top_p, j.min_p, j.u, \
-                           j.choice, j.logp)
-    if (j.in.N <= 512) SAMPLE(64);
-    else if (j.in.N <= 4096) SAMPLE(256);
+    const int n = static_cast<int>(j.in.N);
+    const dim3 grid(static_cast<unsigned>(j.in.B));
+    const ScoreMap m{j.in.cap, j.in.flip};
+    const DrawArgs a{j.in.scale, j.top_p, j.min_p > 0.0 ? -log(j.min_p) : INFINITY, j.shift, j.top_k,
+                     j.u, j.choice, j.logp};
+    const E *x = static_cast<const E *>(j.in.x);
+    const bool picked = j.top_k > 0 && j.top_k <= kMaxPicked;
+    u32 cap;
+    if constexpr (sizeof(E) == 2)
+        if (!picked && n > 4096 && cap_has_bin(j.in.cap, &cap)) {
+            const BinMap bm{j.in.flip >> 16, cap};
+            hipLaunchKernelGGL((sample_values_kernel<1024>), grid, dim3(1024), 0, st, n, j.in.ld, x, m, bm, a);
+            return hipGetLastError();
+        }
+#define SAMPLE(T)                                                                                             \
+    if (picked)                                                                                               \
+        hipLaunchKernelGGL((sample_picked_kernel<T, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m,               \
+                           isfinite(j.in.cap), a);                                                            \
+    else                                                                                                      \
+        hipLaunchKernelGGL((sample_kernel<T, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a)
+    if (n <= 512) SAMPLE(64);
+    else if (n <= 4096) SAMPLE(256);
     else SAMPLE(1024);
 #undef SAMPLE
     return hipGetLastError();

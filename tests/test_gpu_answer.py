@@ -64,6 +64,9 @@ def _scores(kind, B, N, seed):
     elif kind == "signalling":  # NaN of the other kind, and +inf
         x[rng.random((B, N)) < 0.3] = np.inf
         x.view(np.uint32)[rng.random((B, N)) < 0.3] = 0x7f810000
+    elif kind == "lowest":  # masked by the lowest value of the type
+        x[rng.random((B, N)) < 0.6] = -3.3895314e38
+        x[0] = -3.3895314e38
     elif kind == "sorted":  # one thread's share holds many of the largest
         x = np.sort(x, axis=1)
     elif kind == "outlier":
@@ -72,7 +75,7 @@ def _scores(kind, B, N, seed):
     return x
 
 
-KINDS = ["plain", "masked", "ties", "equal", "zeros", "huge", "near", "sorted", "outlier", "signalling"]
+KINDS = ["plain", "masked", "ties", "equal", "zeros", "huge", "near", "sorted", "outlier", "signalling", "lowest"]
 SIZES = [1, 2, 63, 64, 65, 511, 512, 513, 1000, 4096, 4097, 20011]
 
 
@@ -261,7 +264,7 @@ def _check_sample(torch, dstd, x, dtype, scale, cap, top_k, top_p, min_p, seed=0
     w = ref.kept(v.float().cpu().numpy(), scale, cap, top_k, top_p, min_p)
     cum = np.cumsum(w, axis=1)
     # N weights to 2^-(s+1) each, and the reference's own sums
-    slack = N * (2.0 ** -(min(52, 62 - math.ceil(math.log2(N)))) + 2.0 ** -52 * 4)
+    slack = N * (2.0 ** -(min(51, 62 - math.ceil(math.log2(N)))) + 2.0 ** -52 * 4)
     for b in range(B):
         C = cum[b, -1]
         if C == 0:
@@ -289,6 +292,8 @@ def test_sample(kind, N):
         _check_sample(torch, dstd, x, torch.float32, -1.0 / 0.3, 1.5, k, p, m, n, ld=3, shift=1)
         _check_sample(torch, dstd, x, torch.float32, 0.7, None, k, p, m, n + 20)
         _check_sample(torch, dstd, x, torch.bfloat16, 1.1, None, k, p, m, n + 40, ld=1, shift=1)
+        _check_sample(torch, dstd, x, torch.bfloat16, -2.0, 1.5, k, p, m, n + 60)
+        _check_sample(torch, dstd, x, torch.bfloat16, -2.0, 0.1, k, p, m, n + 80)  # no bf16 value
 
 
 @pytest.mark.parametrize("B,N,dtype", [(1, 131072, "bf16"), (2, 131077, "f32"), (40, 50021, "f32"),
