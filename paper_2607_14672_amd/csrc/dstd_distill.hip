@@ -16,45 +16,291 @@ namespace dstd {
 
 namespace {
 
-constexpr int kKdThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kKdChunk = 8192;  // classes of a block
+constexpr int kEach = kKdMaxK / kWave;  // entries of the record a lane
 
-// Bits of the classes [lo, lo + count) that a row's record names. An entry is one
-// if its index is a class and its logit is finite.
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x4_any = f32x4 __attribute__((aligned(4)));
+
+// The entries of a row's record as one wave holds them, entry k = lane + 64 j. An
+// entry is one if its index is a class and its logit is finite.
+template <typename L> struct Entries {
+    int at[kEach];  // -1: no entry
+    float l[kEach], y[kEach];
+    bool fired[kEach];
+
+    __device__ void load(const KdArgs &a, int64_t b, const L *logit, int lane) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int k = lane + kWave * j;
+            at[j] = -1;
+            l[j] = -INFINITY;
+            if (k < a.K) {
+                const int i = a.idx[b * a.K + k];
+                l[j] = widen1(logit[b * a.K + k]);
+                if (i >= 0 && i < a.N && isfinite(l[j])) at[j] = i;
+            }
+        }
+        const float *row = a.t + b * a.ld_t;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const float x = at[j] >= 0 ? row[at[j]] : 0.f;
+            fired[j] = isfinite(x);
+            y[j] = -(fired[j] ? x : a.t_cap);
+        }
+    }
+};
+
+// What a row's gradient goes by: the teacher's logits (p, with the rest), the student's
+// over the named classes (zs), and whether the record has an entry.
+struct RecordSums {
+    ExpSum p, zs;
+    float rest;
+    int any;
+};
+
+// The sums of a record by one wave. first[j]: no earlier entry names the class.
 template <typename L>
-__device__ __forceinline__ bool named(const int32_t *idx, const L *logit, int k, int N, int *i, float *l) {
-    *i = idx[k];
-    *l = widen1(logit[k]);
-    return *i >= 0 && *i < N && isfinite(*l);
+__device__ RecordSums record_sums(const KdArgs &a, int64_t b, const Entries<L> &e, const bool (&first)[kEach]) {
+    RecordSums r;
+    r.rest = a.rest ? a.rest[b] : -INFINITY;
+    if (!isfinite(r.rest)) r.rest = -INFINITY;
+    r.p = ExpSum{r.rest, r.rest > -INFINITY && threadIdx.x % kWave == 0 ? 1.f : 0.f};
+    r.zs = ExpSum{-INFINITY, 0.f};
+    bool some = false;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (e.at[j] >= 0) {
+            some = true;
+            r.p = exp_join(r.p, ExpSum{e.l[j], 1.f}, kLog2e);
+            if (first[j]) r.zs = exp_join(r.zs, ExpSum{e.y[j], 1.f}, a.c2);
+        }
+    r.p = block_exp_sum<kWave>(r.p, kLog2e, nullptr);
+    r.zs = block_exp_sum<kWave>(r.zs, a.c2, nullptr);
+    r.any = __any(some);
+    return r;
 }
 
+// Which of the entries are the first of their class, where some class is named twice.
+template <typename L> __device__ void first_of(const int *list, int K, const Entries<L> &e, bool (&first)[kEach]) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        first[j] = e.at[j] >= 0;
+        const int k = threadIdx.x % kWave + kWave * j;
+        for (int o = 0; first[j] && o < min(k, K); ++o) first[j] = list[o] != e.at[j];
+    }
+}
+
+// Factors of a row's gradient, in z: e^((y - r.m) / tau) * other outside S, and
+// e^((y - z.m) / tau) * one_z - p in S.
+struct RowFactors {
+    ExpSum r, z;
+    float pr, one_z, other;
+    __device__ RowFactors(const RecordSums &s, ExpSum rest, float c2) : r(rest), z(exp_join(rest, s.zs, c2)) {
+        pr = s.rest > -INFINITY ? exp_of(s.rest - s.p.m, kLog2e) / s.p.s : 0.f;
+        one_z = 1.f / z.s;
+        const float qr = r.s * exp_of(r.m - z.m, c2) * one_z;
+        other = r.s > 0.f ? (qr - pr) / r.s : 0.f;
+    }
+};
+
+// The loss of a row, by one wave.
 template <typename L>
-__device__ void mark(u32 *bits, int lo, int count, const int32_t *idx, const L *logit, int K, int N) {
-    for (int k = threadIdx.x; k < (count + 31) / 32; k += kKdThreads) bits[k] = 0;
+__device__ void put_loss(const KdArgs &a, int64_t b, const Entries<L> &e, const RecordSums &s, const RowFactors &f) {
+    // ln p_k = l_k - ln sum, ln q_k = (y_k - z.m) / tau - ln z.s
+    const float logp0 = s.p.m + logf(s.p.s), lz = logf(f.z.s);
+    float term = 0.f;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        if (e.at[j] < 0) continue;
+        const float p = exp_of(e.l[j] - s.p.m, kLog2e) / s.p.s;
+        if (p > 0.f) term += p * (e.l[j] - logp0 - ((e.y[j] - f.z.m) * a.inv - lz));
+    }
+    if (threadIdx.x % kWave == 0 && f.pr > 0.f)
+        term += f.pr * (s.rest - logp0 - ((f.r.m - f.z.m) * a.inv + logf(f.r.s) - lz));
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) term += __shfl_xor(term, o);
+    if (threadIdx.x % kWave == 0) a.loss[1 + b] = s.any ? term * a.weight : 0.f;
+}
+
+// Gradient of the named classes in [lo, hi), by one wave, behind the others': there 0
+// stands, or with accumulate what was there. list: the record's classes.
+template <typename L>
+__device__ void put_named(const KdArgs &a, int64_t b, const Entries<L> &e, const bool (&first)[kEach],
+                          const RecordSums &s, const RowFactors &f, const int *list, const float *logits,
+                          bool twice, int lo, int hi) {
+    float *grad = a.grad + b * a.ld_g;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int i = e.at[j];
+        if (!first[j] || i < lo || i >= hi || !e.fired[j]) continue;
+        float p = exp_of(e.l[j] - s.p.m, kLog2e) / s.p.s;
+        if (twice) {
+            p = 0.f;
+            for (int o = 0; o < a.K; ++o) p += list[o] == i ? exp_of(logits[o] - s.p.m, kLog2e) / s.p.s : 0.f;
+        }
+        const float g = -a.weight * a.inv * (exp_of(e.y[j] - f.z.m, a.c2) * f.one_z - p);
+        grad[i] = a.accumulate ? grad[i] + g : g;
+    }
+}
+
+// ------------------------------------------------------- one block a row --
+// The row stays in registers, V vectors a thread: read once, its exponentials formed
+// once, written once.
+template <int T, int V> struct KdShared {
+    u32 bits[T * V / 8];
+    u64 red[T / kWave + 1];
+    int list[kKdMaxK];
+    float logit[kKdMaxK];
+    RecordSums sums;
+    int twice;
+};
+
+template <int T, int V, typename L>
+__global__ __launch_bounds__(T) void distill_row_kernel(KdArgs a, const L *__restrict__ logit) {
+    __shared__ KdShared<T, V> sh;
+    const int64_t b = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid % kWave, n = a.N;
+    const float *row = a.t + b * a.ld_t;
+    f32x4 x[V];
+    // vector v of the row is v = tid + T j; the last may be cut
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int i = (tid + T * j) * 4;
+        if (i + 4 <= n) {
+            x[j] = *reinterpret_cast<const f32x4_any *>(row + i);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[j][k] = i + k < n ? row[i + k] : 0.f;
+        }
+    }
+    for (int k = tid; k < (n + 31) / 32; k += T) sh.bits[k] = 0;
+    if (tid == 0) sh.twice = 0;
+    Entries<L> e;
+    bool first[kEach];
+    if (tid < kWave) e.load(a, b, logit, lane);
     __syncthreads();
-    for (int k = threadIdx.x; k < K; k += kKdThreads) {
-        int i;
-        float l;
-        if (named(idx, logit, k, N, &i, &l) && i >= lo && i < lo + count)
-            atomicOr(&bits[(i - lo) / 32], 1u << ((i - lo) % 32));
+    if (tid < kWave) {
+        bool twice = false;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            first[j] = e.at[j] >= 0;
+            if (first[j]) twice |= atomicOr(&sh.bits[e.at[j] / 32], 1u << (e.at[j] % 32)) >> (e.at[j] % 32) & 1;
+            sh.list[lane + kWave * j] = e.at[j];
+            sh.logit[lane + kWave * j] = e.l[j];
+        }
+        if (__any(twice)) {
+            if (lane == 0) sh.twice = 1;
+            __builtin_amdgcn_wave_barrier();  // the list is this wave's own
+            first_of(sh.list, a.K, e, first);
+        }
+        const RecordSums s = record_sums(a, b, e, first);
+        if (lane == 0) sh.sums = s;
     }
     __syncthreads();
+    // the others' largest y, their exponentials relative to it, and their sum. An
+    // exponential takes the place of its time, negated where the neuron did not fire.
+    float top = -INFINITY;
+    u32 silent[(V * 4 + 31) / 32] = {};
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int v = tid + T * j;
+        const u32 named = v * 4 < n ? sh.bits[v / 8] >> (v % 8 * 4) : 15u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool fired = isfinite(x[j][k]);
+            const bool out = (named >> k & 1) || v * 4 + k >= n;
+            if (!fired) silent[(j * 4 + k) / 32] |= 1u << (j * 4 + k) % 32;
+            x[j][k] = out ? -INFINITY : -(fired ? x[j][k] : a.t_cap);
+            top = fmaxf(top, x[j][k]);
+        }
+    }
+    top = value_of(static_cast<u32>(block_max<T>(key_of(top), sh.red)));
+    const float ref = top > -INFINITY ? top : 0.f;
+    ExpSum r{top > -INFINITY ? 0.f : -INFINITY, 0.f};
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[j][k] = exp_of(x[j][k] - ref, a.c2);
+            r.s += x[j][k];
+        }
+    r = block_exp_sum<T>(r, a.c2, sh.red);
+    r.m = top;
+    const RecordSums s = sh.sums;
+    const RowFactors f(s, r, a.c2);
+    if (tid < kWave) put_loss(a, b, e, s, f);
+    if (!a.grad) return;
+    const float w = s.any ? -a.weight * a.inv * f.other : 0.f;
+    float *grad = a.grad + b * a.ld_g;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int i = (tid + T * j) * 4;
+        f32x4 g;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            g[k] = silent[(j * 4 + k) / 32] >> ((j * 4 + k) % 32) & 1 ? 0.f : x[j][k] * w;
+        if (i + 4 <= n) {
+            f32x4_any *o = reinterpret_cast<f32x4_any *>(grad + i);
+            *o = a.accumulate ? *o + g : g;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < n) grad[i + k] = a.accumulate ? grad[i + k] + g[k] : g[k];
+        }
+    }
+    __syncthreads();
+    if (tid < kWave && s.any) put_named(a, b, e, first, s, f, sh.list, sh.logit, sh.twice != 0, 0, n);
 }
-__device__ __forceinline__ bool marked(const u32 *bits, int i) { return bits[i / 32] >> (i % 32) & 1; }
 
-// part[b][chunk]: the sum over the chunk's classes that the record does not name
+// ---------------------------------------------------- several blocks a row --
+constexpr int kKdThreads = 256;
+constexpr int kKdChunk = 8192;  // classes of a block
+
+// Blocks [0, chunks): the sum over the chunk's classes that the record does not name.
+// The last block of a row: the record's sums.
 template <typename L>
 __global__ __launch_bounds__(kKdThreads) void distill_rest_kernel(KdArgs a, const L *__restrict__ logit) {
     __shared__ u32 bits[kKdChunk / 32];
     __shared__ u64 red[kKdThreads / kWave + 1];
+    __shared__ int list[kKdMaxK];
     const int64_t b = blockIdx.y;
+    const int chunks = gridDim.x - 1, tid = threadIdx.x;
+    float2 *part = a.part + b * kd_row_parts(chunks);
+    if (static_cast<int>(blockIdx.x) == chunks) {
+        Entries<L> e;
+        if (tid < kWave) {
+            e.load(a, b, logit, tid);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) list[tid + kWave * j] = e.at[j];
+        }
+        __syncthreads();
+        if (tid >= kWave) return;
+        bool first[kEach], twice = false;
+        first_of(list, a.K, e, first);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) twice |= e.at[j] >= 0 && !first[j];
+        twice = __any(twice);
+        const RecordSums s = record_sums(a, b, e, first);
+        if (tid == 0) {
+            part[chunks] = make_float2(s.p.m, s.p.s);
+            part[chunks + 1] = make_float2(s.zs.m, s.zs.s);
+            part[chunks + 2] = make_float2(s.rest, s.any ? (twice ? 2.f : 1.f) : 0.f);
+        }
+        return;
+    }
     const int lo = blockIdx.x * kKdChunk, count = min(kKdChunk, a.N - lo);
     const float *row = a.t + b * a.ld_t + lo;
-    mark(bits, lo, count, a.idx + b * a.K, logit + b * a.K, a.K, a.N);
+    for (int k = tid; k < (count + 31) / 32; k += kKdThreads) bits[k] = 0;
+    __syncthreads();
+    for (int k = tid; k < a.K; k += kKdThreads) {
+        const int i = a.idx[b * a.K + k] - lo;
+        if (i >= 0 && i < count && isfinite(widen1(logit[b * a.K + k]))) atomicOr(&bits[i / 32], 1u << (i % 32));
+    }
+    __syncthreads();
     ExpSum s{-INFINITY, 0.f};
-    row_each<kRowAhead>(row, count, threadIdx.x, kKdThreads, [&](int i, float x) {
-        if (marked(bits, i)) return;
+    row_each<kRowAhead>(row, count, tid, kKdThreads, [&](int i, float x) {
+        if (bits[i / 32] >> (i % 32) & 1) return;
         const float y = -(isfinite(x) ? x : a.t_cap);
         if (y > s.m) {
             s.s *= exp_of(s.m - y, a.c2);
@@ -63,121 +309,102 @@ __global__ __launch_bounds__(kKdThreads) void distill_rest_kernel(KdArgs a, cons
         s.s += exp_of(y - s.m, a.c2);
     });
     s = block_exp_sum<kKdThreads>(s, a.c2, red);
-    if (threadIdx.x == 0) a.part[b * gridDim.x + blockIdx.x] = make_float2(s.m, s.s);
+    if (tid == 0) part[blockIdx.x] = make_float2(s.m, s.s);
 }
 
 template <typename L>
-__global__ __launch_bounds__(kKdThreads) void distill_grad_kernel(KdArgs a, const L *__restrict__ logit_of) {
-    __shared__ u32 bits[kKdChunk / 32];
+__global__ __launch_bounds__(kKdThreads) void distill_grad_kernel(KdArgs a, const L *__restrict__ logit) {
     __shared__ u64 red[kKdThreads / kWave + 1];
-    __shared__ int at[kKdMaxK];
-    __shared__ float prob[kKdMaxK];
+    __shared__ int list[kKdMaxK];
+    __shared__ float logits[kKdMaxK];
     const int64_t b = blockIdx.y;
+    const int chunks = gridDim.x, tid = threadIdx.x;
     const int lo = blockIdx.x * kKdChunk, count = min(kKdChunk, a.N - lo);
-    const float *row = a.t + b * a.ld_t;
-    const int32_t *idx = a.idx + b * a.K;
-    const L *logit = logit_of + b * a.K;
-    mark(bits, lo, count, idx, logit, a.K, a.N);
-    // the teacher
-    float rest = a.rest ? a.rest[b] : -INFINITY;
-    if (!isfinite(rest)) rest = -INFINITY;
-    ExpSum p{rest, rest > -INFINITY && threadIdx.x == 0 ? 1.f : 0.f};
-    u64 some = 0;
-    for (int k = threadIdx.x; k < a.K; k += kKdThreads) {
-        int i;
-        float l;
-        const bool is = named(idx, logit, k, a.N, &i, &l);
-        at[k] = is ? i : -1;
-        if (is) {
-            p = exp_join(p, ExpSum{l, 1.f}, kLog2e);
-            some = 1;
-        }
-    }
-    p = block_exp_sum<kKdThreads>(p, kLog2e, red);
-    const bool any = block_max<kKdThreads>(some, red) != 0;
-    // the student
+    const float *row = a.t + b * a.ld_t + lo;
+    const float2 *part = a.part + b * kd_row_parts(chunks);
     ExpSum r{-INFINITY, 0.f};
-    for (int c = threadIdx.x; c < static_cast<int>(gridDim.x); c += kKdThreads) {
-        const float2 v = a.part[b * gridDim.x + c];
-        r = exp_join(r, ExpSum{v.x, v.y}, a.c2);
-    }
+    for (int c = tid; c < chunks; c += kKdThreads) r = exp_join(r, ExpSum{part[c].x, part[c].y}, a.c2);
     r = block_exp_sum<kKdThreads>(r, a.c2, red);
-    ExpSum z = threadIdx.x == 0 ? r : ExpSum{-INFINITY, 0.f};
-    for (int k = threadIdx.x; k < a.K; k += kKdThreads) {
-        const int i = at[k];
-        if (i < 0) continue;
-        const float l = widen1(logit[k]);
-        prob[k] = exp_of(l - p.m, kLog2e) / p.s;
-        bool first = true;
-        for (int o = 0; o < k; ++o) first = first && at[o] != i;
-        const float x = row[i];
-        if (first) z = exp_join(z, ExpSum{-(isfinite(x) ? x : a.t_cap), 1.f}, a.c2);
-    }
-    z = block_exp_sum<kKdThreads>(z, a.c2, red);
-    const float logp0 = p.m + logf(p.s);
-    const float pr = rest > -INFINITY ? exp_of(rest - p.m, kLog2e) / p.s : 0.f;
-    if (blockIdx.x == 0) {
-        // ln q_k = (y_k - z.m) / tau - ln z.s
-        float term = 0.f;
-        const float lz = logf(z.s);
-        for (int k = threadIdx.x; k < a.K; k += kKdThreads) {
-            if (at[k] < 0 || !(prob[k] > 0.f)) continue;
-            const float x = row[at[k]];
-            const float lq = (-(isfinite(x) ? x : a.t_cap) - z.m) * a.inv - lz;
-            term += prob[k] * (widen1(logit[k]) - logp0 - lq);
-        }
-        if (threadIdx.x == 0 && pr > 0.f) term += pr * (rest - logp0 - ((r.m - z.m) * a.inv + logf(r.s) - lz));
-#pragma unroll
-        for (int o = kWave / 2; o > 0; o >>= 1) term += __shfl_xor(term, o);
-        float *fred = reinterpret_cast<float *>(red);
-        __syncthreads();
-        if (threadIdx.x % kWave == 0) fred[threadIdx.x / kWave] = term;
-        __syncthreads();
-        term = 0.f;
-        for (int k = 0; k < kKdThreads / kWave; ++k) term += fred[k];
-        if (threadIdx.x == 0) a.loss[1 + b] = any ? term * a.weight : 0.f;
+    const float2 sp = part[chunks], sz = part[chunks + 1], sr = part[chunks + 2];
+    const RecordSums s{ExpSum{sp.x, sp.y}, ExpSum{sz.x, sz.y}, sr.x, sr.y > 0.f};
+    const RowFactors f(s, r, a.c2);
+    Entries<L> e;
+    if (tid < kWave) {
+        e.load(a, b, logit, tid);
+        if (blockIdx.x == 0) put_loss(a, b, e, s, f);
     }
     if (!a.grad) return;
-    float *grad = a.grad + b * a.ld_g;
-    const float w = -a.weight * a.inv;
-    // e^z / Z = e^(z - z.m) / z.s; others: times 1 - p_r Z / R = (q_r - p_r) / q_r
-    const float one_z = 1.f / z.s;
-    const float qr = r.s * exp_of(r.m - z.m, a.c2) * one_z;
-    const float other = r.s > 0.f ? (qr - pr) / r.s : 0.f;
+    float *grad = a.grad + b * a.ld_g + lo;
+    const float w = s.any ? -a.weight * a.inv * f.other : 0.f;
+    // the named classes among these get their own behind: with accumulate their old
+    // value is kept till then
+    float old[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) old[j] = 0.f;
+    if (tid < kWave && a.accumulate)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (e.at[j] >= lo && e.at[j] < lo + count) old[j] = grad[e.at[j] - lo];
     __syncthreads();
-    row_each<kRowAhead>(row + lo, count, threadIdx.x, kKdThreads, [&](int i, float x) {
-        float g = 0.f;
-        if (isfinite(x) && any) {
-            if (!marked(bits, i)) {
-                g = exp_of(-x - r.m, a.c2) * other;
-            } else {
-                float pk = 0.f;
-                for (int k = 0; k < a.K; ++k) pk += at[k] == lo + i ? prob[k] : 0.f;
-                g = exp_of(-x - z.m, a.c2) * one_z - pk;
-            }
-            g *= w;
-        }
-        float *o = grad + lo + i;
-        if (a.accumulate) g += *o;
-        *o = g;
+    row_each<kRowAhead>(row, count, tid, kKdThreads, [&](int i, float x) {
+        const float g = isfinite(x) ? exp_of(fminf(-x - f.r.m, 0.f), a.c2) * w : 0.f;
+        grad[i] = a.accumulate ? grad[i] + g : g;
     });
+    if (tid < kWave)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            list[tid + kWave * j] = e.at[j];
+            logits[tid + kWave * j] = e.l[j];
+        }
+    __syncthreads();
+    if (tid >= kWave) return;
+    const bool twice = sr.y > 1.f;
+    bool first[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) first[j] = e.at[j] >= 0;
+    if (twice) first_of(list, a.K, e, first);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (first[j] && e.at[j] >= lo && e.at[j] < lo + count) grad[e.at[j] - lo] = old[j];
+    if (s.any) put_named(a, b, e, first, s, f, list, logits, twice, lo, lo + count);
 }
 
-template <typename L> void launch_t(const KdArgs &a, const L *logit, dim3 grid, hipStream_t st) {
-    hipLaunchKernelGGL((distill_rest_kernel<L>), grid, dim3(kKdThreads), 0, st, a, logit);
-    hipLaunchKernelGGL((distill_grad_kernel<L>), grid, dim3(kKdThreads), 0, st, a, logit);
+template <int T, int V, typename L> void launch_row(const KdArgs &a, int64_t B, const L *logit, hipStream_t st) {
+    hipLaunchKernelGGL((distill_row_kernel<T, V, L>), dim3(static_cast<unsigned>(B)), dim3(T), 0, st, a, logit);
+}
+
+template <typename L> void launch_t(const KdArgs &a, int64_t B, const L *logit, hipStream_t st) {
+    const int n = a.N;
+    if (n > 65536 || (B < 32 && n > 8192)) {
+        const int chunks = (n + kKdChunk - 1) / kKdChunk;
+        hipLaunchKernelGGL((distill_rest_kernel<L>), dim3(chunks + 1, static_cast<unsigned>(B)), dim3(kKdThreads), 0,
+                           st, a, logit);
+        hipLaunchKernelGGL((distill_grad_kernel<L>), dim3(chunks, static_cast<unsigned>(B)), dim3(kKdThreads), 0, st,
+                           a, logit);
+    } else if (n <= 256) {
+        launch_row<64, 1>(a, B, logit, st);
+    } else if (n <= 1024) {
+        launch_row<64, 4>(a, B, logit, st);
+    } else if (n <= 4096) {
+        launch_row<256, 4>(a, B, logit, st);
+    } else if (n <= 16384) {
+        launch_row<512, 8>(a, B, logit, st);
+    } else if (n <= 32768) {
+        launch_row<1024, 8>(a, B, logit, st);
+    } else {
+        launch_row<1024, 16>(a, B, logit, st);
+    }
 }
 
 }  // namespace
 
-int64_t distill_parts(int64_t N) { return (N + kKdChunk - 1) / kKdChunk; }
+int64_t distill_parts(int64_t N) { return kd_row_parts((N + kKdChunk - 1) / kKdChunk); }
 
 hipError_t launch_distill(const KdArgs &a, int64_t B, const void *logit, bool bf16, hipStream_t st) {
     ProfScope prof("distill", st);
     if (B > 0) {
-        const dim3 grid(static_cast<unsigned>(distill_parts(a.N)), static_cast<unsigned>(B));
-        if (bf16) launch_t(a, static_cast<const uint16_t *>(logit), grid, st);
-        else launch_t(a, static_cast<const float *>(logit), grid, st);
+        if (bf16) launch_t(a, B, static_cast<const uint16_t *>(logit), st);
+        else launch_t(a, B, static_cast<const float *>(logit), st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -131,6 +131,8 @@ struct KdArgs {
     float *loss;
     float2 *part;
 };
+// per row: a sum for each chunk of the classes, and three of its record
+__host__ __device__ constexpr int64_t kd_row_parts(int64_t chunks) { return chunks + 3; }
 int64_t distill_parts(int64_t N);
 hipError_t launch_distill(const KdArgs &a, int64_t B, const void *logit, bool bf16, hipStream_t st);
 
