@@ -23,6 +23,10 @@ __device__ __forceinline__ float goodness(float x, const ScoreMap &m) {
     const float v = isfinite(x) ? x : m.cap;
     return __uint_as_float(__float_as_uint(v) ^ m.flip);
 }
+// the same for a score that is finite, or whose kind the caller looks at
+__device__ __forceinline__ float flipped(float x, const ScoreMap &m) {
+    return __uint_as_float(__float_as_uint(x) ^ m.flip);
+}
 __device__ __forceinline__ float widen1(float x) { return x; }
 __device__ __forceinline__ float widen1(uint16_t x) { return bf16_to_f32(x); }
 
@@ -59,56 +63,47 @@ template <typename E> __device__ __forceinline__ typename RowVec<E>::type load_v
     return *reinterpret_cast<const typename RowVec<E>::any *>(p);
 }
 
-// f(index, score) for the first n elements of a row by `count` threads, of which
-// this is number `tid`; kAhead vectors a thread on the way at once, or (0) element by
-// element in a loop of few registers, for what rows in earnest do not reach.
+// f(slot, first index, vector) for the whole vectors of the first n elements of a row, by
+// `count` threads, of which this is number `tid`: kAhead a thread on the way at once,
+// `slot` the number among these. Returns the index of the first element behind them.
 constexpr int kRowAhead = 4;
 template <int kAhead, typename E, typename F>
-__device__ __forceinline__ void row_each(const E *p, int n, int tid, int count, F f) {
+__device__ __forceinline__ int vec_each(const E *p, int n, int tid, int count, F f) {
     using V = RowVec<E>;
-    if constexpr (kAhead == 0) {
+    const int nv = n / V::n, whole = nv - nv % (kAhead * count);
+    int v = tid;
 #pragma unroll 1
-        for (int i = tid; i < n; i += count) f(i, widen1(p[i]));
-    } else {
-        const int nv = n / V::n;
-#pragma unroll 1
-        for (int v0 = tid; v0 < nv; v0 += kAhead * count) {
-            typename V::type r[kAhead] = {};
+    for (; v < whole; v += kAhead * count) {
+        typename V::type r[kAhead];
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a)
-                if (v0 + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v0 + a * count) * V::n);
+        for (int a = 0; a < kAhead; ++a) r[a] = load_vec<E>(p + static_cast<int64_t>(v + a * count) * V::n);
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                if (v0 + a * count >= nv) break;
-#pragma unroll
-                for (int k = 0; k < V::n; ++k)
-                    f((v0 + a * count) * V::n + k, widen1(static_cast<E>(r[a][k])));
-            }
-        }
-        for (int i = nv * V::n + tid; i < n; i += count) f(i, widen1(p[i]));
+        for (int a = 0; a < kAhead; ++a) f(a, (v + a * count) * V::n, r[a]);
     }
+    if (whole < nv) {
+        typename V::type r[kAhead] = {};
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (v + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v + a * count) * V::n);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (v + a * count < nv) f(a, (v + a * count) * V::n, r[a]);
+    }
+    return nv * V::n;
 }
 
-// As row_each over [0, n), f(group, index, score): the entries of a thread fall into
-// kRowAhead groups.
-template <typename E, typename F>
-__device__ __forceinline__ void row_groups(const E *p, int n, int tid, int count, F f) {
-    using V = RowVec<E>;
-    const int nv = n / V::n;
-    for (int v0 = tid; v0 < nv; v0 += kRowAhead * count) {
-        typename V::type r[kRowAhead] = {};
+// f(index, score) for the first n elements of a row, as vec_each, or (kAhead 0) element by
+// element in a loop of few registers, for what rows in earnest do not reach.
+template <int kAhead, typename E, typename F>
+__device__ __forceinline__ void row_each(const E *p, int n, int tid, int count, F f) {
+    int done = 0;
+    if constexpr (kAhead > 0)
+        done = vec_each<kAhead>(p, n, tid, count, [&](int, int i, typename RowVec<E>::type r) {
 #pragma unroll
-        for (int a = 0; a < kRowAhead; ++a)
-            if (v0 + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v0 + a * count) * V::n);
-#pragma unroll
-        for (int a = 0; a < kRowAhead; ++a) {
-            if (v0 + a * count >= nv) break;
-#pragma unroll
-            for (int k = 0; k < V::n; ++k)
-                f(a, (v0 + a * count) * V::n + k, widen1(static_cast<E>(r[a][k])));
-        }
-    }
-    for (int i = nv * V::n + tid; i < n; i += count) f(0, i, widen1(p[i]));
+            for (int k = 0; k < RowVec<E>::n; ++k) f(i + k, widen1(static_cast<E>(r[k])));
+        });
+#pragma unroll 1
+    for (int i = done + tid; i < n; i += count) f(i, widen1(p[i]));
 }
 
 // ------------------------------------------------------ sums over a block --

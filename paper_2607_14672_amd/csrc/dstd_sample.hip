@@ -25,20 +25,22 @@ constexpr int kBins = 2048;  // of a histogram over a row
 // chosen from candidates.
 template <int T> constexpr int kList = T >= 1024 ? 2048 : 1024;
 constexpr int kMaxPicked = 1024;
-constexpr int kGroups = kRowAhead;  // of a thread's share of the row, a maximum each
+// groups of a thread's share of the row, a maximum each
+template <typename E> constexpr int kGroups = sizeof(E) == 2 ? 2 * kRowAhead : kRowAhead;
 
 template <int T> struct RowShared {
     u64 red[T / kWave + 1];
     u64 list[kList<T>];
     u64 hist[kBins];
     u64 found[2];
-    int count;
+    int count, seen;
 };
 
 // What is kept of a row: all up to a place in its order.
 struct Border {
     u64 last;
     __device__ bool has(u32 key, int i) const { return key > kAbsentKey && rank_of(key, i) >= last; }
+    __device__ bool all() const { return last == 0; }
 };
 
 // Weights of the exponentials in 64-bit integers, the largest 2^shift (shift <= 51):
@@ -132,7 +134,7 @@ __device__ int collect(RowShared<T> &sh, const E *row, int n, const ScoreMap &m,
     return sh.count;
 }
 
-// First index where the sum of weight(key, index) up to it exceeds share times
+// First index where the sum of weight(goodness, index) up to it exceeds share times
 // the whole sum (returned in *all), -1 where that is 0. The waves sum a part of
 // the row each; the part that holds the place is read again.
 template <int T, int kAhead, typename E, typename F>
@@ -144,7 +146,7 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m
     const int lo = min(n, wave * part), hi = min(n, lo + part);
     u64 s = 0;
     row_each<kAhead>(row + lo, hi - lo, lane, kWave,
-                [&](int i, float x) { s += weight(key_of(goodness(x, m)), lo + i); });
+                [&](int i, float x) { s += weight(goodness(x, m), lo + i); });
     u64 total;
     u64 before = block_before<T>(s, sh.red, &total);
     *all = total;
@@ -161,22 +163,38 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m
     __syncthreads();
     u64 base = sh.found[0];
     const int first = sh.count * part, last = min(n, first + part);
-    // the place, T runs of `each` elements in turn
-    const int each = (last - first + T - 1) / T;
-    const int a = min(last, first + static_cast<int>(threadIdx.x) * each), b = min(last, a + each);
-    u64 mine = 0;
-    for (int i = a; i < b; ++i) mine += weight(key_of(goodness(widen1(row[i]), m)), i);
-    u64 unused;
-    base += block_before<T>(mine, sh.red, &unused);
-    __syncthreads();
-    if (static_cast<double>(base) <= target && static_cast<double>(base + mine) > target)
-        for (int i = a; i < b; ++i) {
-            base += weight(key_of(goodness(widen1(row[i]), m)), i);
-            if (static_cast<double>(base) > target) {
-                sh.count = i;
-                break;
-            }
+    // the place: a vector's elements a thread at a time
+    constexpr int vn = RowVec<E>::n;
+    for (int from = first; from < last; from += T * vn) {
+        const int a = from + static_cast<int>(threadIdx.x) * vn;
+        u64 w[vn], mine = 0;
+        if (a + vn <= last) {
+            const auto r = load_vec<E>(row + a);
+#pragma unroll
+            for (int k = 0; k < vn; ++k) w[k] = weight(goodness(widen1(static_cast<E>(r[k])), m), a + k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < vn; ++k)
+                w[k] = a + k < last ? weight(goodness(widen1(row[a + k]), m), a + k) : 0;
         }
+#pragma unroll
+        for (int k = 0; k < vn; ++k) mine += w[k];
+        u64 round;
+        u64 at = base + block_before<T>(mine, sh.red, &round);
+        base += round;
+        if (static_cast<double>(base) <= target) continue;
+        __syncthreads();
+        if (static_cast<double>(at) <= target && static_cast<double>(at + mine) > target) {
+            int k = 0;
+#pragma unroll
+            for (int q = 0; q < vn; ++q) {
+                at += w[q];
+                if (static_cast<double>(at) <= target) k = q + 1;
+            }
+            sh.count = a + k;
+        }
+        break;
+    }
     __syncthreads();
     const int got = sh.count;
     __syncthreads();
@@ -260,7 +278,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                     // k entries of that key lie before it
                     u64 all_ties;
                     const u32 tie = lo;
-                    auto is_tie = [&](u32 key, int i) -> u64 { return key == tie && kept.has(key, i); };
+                    auto is_tie = [&](float y, int i) -> u64 { return key_of(y) == tie && kept.has(tie, i); };
                     const int i = by_index<T, kAhead>(sh, row, n, m, (static_cast<double>(k) + 0.5) / count, &all_ties, is_tie);
                     return Border{rank_of(lo, i)};
                 }
@@ -320,6 +338,14 @@ __device__ Extremes row_extremes(RowShared<T> &sh, const E *row, int n, const Sc
     return Extremes{value_of(lo), value_of(hi), count};
 }
 
+// The K first entries of a row, K of them at least. This and other ways that rows in
+// earnest seldom take are not inlined: they would take registers from the loops of those.
+template <int T, typename E>
+__device__ __attribute__((noinline)) Border pick_count(RowShared<T> &sh, const E *row, int n, ScoreMap m, Extremes ex,
+                                                       int K) {
+    return by_order<T, 0>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
+}
+
 // What a draw goes by, and where it is written.
 struct DrawArgs {
     double scale, top_p, dmax;  // dmax: -ln min_p, the largest distance that is kept
@@ -341,7 +367,8 @@ __device__ __forceinline__ double share_of(const DrawArgs &a, int64_t b) {
 
 // One class of a row by its definition, whatever the values.
 template <int T, int kAhead, typename E>
-__device__ void sample_row(RowShared<T> &sh, const E *row, int64_t b, int n, const ScoreMap &m, const DrawArgs &a) {
+__device__ __forceinline__ void sample_row(RowShared<T> &sh, const E *row, int64_t b, int n, const ScoreMap &m,
+                                           const DrawArgs &a) {
     const Extremes ex = row_extremes<T, kAhead>(sh, row, n, m);
     if (ex.count == 0) {
         if (threadIdx.x == 0) put_draw(a, b, -1, 0.0, 0);
@@ -350,15 +377,26 @@ __device__ void sample_row(RowShared<T> &sh, const E *row, int64_t b, int n, con
     const Mass mass{ex.ymax, a.scale, a.shift};
     Border kept{0};
     if (a.top_k > 0 && a.top_k < ex.count)
-        kept = by_order<T, kAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax, INFINITY, One{}, a.top_k, 0.0);
+        kept = pick_count<T, E>(sh, row, n, m, ex, a.top_k);
     if (a.top_p < 1.0)
         kept = by_order<T, kAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax,
                                    0.6931471805599453 * (a.shift + 1) / a.scale, mass, 0, a.top_p);
     u64 all;
-    const int i = by_index<T, kAhead>(sh, row, n, m, share_of(a, b), &all, [&](u32 key, int k) -> u64 {
-        return kept.has(key, k) && mass.distance(key) <= a.dmax ? mass(key) : 0;
-    });
-    if (threadIdx.x == 0) put_draw(a, b, i, mass.distance(key_of(goodness(widen1(row[i]), m))), all);
+    const double share = share_of(a, b);
+    int i;
+    if (kept.all() && a.dmax == INFINITY)
+        i = by_index<T, kAhead>(sh, row, n, m, share, &all, [&](float y, int) { return mass.of(y); });
+    else
+        i = by_index<T, kAhead>(sh, row, n, m, share, &all, [&](float y, int k) -> u64 {
+            return kept.has(key_of(y), k) && mass.distance(y) <= a.dmax ? mass.of(y) : 0;
+        });
+    if (threadIdx.x == 0) put_draw(a, b, i, mass.distance(goodness(widen1(row[i]), m)), all);
+}
+// The same for rows that a faster way does not take.
+template <int T, typename E>
+__device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const E *row, int64_t b, int n, ScoreMap m,
+                                                         DrawArgs a) {
+    sample_row<T, 0>(sh, row, b, n, m, a);
 }
 
 template <int T, typename E>
@@ -366,34 +404,87 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int
                                                                       ScoreMap m, DrawArgs a) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
-    // bf16 rows come here by a cap that no bf16 value equals, or by their size
-    sample_row<T, sizeof(E) == 4 ? 1 : 0>(sh, x + b * ld, b, n, m, a);
+    sample_row<T, 1>(sh, x + b * ld, b, n, m, a);
 }
 
 // Candidates for the K first entries of a row's order: all that reach a bound which K
 // entries reach at least. The bound is the K-th largest of the groups' largest values, or
 // a little less: few others reach it unless the largest lie close together in the row.
-// Goodness y without a look at entries that do not count: y < INF is false for these, and
-// they are no candidates.
-template <int T, typename E>
-__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, bool caps, int K) {
-    float best[kGroups];
+using i16x2 = int16_t __attribute__((ext_vector_type(2)));
+using u32x4 = u32 __attribute__((ext_vector_type(4)));
+
+// bf16 bits as 16-bit integers in the order of the goodness (-0 just below +0; what is
+// not finite at the ends), two at a time; flip: 0, or all ones where smaller scores are
+// likelier. Its own inverse without flip.
+__device__ __forceinline__ i16x2 order16(u32 bits, u32 flip) {
+    const i16x2 h = __builtin_bit_cast(i16x2, bits);
+    const u32 sign = __builtin_bit_cast(u32, h >> 15);
+    return __builtin_bit_cast(i16x2, ((sign & 0x7fff7fffu) ^ bits) ^ flip);
+}
+__device__ __forceinline__ float order16_value(int16_t k) {
+    const u32 bits = static_cast<uint16_t>(k ^ ((k >> 15) & 0x7fff));
+    return __uint_as_float(bits << 16);
+}
+
+__device__ __forceinline__ float larger(float y, float best) { return y > best ? y : best; }  // not NaN
+
+// The largest goodness of each group of a thread. Entries that do not count are not
+// looked for: a NaN changes nothing, and where +inf shows up (a NaN too, in 16 bits)
+// the bound is given up.
+template <int T, bool kCaps, typename E>
+__device__ __forceinline__ void group_best(const E *row, int n, const ScoreMap &m, float (&best)[kGroups<E>]) {
+    auto value = [&](float x) { return kCaps ? goodness(x, m) : flipped(x, m); };
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) best[g] = -INFINITY;
-    row_groups<E>(row, n, threadIdx.x, T, [&](int g, int, float x) {
-        // med3 passes NaN over; +inf gives FLT_MAX, which is looked at below
-        const float y = caps ? goodness(x, m) : __uint_as_float(__float_as_uint(x) ^ m.flip);
-        best[g] = __builtin_amdgcn_fmed3f(y, best[g], FLT_MAX);
-    });
+    for (int g = 0; g < kGroups<E>; ++g) best[g] = -INFINITY;
+    int done;
+    if constexpr (sizeof(E) == 2) {
+        if constexpr (!kCaps) {
+            const u32 flip = m.flip ? 0xffffffffu : 0;
+            i16x2 top[kRowAhead];
+#pragma unroll
+            for (int g = 0; g < kRowAhead; ++g) top[g] = i16x2{-32768, -32768};
+            done = vec_each<kRowAhead>(row, n, threadIdx.x, T, [&](int g, int, typename RowVec<E>::type r) {
+                const u32x4 w = __builtin_bit_cast(u32x4, r);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top[g] = __builtin_elementwise_max(top[g], order16(w[k], flip));
+            });
+#pragma unroll
+            for (int g = 0; g < kRowAhead; ++g)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float y = order16_value(top[g][k]);
+                    best[2 * g + k] = top[g][k] >= 0x7f80 ? INFINITY : y == y ? y : -INFINITY;
+                }
+        } else {
+            done = vec_each<1>(row, n, threadIdx.x, T, [&](int, int, typename RowVec<E>::type r) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) best[k] = larger(value(widen1(r[k])), best[k]);
+            });
+        }
+    } else {
+        done = vec_each<kRowAhead>(row, n, threadIdx.x, T, [&](int g, int, typename RowVec<E>::type r) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) best[g] = larger(value(r[k]), best[g]);
+        });
+    }
+    for (int i = done + threadIdx.x; i < n; i += T)
+        best[0] = larger(value(widen1(row[i])), best[0]);
+}
+
+template <int T, bool kCaps, typename E>
+__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, int K) {
+    constexpr int groups = kGroups<E>;
+    float best[groups];
+    group_best<T, kCaps>(row, n, m, best);
     float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
+    for (int g = 0; g < groups; ++g) {
         if (best[g] > -INFINITY) lo = fminf(lo, best[g]);
-        hi = best[g] == best[g] ? fmaxf(hi, best[g]) : FLT_MAX;
+        hi = fmaxf(hi, best[g]);
     }
     hi = value_of(static_cast<u32>(block_max<T>(key_of(hi), sh.red)));
     lo = value_of(static_cast<u32>(block_min<T>(key_of(lo), sh.red)));
-    if (hi >= FLT_MAX || K > kGroups * T) return -FLT_MAX;
+    if (hi == INFINITY || K > groups * T) return -FLT_MAX;
     if (!(hi > -INFINITY)) return INFINITY;  // nothing counts
     // bins of the range of the maxima
     const float per = static_cast<float>(kBins / (static_cast<double>(hi) - static_cast<double>(lo)));
@@ -401,9 +492,9 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
     for (int k = threadIdx.x; k < kBins; k += T) hist[k] = 0;
     if (threadIdx.x == 0) sh.count = -1;
     __syncthreads();
-    int bin[kGroups];
+    int bin[groups];
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
+    for (int g = 0; g < groups; ++g) {
         bin[g] = kBins;  // a group without an entry
         if (best[g] > -INFINITY) {
             bin[g] = static_cast<int>(fminf((hi - best[g]) * per, kBins - 1.f));
@@ -429,7 +520,7 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
     const int last = sh.count;
     float bound = INFINITY;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g)
+    for (int g = 0; g < groups; ++g)
         if (bin[g] <= last) bound = fminf(bound, best[g]);
     bound = value_of(static_cast<u32>(block_min<T>(key_of(bound), sh.red)));
     return last < 0 ? -FLT_MAX : bound;
@@ -438,73 +529,138 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
 // The K first entries of a row's order and at most a few more, sorted, in the list;
 // returns how many there are (fewer than K where the row has fewer). kSum: *others is the
 // sum over the entries behind the K-th.
-template <int T, bool kSum, typename E>
-__device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, bool caps, int K, float c2,
+// The K first entries into the list where the candidates are too many for it; and the sum
+// over all entries behind a place in the row's order, relative to the largest of them.
+template <int T, typename E>
+__device__ __attribute__((noinline)) int pick_exactly(RowShared<T> &sh, const E *row, int n, ScoreMap m, int K) {
+    const Border kept = pick_count<T, E>(sh, row, n, m, row_extremes<T, 0>(sh, row, n, m), K);
+    return collect<T, 0>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+}
+template <int T, typename E>
+__device__ __attribute__((noinline)) ExpSum sum_behind(const E *row, int n, ScoreMap m, u64 last, float c2) {
+    ExpSum s{-INFINITY, 0.f};
+    row_each<0>(row, n, threadIdx.x, T, [&](int i, float v) {
+        const float y = goodness(v, m);
+        const u32 key = key_of(y);
+        if (key > kAbsentKey && rank_of(key, i) < last) {
+            if (y > s.m) {
+                s.s *= exp_of(s.m - y, c2);
+                s.m = y;
+            }
+            s.s += exp_of(y - s.m, c2);
+        }
+    });
+    return s;
+}
+
+template <int T, bool kSum, bool kCaps, typename E>
+__device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, int K, float c2,
                           ExpSum *others) {
     float bound = -FLT_MAX;
-    if (n > kList<T>) bound = candidate_bound<T>(sh, row, n, m, caps, K);
+    if (n > kList<T>) bound = candidate_bound<T, kCaps>(sh, row, n, m, K);
     if (kSum) *others = ExpSum{-INFINITY, 0.f};
     if (bound == INFINITY) return 0;
+    // the bound among 16-bit keys (the lower of the two zeros)
+    const u32 flip16 = m.flip ? 0xffffffffu : 0;
+    const int bound16 = bound == 0.f ? -1 : order16(__float_as_uint(bound) >> 16, 0)[0];
+    // vectors with a candidate, in the histogram's memory; they are looked through behind
+    // the loop, all at once
+    constexpr int most = 2 * kBins, vn = RowVec<E>::n;
+    u32 *seen = reinterpret_cast<u32 *>(sh.hist);
     __syncthreads();
-    if (threadIdx.x == 0) sh.count = 0;
+    if (threadIdx.x == 0) sh.count = sh.seen = 0;
     __syncthreads();
-    float sum = 0.f;  // of what is below the bound, relative to it
-    row_each<kRowAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
-        const float y = caps ? goodness(x, m) : __uint_as_float(__float_as_uint(x) ^ m.flip);
-        const float d = y - bound;
-        if (d >= 0.f && y < INFINITY) {
+    // what is below the bound is summed relative to it, as 2^(c x - kb); NaN adds 0
+    float kb = bound * c2, sum = 0.f;
+    const float c = m.flip ? -c2 : c2;
+    const bool sums = bound > -FLT_MAX && isfinite(kb);
+    if (!sums) kb = 0.f;
+    auto term = [&](float x) {
+        return __builtin_amdgcn_exp2f(fmaxf(fmaf(x, c, -kb), -1000.f));
+    };
+    auto capped = [&](float x) { return kCaps && !isfinite(x) ? m.cap : x; };
+    auto look = [&](int i) {
+        const float x = capped(widen1(row[i])), y = flipped(x, m);
+        if (y >= bound && y < INFINITY) {
             const int at = atomicAdd(&sh.count, 1);
             if (at < kList<T>) sh.list[at] = rank_of(key_of(y), i);
+        } else if (kSum) {
+            sum += y < bound ? term(x) : 0.f;
         }
-        if (kSum && d < 0.f) sum += exp_of(d, c2);
+    };
+    const int done = vec_each<kRowAhead>(row, n, threadIdx.x, T, [&](int, int i, typename RowVec<E>::type r) {
+        float x[vn];
+        bool some;
+        if constexpr (sizeof(E) == 2 && !kCaps) {
+            const u32x4 w = __builtin_bit_cast(u32x4, r);
+            i16x2 top = order16(w[0], flip16);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) top = __builtin_elementwise_max(top, order16(w[k], flip16));
+            some = max(top[0], top[1]) >= bound16;
+#pragma unroll
+            for (int k = 0; k < vn; ++k) x[k] = widen1(static_cast<E>(r[k]));
+        } else {
+            float top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < vn; ++k) {
+                x[k] = capped(widen1(static_cast<E>(r[k])));
+                top = larger(flipped(x[k], m), top);
+            }
+            some = top >= bound;
+        }
+        if (some) {
+            const int at = atomicAdd(&sh.seen, 1);
+            if (at < most) seen[at] = i;
+        } else if (kSum) {
+#pragma unroll
+            for (int k = 0; k < vn; ++k) sum += term(x[k]);
+        }
     });
+    __syncthreads();
+    if (sh.seen <= most) {
+        for (int k = threadIdx.x; k < sh.seen * vn; k += T) look(seen[k / vn] + k % vn);
+    } else {
+        sum = 0.f;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < done; i += T) look(i);
+    }
+    if (done + static_cast<int>(threadIdx.x) < n) look(done + threadIdx.x);
     __syncthreads();
     int count = sh.count;
     bool listed = bound == -FLT_MAX;  // the sum is that of the list's others alone
     if (count > kList<T>) {
-        const Extremes ex = row_extremes<T, 0>(sh, row, n, m);
-        const Border kept = by_order<T, 0>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
-        count = collect<T, 0>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+        count = pick_exactly<T, E>(sh, row, n, m, K);
         sum = 0.f;
         listed = false;
     }
     sort_list<T>(sh, count);
     if (!kSum || count < K) return count;
+    if (!sums) sum = 0.f;
     ExpSum s{-INFINITY, 0.f};
     const bool some = __syncthreads_or(sum > 0.f);
     if (some || listed) {
-        if (sum > 0.f) s = ExpSum{bound, sum};
+        // kb was rounded
+        if (sum > 0.f) s = ExpSum{bound, sum * __builtin_amdgcn_exp2f(-fmaf(bound, c2, -kb))};
         for (int k = K + threadIdx.x; k < count; k += T)
             s = exp_join(s, ExpSum{value_of(rank_key(sh.list[k])), 1.f}, c2);
     } else {
         // all others far below the bound (their sum there is 0), or no bound was found
-        const u64 last = sh.list[K - 1];
-        row_each<0>(row, n, threadIdx.x, T, [&](int i, float v) {
-            const float y = goodness(v, m);
-            const u32 key = key_of(y);
-            if (key > kAbsentKey && rank_of(key, i) < last) {
-                if (y > s.m) {
-                    s.s *= exp_of(s.m - y, c2);
-                    s.m = y;
-                }
-                s.s += exp_of(y - s.m, c2);
-            }
-        });
+        s = sum_behind<T, E>(row, n, m, sh.list[K - 1], c2);
     }
     *others = block_exp_sum<T>(s, c2, sh.red);
     return count;
 }
 
-template <int T, typename E>
+template <int T, bool kCaps, typename E>
 __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
-                                                       bool caps, double scale, float c2, int K,
+                                                       double scale, float c2, int K,
                                                        int32_t *__restrict__ idx, float *__restrict__ logit,
                                                        float *__restrict__ rest) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
     const E *row = x + b * ld;
     ExpSum s;
-    const int count = candidates<T, true>(sh, row, n, m, caps, K, c2, &s);
+    const int count = candidates<T, true, kCaps>(sh, row, n, m, K, c2, &s);
     for (int k = threadIdx.x; k < K; k += T) {
         const bool some = k < count;
         const u64 r = some ? sh.list[k] : 0;
@@ -517,14 +673,14 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n,
 }
 
 // One class from the top_k <= kMaxPicked first entries of each row.
-template <int T, typename E>
+template <int T, bool kCaps, typename E>
 __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int n, int64_t ld,
                                                                              const E *__restrict__ x, ScoreMap m,
-                                                                             bool caps, DrawArgs a) {
+                                                                             DrawArgs a) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
     const E *row = x + b * ld;
-    int count = candidates<T, false>(sh, row, n, m, caps, a.top_k, 0.f, nullptr);
+    int count = candidates<T, false, kCaps>(sh, row, n, m, a.top_k, 0.f, nullptr);
     if (count == 0) {
         if (threadIdx.x == 0) put_draw(a, b, -1, 0.0, 0);
         return;
@@ -583,35 +739,18 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int
 }
 
 // ---------------------------------------------- rows of few distinct values --
-// bf16 scores of a magnitude in [2^-24, 2^8) take 2 * 4095 values, and 0; how often each
-// occurs says which are kept and what they weigh, with an exponential a value instead of
-// one an entry. Bins fall from the largest value: kHalf - t for the t-th magnitude,
-// kHalf for 0, kHalf + t for its negative, and the last for all that is smaller (of
-// weight 0, or the row is not drawn from here).
-constexpr int kHalf = 4095, kValues = 2 * kHalf + 2, kFirstMag = 0x3381;
-constexpr int kNoBin = -1, kOddBin = -2;
-struct BinMap {
-    u32 flip;  // as of ScoreMap, for 16 bits
-    u32 cap;   // bits of what an entry that is not finite counts as; 0x8000 more: left out
-};
-__device__ __forceinline__ int value_bin(u32 bits, const BinMap &m) {
-    const int t = static_cast<int>(bits & 0x7fff) - kFirstMag + 1;
-    const int neg = static_cast<int>((bits ^ m.flip) << 16) >> 31;  // 0 or -1
-    if (static_cast<u32>(t - 1) < static_cast<u32>(kHalf)) return kHalf + ((t ^ ~neg) - ~neg);
-    if ((bits & 0x7fff) >= 0x7f80) {
-        if (m.cap > 0xffff) return kNoBin;
-        const int tc = static_cast<int>(m.cap & 0x7fff) - kFirstMag + 1;
-        const int nc = static_cast<int>((m.cap ^ m.flip) << 16) >> 31;
-        return (m.cap & 0x7fff) == 0 ? kHalf : kHalf + ((tc ^ ~nc) - ~nc);
-    }
-    if ((bits & 0x7fff) == 0) return kHalf;
-    return neg && t > kHalf ? kValues - 1 : kOddBin;
-}
-__device__ __forceinline__ float bin_value(int bin) {
-    const int t = bin - kHalf;
-    if (t == 0) return 0.f;
-    const u32 mag = (t < 0 ? -t : t) + kFirstMag - 1;
-    return bf16_to_f32(static_cast<uint16_t>(mag | (t > 0 ? 0x8000u : 0u)));
+// bf16 scores of a magnitude in [2^-24, 2^8) take 2 * 4096 values: how often each occurs
+// says which are kept and what they weigh, with an exponential a value instead of one an
+// entry. Zeros are counted apart, and so is what is larger with a goodness below 0, which
+// weighs nothing (or the row is drawn from by its definition, as one with any other value).
+constexpr int kMags = 4096, kFirstMag = 0x3380, kValues = 2 * kMags;
+using u16x2 = uint16_t __attribute__((ext_vector_type(2)));
+
+// A value's place among the counters: its magnitude, its sign bit above.
+__device__ __forceinline__ u32 slots_of(u32 bits, u16x2 *most) {
+    const u16x2 mag = __builtin_bit_cast(u16x2, bits & 0x7fff7fffu) - u16x2{kFirstMag, kFirstMag};
+    *most = __builtin_elementwise_max(*most, mag);
+    return __builtin_bit_cast(u32, mag) | (bits >> 3 & 0x10001000u);
 }
 
 template <int T> struct ValueShared {
@@ -623,80 +762,114 @@ template <int T> struct ValueShared {
     };
     u64 part[T / kWave];
     u32 ties[T / kWave];
-    u64 found, tie_weight;
-    int tie_bin, tie_keep, at;
+    u64 tie_weight, zero_weight;
+    int tie_slot, tie_keep;
+    u32 zeros, below, odd;
+};
+constexpr int kZeroSlot = kValues, kNoSlot = -1;
+
+// The slot of one entry, whatever it is.
+struct OneSlot {
+    u32 flip, cap;  // as of ScoreMap, in 16 bits; 0x10000: left out
+    __device__ int operator()(u32 bits) const {
+        if ((bits & 0x7fff) >= 0x7f80) {
+            if (cap > 0xffff) return kNoSlot;
+            bits = cap;
+        }
+        const u32 mag = (bits & 0x7fff) - kFirstMag;
+        if (mag < static_cast<u32>(kMags)) return static_cast<int>(mag | (bits >> 3 & 0x1000));
+        if ((bits & 0x7fff) == 0) return kZeroSlot;
+        // too large: below all (-2), or of a goodness above 0, or too small (-3)
+        return ((bits ^ flip) & 0x8000) && (bits & 0x7fff) > kFirstMag ? -2 : -3;
+    }
 };
 
-// f(index, bits) as row_each
-template <typename F>
-__device__ __forceinline__ void bits_each(const uint16_t *p, int n, int tid, int count, F f) {
-    const int nv = n / 8;
-#pragma unroll 1
-    for (int v0 = tid; v0 < nv; v0 += 2 * count) {
-        RowVec<uint16_t>::type r[2] = {};
-#pragma unroll
-        for (int a = 0; a < 2; ++a)
-            if (v0 + a * count < nv) r[a] = load_vec<uint16_t>(p + static_cast<int64_t>(v0 + a * count) * 8);
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            if (v0 + a * count >= nv) break;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f((v0 + a * count) * 8 + k, static_cast<u32>(r[a][k]));
-        }
-    }
-    for (int i = nv * 8 + tid; i < n; i += count) f(i, static_cast<u32>(p[i]));
-}
-
 template <int T>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_values_kernel(int n, int64_t ld,
-                                                                             const uint16_t *__restrict__ x,
-                                                                             ScoreMap m, BinMap bm, DrawArgs a) {
+__global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, const uint16_t *__restrict__ x,
+                                                             ScoreMap m, OneSlot one, DrawArgs a) {
     __shared__ ValueShared<T> sh;
     constexpr int each = kValues / T, waves = T / kWave;
-    static_assert(kValues % T == 0, "");
     const int64_t b = blockIdx.x;
     const uint16_t *row = x + b * ld;
     const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
     for (int k = tid; k < kValues; k += T) sh.count[k] = 0;
+    if (tid == 0) sh.zeros = sh.below = sh.odd = 0;
     __syncthreads();
-    bool odd = false;
-    bits_each(row, n, tid, T, [&](int, u32 bits) {
-        const int bin = value_bin(bits, bm);
-        if (bin >= 0) atomicAdd(&sh.count[bin], 1u);
-        odd |= bin == kOddBin;
+    auto count_one = [&](u32 bits) {
+        const int slot = one(bits);
+        if (slot >= 0) atomicAdd(slot == kZeroSlot ? &sh.zeros : &sh.count[slot], 1u);
+        else if (slot == -2) sh.below = 1;
+        else if (slot == -3) sh.odd = 1;
+    };
+    int done = vec_each<kRowAhead>(row, n, tid, T, [&](int, int i, RowVec<uint16_t>::type r) {
+        const u32x4 w = __builtin_bit_cast(u32x4, r);
+        u16x2 most = {0, 0};
+        u32 s[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] = slots_of(w[k], &most);
+        if (max(most[0], most[1]) < kMags) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                atomicAdd(&sh.count[s[k] & 0xffff], 1u);
+                atomicAdd(&sh.count[s[k] >> 16], 1u);
+            }
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                const u32 v = k == 0 ? w[0] : k == 1 ? w[1] : k == 2 ? w[2] : w[3];
+                count_one(v & 0xffff);
+                count_one(v >> 16);
+            }
+        }
     });
-    odd = __syncthreads_or(odd);
-    // each thread's bins
-    u32 count[each];
-    u64 first = kValues;
-    u64 counted = 0;
+    if (done + tid < n) count_one(row[done + tid]);
+    __syncthreads();
+    // the values in falling order: place p of the first half is magnitude kMags - 1 - p
+    // above 0, of the second p - kMags below 0; 0 is taken behind the first half's last
+    const u32 above = one.flip ? kMags : 0;
+    auto slot_at = [&](int p) -> int {
+        return p < kMags ? static_cast<int>(above) + kMags - 1 - p : static_cast<int>(above ^ kMags) + p - kMags;
+    };
+    auto value_at = [&](int p) {
+        const u32 mag = (p < kMags ? kMags - 1 - p : p - kMags) + kFirstMag;
+        return __uint_as_float(mag << 16 | (p < kMags ? 0u : 0x80000000u));
+    };
+    const bool has_zero = tid == kMags / each - 1;
+    u32 count[each + 1];
+    u64 first = 2 * kValues, counted = 0;
+    count[each] = has_zero ? sh.zeros : 0;
+    if (count[each]) first = 2 * (tid * each + each) - 1;
 #pragma unroll
     for (int k = each - 1; k >= 0; --k) {
-        count[k] = sh.count[tid * each + k];
-        counted += count[k];
-        if (count[k]) first = tid * each + k;
+        count[k] = sh.count[slot_at(tid * each + k)];
+        if (count[k]) first = 2 * (tid * each + k);
     }
-    const u32 below = sh.count[kValues - 1];
+#pragma unroll
+    for (int k = 0; k <= each; ++k) counted += count[k];
+    const bool odd = sh.odd, below = sh.below;
     first = block_min<T>(first, sh.red);
-    if (first == kValues && !odd) {
+    if (first == 2 * kValues && !odd && !below) {
         if (tid == 0) put_draw(a, b, -1, 0.0, 0);
         return;
     }
-    const Mass mass{bin_value(static_cast<int>(first)), a.scale, a.shift};
-    if (odd || (below > 0 && (first == kValues - 1 || mass.of(bin_value(kValues - 2)) != 0))) {
+    const Mass mass{first % 2 ? 0.f : value_at(static_cast<int>(first / 2)), a.scale, a.shift};
+    if (odd || (below && (first == 2 * kValues || mass.of(value_at(kValues - 1)) != 0))) {
         __syncthreads();
-        sample_row<T, 0>(sh.row, row, b, n, m, a);
+        sample_any_row<T, uint16_t>(sh.row, row, b, n, m, a);
         return;
     }
-    u64 unused, w[each], sum = 0;
+    auto entry = [&](int k) { return k == each ? 0.f : value_at(tid * each + k); };
+    u64 unused, w[each + 1], sum = 0;
     u64 before = block_before<T>(counted, sh.red, &unused);
+    u32 partly = 0;  // bits of the entries of which not all are kept
 #pragma unroll
-    for (int k = 0; k < each; ++k) {
+    for (int k = 0; k <= each; ++k) {
         u64 keep = count[k];
         if (a.top_k > 0) keep = before >= static_cast<u64>(a.top_k) ? 0 : min(keep, a.top_k - before);
         before += count[k];
-        const int bin = tid * each + k;
-        w[k] = keep && bin < kValues - 1 ? mass.of(bin_value(bin)) : 0;
+        w[k] = 0;
+        if (keep) w[k] = mass.of(entry(k));
+        if (keep < count[k]) partly |= 1u << k;
         count[k] = static_cast<u32>(keep);
         sum += keep * w[k];
     }
@@ -704,116 +877,163 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_values_kernel(int
     u64 at = block_before<T>(sum, sh.red, &all);
     // the counts are in registers: their place takes the weights
     if (tid == 0) {
-        sh.tie_bin = -1;
+        sh.tie_slot = -1;
         sh.tie_keep = 0;
-        sh.tie_weight = 0;
+        sh.tie_weight = sh.zero_weight = 0;
     }
     __syncthreads();
-    u64 in_bin[each];
-#pragma unroll
-    for (int k = 0; k < each; ++k) in_bin[k] = sh.count[tid * each + k];
-    __syncthreads();
     const double target = a.top_p < 1.0 ? a.top_p * static_cast<double>(all) : INFINITY;
-    u64 last = 0;
 #pragma unroll
-    for (int k = 0; k < each; ++k) {
-        const int bin = tid * each + k;
+    for (int k = 0; k <= each; ++k) {
+        const int slot = k == each ? kZeroSlot : slot_at(tid * each + k);
         u64 keep = w[k] ? count[k] : 0;
         if (keep) {
-            if (static_cast<double>(at) >= target || mass.distance(bin_value(bin)) > a.dmax) {
+            if (static_cast<double>(at) >= target || mass.distance(entry(k)) > a.dmax) {
                 keep = 0;
             } else if (static_cast<double>(at + keep * w[k]) >= target) {
                 // the fewest that reach the target
                 u64 c = static_cast<u64>((target - static_cast<double>(at)) / static_cast<double>(w[k]));
                 while (c > 0 && static_cast<double>(at + (c - 1) * w[k]) >= target) --c;
                 while (static_cast<double>(at + c * w[k]) < target) ++c;
+                if (c < keep) partly |= 1u << k;
                 at += keep * w[k];
                 keep = min(keep, c);
             } else {
                 at += keep * w[k];
             }
-            if (keep) last = bin;
-            if (keep && keep < in_bin[k]) {
-                sh.tie_bin = bin;
+            if (keep && (partly >> k & 1)) {
+                sh.tie_slot = slot;
                 sh.tie_keep = static_cast<int>(keep);
                 sh.tie_weight = w[k];
                 keep = 0;
             }
         }
-        sh.weight[bin] = keep ? w[k] : 0;
+        if (k < each) sh.weight[slot] = keep ? w[k] : 0;
+        else if (has_zero) sh.zero_weight = keep ? w[k] : 0;
     }
-    last = block_max<T>(last, sh.red);
-    const int tie_bin = sh.tie_bin;
+    __syncthreads();
+    const int tie_slot = sh.tie_slot;
     const u64 tie_keep = sh.tie_keep, tie_weight = sh.tie_weight;
-    // the kept weights of each wave's part of the row; of the bin that is kept in part, the
+    // the kept weights of each wave's part of the row; of the value that is kept in part, the
     // entries, of which the first tie_keep count
     constexpr int unit = kWave * 8;
     const int part = (n + waves * unit - 1) / (waves * unit) * unit;
     const int lo = min(n, wave * part), hi = min(n, lo + part);
-    u64 s = 0, ties = 0;
-    auto add = [&](u32 bits) {
-        const int bin = value_bin(bits, bm);
-        if (static_cast<u32>(bin) <= static_cast<u32>(last)) {
-            if (bin == tie_bin) ++ties;
-            else s += sh.weight[bin];
-        }
+    u64 s = 0;
+    u32 ties = 0;
+    auto weigh_one = [&](u32 bits) -> u64 {
+        const int slot = one(bits);
+        return slot < 0 ? 0 : slot == kZeroSlot ? sh.zero_weight : sh.weight[slot];
     };
-    bits_each(row + lo, hi - lo, lane, kWave, [&](int, u32 bits) { add(bits); });
-    auto plus = [](u64 p, u64 q) { return p + q; };
-    s = block_fold<kWave>(s, nullptr, plus);
-    ties = block_fold<kWave>(ties, nullptr, plus);
-    if (lane == 0) {
-        sh.part[wave] = s;
-        sh.ties[wave] = static_cast<u32>(ties);
-    }
-    __syncthreads();
-    u64 t = 0;
-    all = 0;
-    for (int k = 0; k < waves; ++k) {
-        all += sh.part[k] + tie_weight * min<u64>(sh.ties[k], tie_keep - min(t, tie_keep));
-        t += sh.ties[k];
-    }
-    const double goal = share_of(a, b) * static_cast<double>(all);
-    u64 base = 0;
-    t = 0;
-    int from = 0;
-    for (; from < waves - 1; ++from) {
-        const u64 next = base + sh.part[from] + tie_weight * min<u64>(sh.ties[from], tie_keep - min(t, tie_keep));
-        if (static_cast<double>(next) > goal) break;
-        base = next;
-        t += sh.ties[from];
-    }
-    // the place in that part, runs of `len` entries a thread
-    const int start = from * part, end = min(n, start + part);
-    const int len = (end - start + T - 1) / T;
-    const int p0 = min(end, start + tid * len), p1 = min(end, p0 + len);
-    s = ties = 0;
-    for (int i = p0; i < p1; ++i) add(row[i]);
-    t += block_before<T>(ties, sh.red, &unused);
-    const u64 mine = s + tie_weight * min(ties, tie_keep - min(t, tie_keep));
-    base += block_before<T>(mine, sh.red, &unused);
-    if (static_cast<double>(base) <= goal && static_cast<double>(base + mine) > goal)
-        for (int i = p0; i < p1; ++i) {
-            const int bin = value_bin(row[i], bm);
-            if (static_cast<u32>(bin) > static_cast<u32>(last)) continue;
-            if (bin == tie_bin) base += t++ < tie_keep ? tie_weight : 0;
-            else base += sh.weight[bin];
-            if (static_cast<double>(base) > goal) {
-                put_draw(a, b, i, mass.distance(bin_value(bin)), all);
-                break;
+    auto is_tie = [&](u32 bits) { return one(bits) == tie_slot && tie_slot >= 0; };
+    done = lo + vec_each<kRowAhead>(row + lo, hi - lo, lane, kWave, [&](int, int i, RowVec<uint16_t>::type r) {
+        const u32x4 v = __builtin_bit_cast(u32x4, r);
+        u16x2 most = {0, 0};
+        u32 p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = slots_of(v[k], &most);
+        if (max(most[0], most[1]) < kMags) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int p0 = p[k] & 0xffff, p1 = p[k] >> 16;
+                s += sh.weight[p0] + sh.weight[p1];
+                ties += p0 == tie_slot;
+                ties += p1 == tie_slot;
+            }
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+                const u32 q = k < 4 ? (k < 2 ? v[0] : v[1]) : (k < 6 ? v[2] : v[3]);
+                const u32 bits = k % 2 ? q >> 16 : q & 0xffff;
+                s += weigh_one(bits);
+                ties += is_tie(bits);
             }
         }
+    });
+    if (done + lane < hi) {
+        s += weigh_one(row[done + lane]);
+        ties += is_tie(row[done + lane]);
+    }
+    auto plus = [](u64 p, u64 q) { return p + q; };
+    s = block_fold<kWave>(s, nullptr, plus);
+    const u64 tied = block_fold<kWave>(ties, nullptr, plus);
+    if (lane == 0) {
+        sh.part[wave] = s;
+        sh.ties[wave] = static_cast<u32>(tied);
+    }
+    __syncthreads();
+    // every wave finds the part for itself, a lane for each
+    u64 wave_s = lane < waves ? sh.part[lane] : 0, wave_t = lane < waves ? sh.ties[lane] : 0;
+    u64 upto_t = wave_t;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const u64 up = __shfl_up(upto_t, o);
+        if (lane >= o) upto_t += up;
+    }
+    const u64 t_before = upto_t - wave_t;
+    u64 upto = wave_s + tie_weight * (min(upto_t, tie_keep) - min(t_before, tie_keep));
+    const u64 own = upto;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const u64 up = __shfl_up(upto, o);
+        if (lane >= o) upto += up;
+    }
+    all = __shfl(upto, kWave - 1);
+    const double goal = share_of(a, b) * static_cast<double>(all);
+    const int from = __ffsll(__ballot(static_cast<double>(upto) > goal)) - 1;
+    u64 base = __shfl(upto - own, from), t = __shfl(t_before, from);
+    // the place in that part, a vector's entries a thread at a time
+    const int start = from * part, end = min(n, start + part);
+    for (int p = start; p < end; p += T * 8) {
+        const int p0 = p + tid * 8;
+        u32 bits[8];
+        if (p0 + 8 <= end) {
+            const u32x4 v = __builtin_bit_cast(u32x4, load_vec<uint16_t>(row + p0));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) bits[k] = k % 2 ? v[k / 2] >> 16 : v[k / 2] & 0xffff;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) bits[k] = p0 + k < end ? row[p0 + k] : 0x10000u;
+        }
+        u64 each_w[8], mine = 0;
+        u32 tie_bits = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            each_w[k] = 0;
+            if (bits[k] > 0xffff) continue;
+            each_w[k] = weigh_one(bits[k]);
+            mine += each_w[k];
+            tie_bits |= static_cast<u32>(is_tie(bits[k])) << k;
+        }
+        u64 round_t, round;
+        u64 tt = t + block_before<T>(__popc(tie_bits), sh.red, &round_t);
+        mine += tie_weight * (min(tt + __popc(tie_bits), tie_keep) - min(tt, tie_keep));
+        u64 g = base + block_before<T>(mine, sh.red, &round);
+        if (static_cast<double>(g) <= goal && static_cast<double>(g + mine) > goal) {
+            int k = 0;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (tie_bits >> q & 1) g += tt++ < tie_keep ? tie_weight : 0;
+                else g += each_w[q];
+                if (static_cast<double>(g) <= goal) k = q + 1;
+            }
+            put_draw(a, b, p0 + k, mass.distance(goodness(widen1(row[p0 + k]), m)), all);
+        }
+        base += round;
+        t += round_t;
+        if (static_cast<double>(base) > goal) return;
+    }
 }
 
-// Whether a cap is one of the values that have a bin, or is none.
-bool cap_has_bin(float cap, u32 *bits) {
+// Whether a cap is one of the values that are counted, or is none.
+bool cap_has_slot(float cap, u32 *bits) {
     *bits = 0x10000u;
     if (!isfinite(cap)) return true;
     u32 f;
     memcpy(&f, &cap, 4);
     *bits = f >> 16;
-    const int t = static_cast<int>(*bits & 0x7fff) - kFirstMag;
-    return (f & 0xffff) == 0 && ((*bits & 0x7fff) == 0 || (t >= 0 && t < kHalf));
+    const u32 mag = (*bits & 0x7fff) - kFirstMag;
+    return (f & 0xffff) == 0 && ((*bits & 0x7fff) == 0 || mag < static_cast<u32>(kMags));
 }
 
 template <typename E>
@@ -824,19 +1044,20 @@ hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
     const DrawArgs a{j.in.scale, j.top_p, j.min_p > 0.0 ? -log(j.min_p) : INFINITY, j.shift, j.top_k,
                      j.u, j.choice, j.logp};
     const E *x = static_cast<const E *>(j.in.x);
-    const bool picked = j.top_k > 0 && j.top_k <= kMaxPicked;
+    const bool picked = j.top_k > 0 && j.top_k <= kMaxPicked, caps = isfinite(j.in.cap);
     u32 cap;
     if constexpr (sizeof(E) == 2)
-        if (!picked && n > 4096 && cap_has_bin(j.in.cap, &cap)) {
-            const BinMap bm{j.in.flip >> 16, cap};
-            hipLaunchKernelGGL((sample_values_kernel<1024>), grid, dim3(1024), 0, st, n, j.in.ld, x, m, bm, a);
+        if (!picked && n > 4096 && cap_has_slot(j.in.cap, &cap)) {
+            const OneSlot one{j.in.flip >> 16, cap};
+            hipLaunchKernelGGL((sample_values_kernel<1024>), grid, dim3(1024), 0, st, n, j.in.ld, x, m, one, a);
             return hipGetLastError();
         }
-#define SAMPLE(T)                                                                                             \
-    if (picked)                                                                                               \
-        hipLaunchKernelGGL((sample_picked_kernel<T, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m,               \
-                           isfinite(j.in.cap), a);                                                            \
-    else                                                                                                      \
+#define SAMPLE(T)                                                                                               \
+    if (picked && caps)                                                                                         \
+        hipLaunchKernelGGL((sample_picked_kernel<T, true, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a);      \
+    else if (picked)                                                                                            \
+        hipLaunchKernelGGL((sample_picked_kernel<T, false, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a);     \
+    else                                                                                                        \
         hipLaunchKernelGGL((sample_kernel<T, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a)
     if (n <= 512) SAMPLE(64);
     else if (n <= 4096) SAMPLE(256);
@@ -847,14 +1068,20 @@ hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
 
 template <typename E>
 hipError_t launch_top_t(const TopJob &j, hipStream_t st) {
+    const int n = static_cast<int>(j.in.N);
+    const dim3 grid(static_cast<unsigned>(j.in.B));
+    const ScoreMap m{j.in.cap, j.in.flip};
+    const E *x = static_cast<const E *>(j.in.x);
     const float c2 = static_cast<float>(j.in.scale * 1.4426950408889634);
-#define TOP(T)                                                                                              \
-    hipLaunchKernelGGL((top_logits_kernel<T, E>), dim3(static_cast<unsigned>(j.in.B)), dim3(T), 0, st,      \
-                       static_cast<int>(j.in.N), j.in.ld, static_cast<const E *>(j.in.x),                   \
-                       ScoreMap{j.in.cap, j.in.flip}, isfinite(j.in.cap), j.in.scale, c2, j.K, j.idx,       \
-                       j.logit, j.rest)
-    if (j.in.N <= 512) TOP(64);
-    else if (j.in.N <= 4096) TOP(256);
+#define TOP(T)                                                                                                  \
+    if (isfinite(j.in.cap))                                                                                     \
+        hipLaunchKernelGGL((top_logits_kernel<T, true, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, j.in.scale, \
+                           c2, j.K, j.idx, j.logit, j.rest);                                                    \
+    else                                                                                                        \
+        hipLaunchKernelGGL((top_logits_kernel<T, false, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m,            \
+                           j.in.scale, c2, j.K, j.idx, j.logit, j.rest)
+    if (n <= 512) TOP(64);
+    else if (n <= 4096) TOP(256);
     else TOP(1024);
 #undef TOP
     return hipGetLastError();
