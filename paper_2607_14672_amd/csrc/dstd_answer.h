@@ -107,53 +107,30 @@ __device__ __forceinline__ void row_each(const E *p, int n, int tid, int count, 
 }
 
 // ------------------------------------------------------ sums over a block --
-// Every result goes to every thread; `red` holds a u64 per wave and one more.
-// The order of each is fixed.
-template <int T, typename F> __device__ u64 block_fold(u64 v, u64 *red, F f) {
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
-    if (T == kWave) return v;
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = red[threadIdx.x % (T / kWave)];
-#pragma unroll
-    for (int o = T / kWave / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
-    return v;
+// Lanes exchange by DPP moves (in the vector unit; a shuffle goes through LDS and takes
+// some 50 ns more of latency, which is what blocks of one row wait for). A lane without a
+// source keeps `none`.
+template <int kCtrl, int kRows> __device__ __forceinline__ u32 lane_move(u32 none, u32 v) {
+    return static_cast<u32>(__builtin_amdgcn_update_dpp(static_cast<int>(none), static_cast<int>(v), kCtrl, kRows,
+                                                        0xf, false));
 }
-template <int T> __device__ u64 block_max(u64 v, u64 *red) {
-    return block_fold<T>(v, red, [](u64 a, u64 b) { return a > b ? a : b; });
+template <int kCtrl, int kRows> __device__ __forceinline__ u64 lane_move(u64 none, u64 v) {
+    const u32 lo = lane_move<kCtrl, kRows>(static_cast<u32>(none), static_cast<u32>(v));
+    return static_cast<u64>(lane_move<kCtrl, kRows>(static_cast<u32>(none >> 32), static_cast<u32>(v >> 32))) << 32 |
+           lo;
 }
-template <int T> __device__ u64 block_min(u64 v, u64 *red) {
-    return block_fold<T>(v, red, [](u64 a, u64 b) { return a < b ? a : b; });
+template <int kCtrl, int kRows> __device__ __forceinline__ float lane_move(float none, float v) {
+    return __uint_as_float(lane_move<kCtrl, kRows>(__float_as_uint(none), __float_as_uint(v)));
 }
-template <int T> __device__ u64 block_add(u64 v, u64 *red) {
-    return block_fold<T>(v, red, [](u64 a, u64 b) { return a + b; });
+// The value of a lane that is the same for all.
+__device__ __forceinline__ u32 lane_value(u32 v, int lane) {
+    return static_cast<u32>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
 }
-// Sum of what lower threads have; the whole in *total.
-template <int T> __device__ u64 block_before(u64 v, u64 *red, u64 *total) {
-    u64 s = v;
-    const int lane = threadIdx.x % kWave;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const u64 up = __shfl_up(s, o);
-        if (lane >= o) s += up;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) red[threadIdx.x / kWave] = s;
-    __syncthreads();
-    // every wave forms the sums over the waves for itself
-    constexpr int waves = T / kWave;
-    u64 x = red[lane % waves];
-#pragma unroll
-    for (int o = 1; o < waves; o <<= 1) {
-        const u64 up = __shfl_up(x, o);
-        if (lane % waves >= o) x += up;
-    }
-    *total = __shfl(x, waves - 1);
-    const int wave = threadIdx.x / kWave;
-    const u64 base = __shfl(x, wave > 0 ? wave - 1 : 0);
-    return (wave > 0 ? base : 0) + s - v;
+__device__ __forceinline__ u64 lane_value(u64 v, int lane) {
+    return static_cast<u64>(lane_value(static_cast<u32>(v >> 32), lane)) << 32 | lane_value(static_cast<u32>(v), lane);
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float(lane_value(__float_as_uint(v), lane));
 }
 
 // A sum of exponentials e^(scale y): the largest y, and the sum relative to it.
@@ -169,21 +146,71 @@ __device__ __forceinline__ ExpSum exp_join(ExpSum a, ExpSum b, float c2) {
     if (!(m > -INFINITY)) return ExpSum{-INFINITY, 0.f};
     return ExpSum{m, a.s * exp_of(a.m - m, c2) + b.s * exp_of(b.m - m, c2)};
 }
-template <int T> __device__ ExpSum block_exp_sum(ExpSum v, float c2, u64 *red) {
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1)
-        v = exp_join(v, ExpSum{__shfl_xor(v.m, o), __shfl_xor(v.s, o)}, c2);
-    if (T == kWave) return v;
-    __syncthreads();
-    if (threadIdx.x % kWave == 0)
-        red[threadIdx.x / kWave] = (static_cast<u64>(__float_as_uint(v.m)) << 32) | __float_as_uint(v.s);
-    __syncthreads();
-    const u64 x = red[threadIdx.x % (T / kWave)];
-    v = ExpSum{__uint_as_float(static_cast<u32>(x >> 32)), __uint_as_float(static_cast<u32>(x))};
-#pragma unroll
-    for (int o = T / kWave / 2; o > 0; o >>= 1)
-        v = exp_join(v, ExpSum{__shfl_xor(v.m, o), __shfl_xor(v.s, o)}, c2);
+template <int kCtrl, int kRows> __device__ __forceinline__ ExpSum lane_move(ExpSum none, ExpSum v) {
+    return ExpSum{lane_move<kCtrl, kRows>(none.m, v.m), lane_move<kCtrl, kRows>(none.s, v.s)};
+}
+__device__ __forceinline__ ExpSum lane_value(ExpSum v, int lane) {
+    return ExpSum{lane_value(v.m, lane), lane_value(v.s, lane)};
+}
+
+// f over lanes up to and with the own one, of each run of kLanes (a power of two): the
+// lanes of a row of 16 by shifts, then row 0's last lane to row 1 and 2's to 3, then
+// lane 31 to the upper half.
+template <int kLanes, typename V, typename F> __device__ __forceinline__ V wave_upto(V v, V none, F f) {
+    if constexpr (kLanes > 1) v = f(v, lane_move<0x111, 0xf>(none, v));
+    if constexpr (kLanes > 2) v = f(v, lane_move<0x112, 0xf>(none, v));
+    if constexpr (kLanes > 4) v = f(v, lane_move<0x114, 0xf>(none, v));
+    if constexpr (kLanes > 8) v = f(v, lane_move<0x118, 0xf>(none, v));
+    if constexpr (kLanes > 16) v = f(v, lane_move<0x142, 0xa>(none, v));
+    if constexpr (kLanes > 32) v = f(v, lane_move<0x143, 0xc>(none, v));
     return v;
+}
+
+// f over all values of a block, to every thread, in a fixed order. `red`: a V for every
+// wave. `none`: what leaves a value as it is.
+template <int T, typename V, typename F> __device__ __forceinline__ V block_fold(V v, V none, void *red, F f) {
+    constexpr int waves = T / kWave;
+    v = lane_value(wave_upto<kWave>(v, none, f), kWave - 1);
+    if constexpr (waves > 1) {
+        V *mem = static_cast<V *>(red);
+        __syncthreads();
+        if (threadIdx.x % kWave == 0) mem[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = lane_value(wave_upto<waves>(mem[threadIdx.x % waves], none, f), waves - 1);
+    }
+    return v;
+}
+template <int T> __device__ __forceinline__ u32 block_max(u32 v, void *red) {
+    return block_fold<T>(v, 0u, red, [](u32 a, u32 b) { return a > b ? a : b; });
+}
+template <int T> __device__ __forceinline__ u32 block_min(u32 v, void *red) {
+    return block_fold<T>(v, 0xffffffffu, red, [](u32 a, u32 b) { return a < b ? a : b; });
+}
+template <int T, typename V> __device__ __forceinline__ V block_add(V v, void *red) {
+    return block_fold<T>(v, V{0}, red, [](V a, V b) { return a + b; });
+}
+template <int T> __device__ __forceinline__ ExpSum block_exp_sum(ExpSum v, float c2, void *red) {
+    return block_fold<T>(v, ExpSum{-INFINITY, 0.f}, red, [c2](ExpSum a, ExpSum b) { return exp_join(a, b, c2); });
+}
+// Sum of what lower threads have; the whole in *total.
+template <int T, typename V> __device__ __forceinline__ V block_before(V v, void *red, V *total) {
+    constexpr int waves = T / kWave;
+    auto plus = [](V a, V b) { return a + b; };
+    const V s = wave_upto<kWave>(v, V{0}, plus);
+    if constexpr (waves == 1) {
+        *total = lane_value(s, kWave - 1);
+        return s - v;
+    } else {
+        V *mem = static_cast<V *>(red);
+        __syncthreads();
+        if (threadIdx.x % kWave == kWave - 1) mem[threadIdx.x / kWave] = s;
+        __syncthreads();
+        // every wave forms the sums over the waves for itself
+        const V x = wave_upto<waves>(mem[threadIdx.x % waves], V{0}, plus);
+        *total = lane_value(x, waves - 1);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        return (wave > 0 ? lane_value(x, wave - 1) : V{0}) + s - v;
+    }
 }
 
 }  // namespace dstd

@@ -118,8 +118,7 @@ __device__ void put_loss(const KdArgs &a, int64_t b, const Entries<L> &e, const 
     }
     if (threadIdx.x % kWave == 0 && f.pr > 0.f)
         term += f.pr * (s.rest - logp0 - ((f.r.m - f.z.m) * a.inv + logf(f.r.s) - lz));
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) term += __shfl_xor(term, o);
+    term = block_add<kWave>(term, nullptr);
     if (threadIdx.x % kWave == 0) a.loss[1 + b] = s.any ? term * a.weight : 0.f;
 }
 
@@ -215,7 +214,7 @@ __global__ __launch_bounds__(T) void distill_row_kernel(KdArgs a, const L *__res
             top = fmaxf(top, x[j][k]);
         }
     }
-    top = value_of(static_cast<u32>(block_max<T>(key_of(top), sh.red)));
+    top = value_of(block_max<T>(key_of(top), sh.red));
     const float ref = top > -INFINITY ? top : 0.f;
     ExpSum r{top > -INFINITY ? 0.f : -INFINITY, 0.f};
 #pragma unroll

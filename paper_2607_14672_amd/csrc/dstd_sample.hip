@@ -25,6 +25,7 @@ constexpr int kBins = 2048;  // of a histogram over a row
 // chosen from candidates.
 template <int T> constexpr int kList = T >= 1024 ? 2048 : 1024;
 constexpr int kMaxPicked = 1024;
+constexpr int kMostSkip = 8;
 // groups of a thread's share of the row, a maximum each
 template <typename E> constexpr int kGroups = sizeof(E) == 2 ? 2 * kRowAhead : kRowAhead;
 
@@ -41,6 +42,9 @@ struct Border {
     u64 last;
     __device__ bool has(u32 key, int i) const { return key > kAbsentKey && rank_of(key, i) >= last; }
     __device__ bool all() const { return last == 0; }
+    // the same by goodness and index: y above `at`, or equal with an index up to `upto`
+    __device__ float at() const { return all() ? -INFINITY : value_of(rank_key(last)); }
+    __device__ int upto() const { return all() ? -1 : rank_index(last); }
 };
 
 // Weights of the exponentials in 64-bit integers, the largest 2^shift (shift <= 51):
@@ -78,32 +82,82 @@ struct Mass {
     __device__ u64 operator()(u32 key) const { return fixed_exp(distance(key), shift); }
 };
 struct One {
+    __device__ u64 of(float) const { return 1; }
     __device__ u64 operator()(u32) const { return 1; }
 };
 
-// The first n entries of the list in falling order, in place. Few are placed by how
-// many are larger, each against all (written back from the histogram's memory); more by
-// a bitonic network over the next power of two.
-template <int T> __device__ void sort_list(RowShared<T> &sh, int n) {
+// The first n entries of the list in falling order, in place; their high words fall as
+// bin(entry), in [0, kBins), rises. Up to 64 are placed by how many are larger. More go to
+// their bins' places (counts, and their sums over the bins), and in those by how many of
+// the bin are larger; where a bin has too many for that, all by a bitonic network.
+template <int T, typename F> __device__ void sort_list(RowShared<T> &sh, int n, F bin) {
     __syncthreads();
-    if (n <= 128) {
-        for (int i = threadIdx.x; i < n; i += T) {
-            const u64 mine = sh.list[i];
+    if (n <= kWave) {
+        if (threadIdx.x < kWave) {
+            const u64 mine = static_cast<int>(threadIdx.x) < n ? sh.list[threadIdx.x] : 0;
             int at = 0;
             for (int k = 0; k < n; ++k) at += sh.list[k] > mine;
-            sh.hist[at] = mine;
+            __builtin_amdgcn_wave_barrier();
+            if (static_cast<int>(threadIdx.x) < n) sh.list[at] = mine;
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += T) sh.list[i] = sh.hist[i];
         __syncthreads();
         return;
     }
-    int p = 256;
+    constexpr int most = 256, share = kList<T> / T, per = kBins / T;
+    u32 *count = reinterpret_cast<u32 *>(sh.hist), *first = count + kBins;
+    for (int k = threadIdx.x; k < kBins; k += T) count[k] = 0;
+    __syncthreads();
+    u64 v[share];
+    u32 place[share];  // the bin, and how many were there before
+    bool over = false;
+#pragma unroll
+    for (int e = 0; e < share; ++e) {
+        const int i = e * T + threadIdx.x;
+        if (i >= n) continue;
+        v[e] = sh.list[i];
+        const u32 at = bin(v[e]), had = atomicAdd(&count[at], 1u);
+        over |= had >= most;
+        place[e] = at << 16 | had;
+    }
+    if (!__syncthreads_or(over)) {
+        u32 mine = 0, all;
+#pragma unroll
+        for (int k = 0; k < per; ++k) mine += count[threadIdx.x * per + k];
+        u32 at = block_before<T>(mine, sh.red, &all);
+#pragma unroll
+        for (int k = 0; k < per; ++k) {
+            first[threadIdx.x * per + k] = at;
+            at += count[threadIdx.x * per + k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < share; ++e)
+            if (e * T + static_cast<int>(threadIdx.x) < n) sh.list[first[place[e] >> 16] + (place[e] & 0xffff)] = v[e];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < share; ++e) {
+            if (e * T + static_cast<int>(threadIdx.x) >= n) continue;
+            const u32 lo = first[place[e] >> 16], hi = lo + count[place[e] >> 16];
+            u32 to = lo;
+            for (u32 k = lo; k < hi; ++k) to += sh.list[k] > v[e];
+            place[e] = to;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < share; ++e)
+            if (e * T + static_cast<int>(threadIdx.x) < n) sh.list[place[e]] = v[e];
+        __syncthreads();
+        return;
+    }
+    int p = 2 * kWave;
     while (p < n) p *= 2;
     for (int i = n + threadIdx.x; i < p; i += T) sh.list[i] = 0;
+#pragma unroll 1
     for (int k = 2; k <= p; k *= 2)
+#pragma unroll 1
         for (int j = k / 2; j > 0; j /= 2) {
             __syncthreads();
+#pragma unroll 1
             for (int t = threadIdx.x; t < p / 2; t += T) {
                 const int i = 2 * t - (t & (j - 1)), o = i + j;
                 const u64 x = sh.list[i], y = sh.list[o];
@@ -114,6 +168,24 @@ template <int T> __device__ void sort_list(RowShared<T> &sh, int n) {
             }
         }
     __syncthreads();
+}
+// The list in the order of a row: bins of the range of its values.
+template <int T> __device__ void sort_by_value(RowShared<T> &sh, int n) {
+    float per = 0.f, ymax = 0.f;
+    if (n > kWave) {
+        u32 hi = 0, lo = 0;  // largest key, largest complement
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += T) {
+            hi = max(hi, rank_key(sh.list[i]));
+            lo = max(lo, ~rank_key(sh.list[i]));
+        }
+        ymax = value_of(block_max<T>(hi, sh.red));
+        lo = ~block_max<T>(lo, sh.red);
+        per = static_cast<float>(kBins / (static_cast<double>(ymax) - static_cast<double>(value_of(lo))));
+    }
+    sort_list<T>(sh, n, [&](u64 r) {
+        return static_cast<u32>(fminf((ymax - value_of(rank_key(r))) * per, kBins - 1.f));
+    });
 }
 
 // Entries of a row that `want` (key, index) holds for, into the list, as many as
@@ -153,8 +225,8 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m
     if (total == 0) return -1;
     const double target = share * static_cast<double>(total);
     // the part: the first whose end exceeds the target
-    const u64 wave_s = block_fold<kWave>(s, nullptr, [](u64 a, u64 b) { return a + b; });
-    before = __shfl(before, 0);
+    const u64 wave_s = block_add<kWave>(s, nullptr);
+    before = lane_value(before, 0);
     __syncthreads();
     if (lane == 0 && static_cast<double>(before) <= target && static_cast<double>(before + wave_s) > target) {
         sh.found[0] = before;
@@ -228,12 +300,24 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
             __syncthreads();
             for (int k = threadIdx.x; k < kBins; k += T) sh.hist[k] = 0;
             __syncthreads();
-            row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
-                const u32 key = key_of(goodness(x, m));
-                if (!in_range(key, i)) return;
-                const u64 w = weight(key);
-                if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[bin_of(key)]), w);
-            });
+            auto *hist = reinterpret_cast<unsigned long long *>(sh.hist);
+            if (shift < 0) {
+                const float at = kept.at();
+                const int upto = kept.upto();
+                row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
+                    const float y = goodness(x, m);
+                    if (!(y > at || (y == at && i <= upto))) return;
+                    const u64 w = weight.of(y);
+                    if (w) atomicAdd(&hist[static_cast<int>(fminf((ymax - y) * per, kBins - 1.f))], w);
+                });
+            } else {
+                row_each<0>(row, n, threadIdx.x, T, [&](int i, float x) {
+                    const u32 key = key_of(goodness(x, m));
+                    if (!in_range(key, i)) return;
+                    const u64 w = weight(key);
+                    if (w) atomicAdd(&hist[static_cast<int>((hi - key) >> shift)], w);
+                });
+            }
             __syncthreads();
             constexpr int per_thread = kBins / T;
             u64 mine = 0;
@@ -260,15 +344,15 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
             });
             if (count > kList<T>) {
                 u32 a = 0xffffffffu, b = 0;
-                row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
+                row_each<0>(row, n, threadIdx.x, T, [&](int i, float x) {
                     const u32 key = key_of(goodness(x, m));
                     if (in_range(key, i) && bin_of(key) == bin) {
                         a = min(a, key);
                         b = max(b, key);
                     }
                 });
-                lo = static_cast<u32>(block_min<T>(a, sh.red));
-                hi = static_cast<u32>(block_max<T>(b, sh.red));
+                lo = block_min<T>(a, sh.red);
+                hi = block_max<T>(b, sh.red);
                 if (lo == hi) {
                     // entries of one weight: the one that reaches the target
                     const u64 w = weight(lo);
@@ -291,7 +375,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
         }
         // the list in order, and the sums of its weights
         const int count = sh.count;
-        sort_list<T>(sh, count);
+        sort_by_value<T>(sh, count);
         constexpr int each = kList<T> / T;
         u64 w[each], mine = 0;
 #pragma unroll
@@ -333,7 +417,7 @@ __device__ Extremes row_extremes(RowShared<T> &sh, const E *row, int n, const Sc
             ++c;
         }
     });
-    const u32 lo = static_cast<u32>(block_min<T>(a, sh.red)), hi = static_cast<u32>(block_max<T>(b, sh.red));
+    const u32 lo = block_min<T>(a, sh.red), hi = block_max<T>(b, sh.red);
     const int count = static_cast<int>(block_add<T>(c, sh.red));
     return Extremes{value_of(lo), value_of(hi), count};
 }
@@ -386,10 +470,13 @@ __device__ __forceinline__ void sample_row(RowShared<T> &sh, const E *row, int64
     int i;
     if (kept.all() && a.dmax == INFINITY)
         i = by_index<T, kAhead>(sh, row, n, m, share, &all, [&](float y, int) { return mass.of(y); });
-    else
+    else {
+        const float at = kept.at();
+        const int upto = kept.upto();
         i = by_index<T, kAhead>(sh, row, n, m, share, &all, [&](float y, int k) -> u64 {
-            return kept.has(key_of(y), k) && mass.distance(y) <= a.dmax ? mass.of(y) : 0;
+            return (y > at || (y == at && k <= upto)) && mass.distance(y) <= a.dmax ? mass.of(y) : 0;
         });
+    }
     if (threadIdx.x == 0) put_draw(a, b, i, mass.distance(goodness(widen1(row[i]), m)), all);
 }
 // The same for rows that a faster way does not take.
@@ -400,7 +487,7 @@ __device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const
 }
 
 template <int T, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
                                                                       ScoreMap m, DrawArgs a) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
@@ -428,62 +515,70 @@ __device__ __forceinline__ float order16_value(int16_t k) {
 
 __device__ __forceinline__ float larger(float y, float best) { return y > best ? y : best; }  // not NaN
 
-// The largest goodness of each group of a thread. Entries that do not count are not
-// looked for: a NaN changes nothing, and where +inf shows up (a NaN too, in 16 bits)
-// the bound is given up.
+// The largest goodness of each group of a thread, over one of `skip` runs of 64 vectors of
+// the row. Entries that do not count are not looked for: a NaN changes nothing, and where
+// +inf shows up (a NaN too, in 16 bits) the bound is given up.
 template <int T, bool kCaps, typename E>
-__device__ __forceinline__ void group_best(const E *row, int n, const ScoreMap &m, float (&best)[kGroups<E>]) {
+__device__ __forceinline__ void group_best(const E *row, int n, int skip, const ScoreMap &m,
+                                           float (&best)[kGroups<E>]) {
+    using V = RowVec<E>;
     auto value = [&](float x) { return kCaps ? goodness(x, m) : flipped(x, m); };
+    constexpr bool packed = sizeof(E) == 2 && !kCaps;
+    const u32 flip = m.flip ? 0xffffffffu : 0;
+    i16x2 top[kRowAhead];
+#pragma unroll
+    for (int g = 0; g < kRowAhead; ++g) top[g] = i16x2{-32768, -32768};
 #pragma unroll
     for (int g = 0; g < kGroups<E>; ++g) best[g] = -INFINITY;
-    int done;
-    if constexpr (sizeof(E) == 2) {
-        if constexpr (!kCaps) {
-            const u32 flip = m.flip ? 0xffffffffu : 0;
-            i16x2 top[kRowAhead];
+    auto take = [&](int g, typename V::type r) {
+        if constexpr (packed) {
+            const u32x4 w = __builtin_bit_cast(u32x4, r);
 #pragma unroll
-            for (int g = 0; g < kRowAhead; ++g) top[g] = i16x2{-32768, -32768};
-            done = vec_each<kRowAhead>(row, n, threadIdx.x, T, [&](int g, int, typename RowVec<E>::type r) {
-                const u32x4 w = __builtin_bit_cast(u32x4, r);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top[g] = __builtin_elementwise_max(top[g], order16(w[k], flip));
-            });
-#pragma unroll
-            for (int g = 0; g < kRowAhead; ++g)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float y = order16_value(top[g][k]);
-                    best[2 * g + k] = top[g][k] >= 0x7f80 ? INFINITY : y == y ? y : -INFINITY;
-                }
+            for (int k = 0; k < 4; ++k) top[g] = __builtin_elementwise_max(top[g], order16(w[k], flip));
         } else {
-            done = vec_each<1>(row, n, threadIdx.x, T, [&](int, int, typename RowVec<E>::type r) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) best[k] = larger(value(widen1(r[k])), best[k]);
-            });
+            for (int k = 0; k < V::n; ++k) best[g] = larger(value(widen1(static_cast<E>(r[k]))), best[g]);
         }
-    } else {
-        done = vec_each<kRowAhead>(row, n, threadIdx.x, T, [&](int g, int, typename RowVec<E>::type r) {
+    };
+    const int nv = n / V::n, lane = threadIdx.x % kWave, step = T * skip;
+    int v = (threadIdx.x - lane) * skip + lane;
+#pragma unroll 1
+    for (; v + (kRowAhead - 1) * step < nv; v += kRowAhead * step) {
+        typename V::type r[kRowAhead];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) best[g] = larger(value(r[k]), best[g]);
-        });
+        for (int a = 0; a < kRowAhead; ++a) r[a] = load_vec<E>(row + static_cast<int64_t>(v + a * step) * V::n);
+#pragma unroll
+        for (int a = 0; a < kRowAhead; ++a) take(a, r[a]);
     }
-    for (int i = done + threadIdx.x; i < n; i += T)
-        best[0] = larger(value(widen1(row[i])), best[0]);
+#pragma unroll
+    for (int a = 0; a < kRowAhead - 1; ++a)
+        if (v + a * step < nv) take(a, load_vec<E>(row + static_cast<int64_t>(v + a * step) * V::n));
+    if constexpr (packed) {
+#pragma unroll
+        for (int g = 0; g < kRowAhead; ++g)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float y = order16_value(top[g][k]);
+                best[2 * g + k] = top[g][k] >= 0x7f80 ? INFINITY : y == y ? y : -INFINITY;
+            }
+    }
+    const int i = nv * V::n + threadIdx.x;
+    if (i < n) best[0] = larger(value(widen1(row[i])), best[0]);
 }
 
 template <int T, bool kCaps, typename E>
-__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, int K) {
+__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, int skip, const ScoreMap &m, int K) {
     constexpr int groups = kGroups<E>;
     float best[groups];
-    group_best<T, kCaps>(row, n, m, best);
+    group_best<T, kCaps>(row, n, skip, m, best);
     float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
     for (int g = 0; g < groups; ++g) {
         if (best[g] > -INFINITY) lo = fminf(lo, best[g]);
         hi = fmaxf(hi, best[g]);
     }
-    hi = value_of(static_cast<u32>(block_max<T>(key_of(hi), sh.red)));
-    lo = value_of(static_cast<u32>(block_min<T>(key_of(lo), sh.red)));
+    hi = value_of(block_max<T>(key_of(hi), sh.red));
+    lo = value_of(block_min<T>(key_of(lo), sh.red));
     if (hi == INFINITY || K > groups * T) return -FLT_MAX;
     if (!(hi > -INFINITY)) return INFINITY;  // nothing counts
     // bins of the range of the maxima
@@ -503,15 +598,15 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
     }
     __syncthreads();
     constexpr int each = kBins / T;
-    u64 mine = 0;
+    u32 mine = 0;
 #pragma unroll
     for (int k = 0; k < each; ++k) mine += hist[threadIdx.x * each + k];
-    u64 all;
-    u64 at = block_before<T>(mine, sh.red, &all);
-    if (at < static_cast<u64>(K) && at + mine >= static_cast<u64>(K))
+    u32 all;
+    u32 at = block_before<T>(mine, sh.red, &all);
+    if (at < static_cast<u32>(K) && at + mine >= static_cast<u32>(K))
         for (int k = 0; k < each; ++k) {
             at += hist[threadIdx.x * each + k];
-            if (at >= static_cast<u64>(K)) {
+            if (at >= static_cast<u32>(K)) {
                 sh.count = threadIdx.x * each + k;
                 break;
             }
@@ -522,7 +617,7 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
 #pragma unroll
     for (int g = 0; g < groups; ++g)
         if (bin[g] <= last) bound = fminf(bound, best[g]);
-    bound = value_of(static_cast<u32>(block_min<T>(key_of(bound), sh.red)));
+    bound = value_of(block_min<T>(key_of(bound), sh.red));
     return last < 0 ? -FLT_MAX : bound;
 }
 
@@ -556,10 +651,18 @@ __device__ __attribute__((noinline)) ExpSum sum_behind(const E *row, int n, Scor
 template <int T, bool kSum, bool kCaps, typename E>
 __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, int K, float c2,
                           ExpSum *others) {
-    float bound = -FLT_MAX;
-    if (n > kList<T>) bound = candidate_bound<T, kCaps>(sh, row, n, m, K);
     if (kSum) *others = ExpSum{-INFINITY, 0.f};
-    if (bound == INFINITY) return 0;
+    // a bound from a part of the row lets the more through: some skip K, the list holds them
+    int skip = 1;
+    while (skip < kMostSkip && 2 * skip * K <= kList<T> / 2 && n / skip >= 4 * kGroups<E> * T) skip *= 2;
+restart:
+    float bound = -FLT_MAX;
+    if (n > kList<T>) bound = candidate_bound<T, kCaps>(sh, row, n, skip, m, K);
+    if (bound == INFINITY) {
+        if (skip == 1) return 0;
+        skip = 1;
+        goto restart;
+    }
     // the bound among 16-bit keys (the lower of the two zeros)
     const u32 flip16 = m.flip ? 0xffffffffu : 0;
     const int bound16 = bound == 0.f ? -1 : order16(__float_as_uint(bound) >> 16, 0)[0];
@@ -629,11 +732,15 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     int count = sh.count;
     bool listed = bound == -FLT_MAX;  // the sum is that of the list's others alone
     if (count > kList<T>) {
+        if (skip > 1) {
+            skip = 1;
+            goto restart;
+        }
         count = pick_exactly<T, E>(sh, row, n, m, K);
         sum = 0.f;
         listed = false;
     }
-    sort_list<T>(sh, count);
+    sort_by_value<T>(sh, count);
     if (!kSum || count < K) return count;
     if (!sums) sum = 0.f;
     ExpSum s{-INFINITY, 0.f};
@@ -652,7 +759,7 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
 }
 
 template <int T, bool kCaps, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
                                                        double scale, float c2, int K,
                                                        int32_t *__restrict__ idx, float *__restrict__ logit,
                                                        float *__restrict__ rest) {
@@ -674,7 +781,7 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n,
 
 // One class from the top_k <= kMaxPicked first entries of each row.
 template <int T, bool kCaps, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int n, int64_t ld,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_picked_kernel(int n, int64_t ld,
                                                                              const E *__restrict__ x, ScoreMap m,
                                                                              DrawArgs a) {
     __shared__ RowShared<T> sh;
@@ -698,7 +805,7 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int
     u64 all;
     u64 at = block_before<T>(mine, sh.red, &all);
     const double target = a.top_p < 1.0 ? a.top_p * static_cast<double>(all) : INFINITY;
-    u64 keeps = 0;
+    u32 keeps = 0;
 #pragma unroll
     for (int k = 0; k < each; ++k) {
         if (first + k < count && static_cast<double>(at) < target &&
@@ -718,7 +825,10 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int
 #pragma unroll
     for (int k = 0; k < each; ++k)
         if (first + k < count) sh.list[first + k] = back[k];
-    sort_list<T>(sh, count);
+    const float per = static_cast<float>(kBins) / static_cast<float>(n);
+    sort_list<T>(sh, count, [&](u64 r) {
+        return static_cast<u32>(fminf(static_cast<float>(~static_cast<u32>(r >> 32)) * per, kBins - 1.f));
+    });
     mine = 0;
 #pragma unroll
     for (int k = 0; k < each; ++k) {
@@ -836,7 +946,7 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
     };
     const bool has_zero = tid == kMags / each - 1;
     u32 count[each + 1];
-    u64 first = 2 * kValues, counted = 0;
+    u32 first = 2 * kValues, counted = 0;
     count[each] = has_zero ? sh.zeros : 0;
     if (count[each]) first = 2 * (tid * each + each) - 1;
 #pragma unroll
@@ -859,20 +969,23 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
         return;
     }
     auto entry = [&](int k) { return k == each ? 0.f : value_at(tid * each + k); };
-    u64 unused, w[each + 1], sum = 0;
-    u64 before = block_before<T>(counted, sh.red, &unused);
-    u32 partly = 0;  // bits of the entries of which not all are kept
+    // Values in turn, one at a time: nothing but the counts stays in registers, a weight
+    // is formed again where it is needed again.
+    u64 sum = 0;
+    u32 counts;
+    u32 before = block_before<T>(counted, sh.red, &counts);
+    u32 partly = 0;  // bits of the values of which not all entries are kept
 #pragma unroll
     for (int k = 0; k <= each; ++k) {
-        u64 keep = count[k];
-        if (a.top_k > 0) keep = before >= static_cast<u64>(a.top_k) ? 0 : min(keep, a.top_k - before);
+        __builtin_amdgcn_sched_barrier(0);
+        u32 keep = count[k];
+        if (a.top_k > 0) keep = before >= static_cast<u32>(a.top_k) ? 0 : min(keep, a.top_k - before);
         before += count[k];
-        w[k] = 0;
-        if (keep) w[k] = mass.of(entry(k));
         if (keep < count[k]) partly |= 1u << k;
-        count[k] = static_cast<u32>(keep);
-        sum += keep * w[k];
+        count[k] = keep;
+        if (keep) sum += static_cast<u64>(keep) * mass.of(entry(k));
     }
+    __builtin_amdgcn_sched_barrier(0);
     u64 all;
     u64 at = block_before<T>(sum, sh.red, &all);
     // the counts are in registers: their place takes the weights
@@ -883,33 +996,39 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
     }
     __syncthreads();
     const double target = a.top_p < 1.0 ? a.top_p * static_cast<double>(all) : INFINITY;
+    u64 tie_at = 0, tie_w = 0;
+    u32 tie_keeps = 0;
+    int tie = -1;  // the value of which some entries are kept
 #pragma unroll
     for (int k = 0; k <= each; ++k) {
-        const int slot = k == each ? kZeroSlot : slot_at(tid * each + k);
-        u64 keep = w[k] ? count[k] : 0;
-        if (keep) {
-            if (static_cast<double>(at) >= target || mass.distance(entry(k)) > a.dmax) {
-                keep = 0;
-            } else if (static_cast<double>(at + keep * w[k]) >= target) {
-                // the fewest that reach the target
-                u64 c = static_cast<u64>((target - static_cast<double>(at)) / static_cast<double>(w[k]));
-                while (c > 0 && static_cast<double>(at + (c - 1) * w[k]) >= target) --c;
-                while (static_cast<double>(at + c * w[k]) < target) ++c;
-                if (c < keep) partly |= 1u << k;
-                at += keep * w[k];
-                keep = min(keep, c);
-            } else {
-                at += keep * w[k];
+        __builtin_amdgcn_sched_barrier(0);
+        u64 w = 0;
+        if (count[k] && static_cast<double>(at) < target && mass.distance(entry(k)) <= a.dmax) {
+            w = mass.of(entry(k));
+            const u64 next = at + count[k] * w;
+            if (static_cast<double>(next) >= target || (partly >> k & 1)) {
+                tie = k;
+                tie_at = at;
+                tie_w = w;
+                tie_keeps = count[k];
             }
-            if (keep && (partly >> k & 1)) {
-                sh.tie_slot = slot;
-                sh.tie_keep = static_cast<int>(keep);
-                sh.tie_weight = w[k];
-                keep = 0;
-            }
+            at = next;
         }
-        if (k < each) sh.weight[slot] = keep ? w[k] : 0;
-        else if (has_zero) sh.zero_weight = keep ? w[k] : 0;
+        if (k < each) sh.weight[slot_at(tid * each + k)] = tie == k ? 0 : w;
+        else if (has_zero) sh.zero_weight = tie == k ? 0 : w;
+    }
+    if (tie >= 0 && tie_w) {
+        // the fewest of its entries that reach the target; all of it may be
+        u64 keep = tie_keeps;
+        if (static_cast<double>(tie_at + keep * tie_w) >= target) {
+            u64 c = static_cast<u64>((target - static_cast<double>(tie_at)) / static_cast<double>(tie_w));
+            while (c > 0 && static_cast<double>(tie_at + (c - 1) * tie_w) >= target) --c;
+            while (static_cast<double>(tie_at + c * tie_w) < target) ++c;
+            keep = min(keep, c);
+        }
+        sh.tie_slot = tie == each ? kZeroSlot : slot_at(tid * each + tie);
+        sh.tie_keep = static_cast<int>(keep);
+        sh.tie_weight = tie_w;
     }
     __syncthreads();
     const int tie_slot = sh.tie_slot;
@@ -954,59 +1073,56 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
         s += weigh_one(row[done + lane]);
         ties += is_tie(row[done + lane]);
     }
-    auto plus = [](u64 p, u64 q) { return p + q; };
-    s = block_fold<kWave>(s, nullptr, plus);
-    const u64 tied = block_fold<kWave>(ties, nullptr, plus);
+    s = block_add<kWave>(s, nullptr);
+    const u32 tied = block_add<kWave>(ties, nullptr);
     if (lane == 0) {
         sh.part[wave] = s;
-        sh.ties[wave] = static_cast<u32>(tied);
+        sh.ties[wave] = tied;
     }
     __syncthreads();
     // every wave finds the part for itself, a lane for each
-    u64 wave_s = lane < waves ? sh.part[lane] : 0, wave_t = lane < waves ? sh.ties[lane] : 0;
-    u64 upto_t = wave_t;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const u64 up = __shfl_up(upto_t, o);
-        if (lane >= o) upto_t += up;
-    }
-    const u64 t_before = upto_t - wave_t;
-    u64 upto = wave_s + tie_weight * (min(upto_t, tie_keep) - min(t_before, tie_keep));
-    const u64 own = upto;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const u64 up = __shfl_up(upto, o);
-        if (lane >= o) upto += up;
-    }
-    all = __shfl(upto, kWave - 1);
+    auto plus = [](u64 p, u64 q) { return p + q; };
+    const u64 wave_t = sh.ties[lane % waves];
+    const u64 t_before = wave_upto<waves>(wave_t, u64{0}, plus) - wave_t;
+    const u64 own = sh.part[lane % waves] +
+                    tie_weight * (min(t_before + wave_t, tie_keep) - min(t_before, tie_keep));
+    const u64 upto = wave_upto<waves>(own, u64{0}, plus);
+    all = lane_value(upto, waves - 1);
     const double goal = share_of(a, b) * static_cast<double>(all);
-    const int from = __ffsll(__ballot(static_cast<double>(upto) > goal)) - 1;
-    u64 base = __shfl(upto - own, from), t = __shfl(t_before, from);
+    const int from = __builtin_amdgcn_readfirstlane(
+        __ffsll(__ballot(lane < waves && static_cast<double>(upto) > goal)) - 1);
+    u64 base = lane_value(upto - own, from), t = lane_value(t_before, from);
     // the place in that part, a vector's entries a thread at a time
     const int start = from * part, end = min(n, start + part);
     for (int p = start; p < end; p += T * 8) {
         const int p0 = p + tid * 8;
-        u32 bits[8];
-        if (p0 + 8 <= end) {
-            const u32x4 v = __builtin_bit_cast(u32x4, load_vec<uint16_t>(row + p0));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) bits[k] = k % 2 ? v[k / 2] >> 16 : v[k / 2] & 0xffff;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) bits[k] = p0 + k < end ? row[p0 + k] : 0x10000u;
-        }
         u64 each_w[8], mine = 0;
         u32 tie_bits = 0;
+        u32x4 v = {0, 0, 0, 0};
+        u16x2 most = {0, 0};
+        u32 q[4];
+        const int have = min(8, end - p0);
+        if (have == 8) v = __builtin_bit_cast(u32x4, load_vec<uint16_t>(row + p0));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            each_w[k] = 0;
-            if (bits[k] > 0xffff) continue;
-            each_w[k] = weigh_one(bits[k]);
-            mine += each_w[k];
-            tie_bits |= static_cast<u32>(is_tie(bits[k])) << k;
+        for (int k = 0; k < 4; ++k) q[k] = slots_of(v[k], &most);
+        if (have == 8 && max(most[0], most[1]) < kMags) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int slot = k % 2 ? q[k / 2] >> 16 : q[k / 2] & 0xffff;
+                each_w[k] = sh.weight[slot];
+                tie_bits |= static_cast<u32>(slot == tie_slot) << k;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                each_w[k] = k < have ? weigh_one(row[p0 + k]) : 0;
+                if (k < have) tie_bits |= static_cast<u32>(is_tie(row[p0 + k])) << k;
+            }
         }
-        u64 round_t, round;
-        u64 tt = t + block_before<T>(__popc(tie_bits), sh.red, &round_t);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mine += each_w[k];
+        u32 round_t;
+        u64 round, tt = t + block_before<T>(static_cast<u32>(__popc(tie_bits)), sh.red, &round_t);
         mine += tie_weight * (min(tt + __popc(tie_bits), tie_keep) - min(tt, tie_keep));
         u64 g = base + block_before<T>(mine, sh.red, &round);
         if (static_cast<double>(g) <= goal && static_cast<double>(g + mine) > goal) {
