@@ -25,7 +25,6 @@ constexpr int kBins = 2048;  // of a histogram over a row
 // chosen from candidates.
 template <int T> constexpr int kList = T >= 1024 ? 2048 : 1024;
 constexpr int kMaxPicked = 1024;
-constexpr int kMostSkip = 8;
 // groups of a thread's share of the row, a maximum each
 template <typename E> constexpr int kGroups = sizeof(E) == 2 ? 2 * kRowAhead : kRowAhead;
 
@@ -515,12 +514,11 @@ __device__ __forceinline__ float order16_value(int16_t k) {
 
 __device__ __forceinline__ float larger(float y, float best) { return y > best ? y : best; }  // not NaN
 
-// The largest goodness of each group of a thread, over one of `skip` runs of 64 vectors of
-// the row. Entries that do not count are not looked for: a NaN changes nothing, and where
-// +inf shows up (a NaN too, in 16 bits) the bound is given up.
+// The largest goodness of each group of a thread. Entries that do not count are not
+// looked for: a NaN changes nothing, and where +inf shows up (a NaN too, in 16 bits)
+// the bound is given up.
 template <int T, bool kCaps, typename E>
-__device__ __forceinline__ void group_best(const E *row, int n, int skip, const ScoreMap &m,
-                                           float (&best)[kGroups<E>]) {
+__device__ __forceinline__ void group_best(const E *row, int n, const ScoreMap &m, float (&best)[kGroups<E>]) {
     using V = RowVec<E>;
     auto value = [&](float x) { return kCaps ? goodness(x, m) : flipped(x, m); };
     constexpr bool packed = sizeof(E) == 2 && !kCaps;
@@ -540,19 +538,7 @@ __device__ __forceinline__ void group_best(const E *row, int n, int skip, const 
             for (int k = 0; k < V::n; ++k) best[g] = larger(value(widen1(static_cast<E>(r[k]))), best[g]);
         }
     };
-    const int nv = n / V::n, lane = threadIdx.x % kWave, step = T * skip;
-    int v = (threadIdx.x - lane) * skip + lane;
-#pragma unroll 1
-    for (; v + (kRowAhead - 1) * step < nv; v += kRowAhead * step) {
-        typename V::type r[kRowAhead];
-#pragma unroll
-        for (int a = 0; a < kRowAhead; ++a) r[a] = load_vec<E>(row + static_cast<int64_t>(v + a * step) * V::n);
-#pragma unroll
-        for (int a = 0; a < kRowAhead; ++a) take(a, r[a]);
-    }
-#pragma unroll
-    for (int a = 0; a < kRowAhead - 1; ++a)
-        if (v + a * step < nv) take(a, load_vec<E>(row + static_cast<int64_t>(v + a * step) * V::n));
+    const int done = vec_each<kRowAhead>(row, n, threadIdx.x, T, [&](int g, int, typename V::type r) { take(g, r); });
     if constexpr (packed) {
 #pragma unroll
         for (int g = 0; g < kRowAhead; ++g)
@@ -562,15 +548,15 @@ __device__ __forceinline__ void group_best(const E *row, int n, int skip, const 
                 best[2 * g + k] = top[g][k] >= 0x7f80 ? INFINITY : y == y ? y : -INFINITY;
             }
     }
-    const int i = nv * V::n + threadIdx.x;
+    const int i = done + threadIdx.x;
     if (i < n) best[0] = larger(value(widen1(row[i])), best[0]);
 }
 
 template <int T, bool kCaps, typename E>
-__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, int skip, const ScoreMap &m, int K) {
+__device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, int K) {
     constexpr int groups = kGroups<E>;
     float best[groups];
-    group_best<T, kCaps>(row, n, skip, m, best);
+    group_best<T, kCaps>(row, n, m, best);
     float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
     for (int g = 0; g < groups; ++g) {
@@ -652,17 +638,9 @@ template <int T, bool kSum, bool kCaps, typename E>
 __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, int K, float c2,
                           ExpSum *others) {
     if (kSum) *others = ExpSum{-INFINITY, 0.f};
-    // a bound from a part of the row lets the more through: some skip K, the list holds them
-    int skip = 1;
-    while (skip < kMostSkip && 2 * skip * K <= kList<T> / 2 && n / skip >= 4 * kGroups<E> * T) skip *= 2;
-restart:
     float bound = -FLT_MAX;
-    if (n > kList<T>) bound = candidate_bound<T, kCaps>(sh, row, n, skip, m, K);
-    if (bound == INFINITY) {
-        if (skip == 1) return 0;
-        skip = 1;
-        goto restart;
-    }
+    if (n > kList<T>) bound = candidate_bound<T, kCaps>(sh, row, n, m, K);
+    if (bound == INFINITY) return 0;
     // the bound among 16-bit keys (the lower of the two zeros)
     const u32 flip16 = m.flip ? 0xffffffffu : 0;
     const int bound16 = bound == 0.f ? -1 : order16(__float_as_uint(bound) >> 16, 0)[0];
@@ -732,10 +710,6 @@ restart:
     int count = sh.count;
     bool listed = bound == -FLT_MAX;  // the sum is that of the list's others alone
     if (count > kList<T>) {
-        if (skip > 1) {
-            skip = 1;
-            goto restart;
-        }
         count = pick_exactly<T, E>(sh, row, n, m, K);
         sum = 0.f;
         listed = false;
