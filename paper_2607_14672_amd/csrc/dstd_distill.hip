@@ -162,15 +162,18 @@ __global__ __launch_bounds__(T) void distill_row_kernel(KdArgs a, const L *__res
     const int tid = threadIdx.x, lane = tid % kWave, n = a.N;
     const float *row = a.t + b * a.ld_t;
     f32x4 x[V];
-    // vector v of the row is v = tid + T j; the last may be cut
+    // vector v of the row is v = tid + T j; the last may be cut, what is behind it is taken
+    // for silent
+    int behind = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int i = (tid + T * j) * 4;
         if (i + 4 <= n) {
             x[j] = *reinterpret_cast<const f32x4_any *>(row + i);
         } else {
+            behind += 4 - max(0, n - i);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[j][k] = i + k < n ? row[i + k] : 0.f;
+            for (int k = 0; k < 4; ++k) x[j][k] = i + k < n ? row[i + k] : INFINITY;
         }
     }
     for (int k = tid; k < (n + 31) / 32; k += T) sh.bits[k] = 0;
@@ -197,48 +200,63 @@ __global__ __launch_bounds__(T) void distill_row_kernel(KdArgs a, const L *__res
         if (lane == 0) sh.sums = s;
     }
     __syncthreads();
-    // the others' largest y, their exponentials relative to it, and their sum. An
-    // exponential takes the place of its time, negated where the neuron did not fire.
+    // The others' largest y, their exponentials relative to it, which take the places of
+    // the times, and their sum. Silent neurons are counted: each adds what t_cap adds, and
+    // the 0 in its place is its gradient. So do the named classes' places hold 0.
+    int silent = -behind;
     float top = -INFINITY;
-    u32 silent[(V * 4 + 31) / 32] = {};
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int v = tid + T * j;
-        const u32 named = v * 4 < n ? sh.bits[v / 8] >> (v % 8 * 4) : 15u;
+        const u32 named = v * 4 < n ? sh.bits[v / 8] >> (v % 8 * 4) & 15u : 0u;
+        if (named) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (named >> k & 1) {
+                    x[j][k] = INFINITY;
+                    --silent;
+                }
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const bool fired = isfinite(x[j][k]);
-            const bool out = (named >> k & 1) || v * 4 + k >= n;
-            if (!fired) silent[(j * 4 + k) / 32] |= 1u << (j * 4 + k) % 32;
-            x[j][k] = out ? -INFINITY : -(fired ? x[j][k] : a.t_cap);
+            silent += !fired;
+            x[j][k] = fired ? -x[j][k] : -INFINITY;
             top = fmaxf(top, x[j][k]);
         }
     }
+    if (silent > 0) top = fmaxf(top, -a.t_cap);
     top = value_of(block_max<T>(key_of(top), sh.red));
-    const float ref = top > -INFINITY ? top : 0.f;
-    ExpSum r{top > -INFINITY ? 0.f : -INFINITY, 0.f};
+    // 2^(c2 y - kb); kb may leave fp32 where times are huge, then by the difference itself
+    const float ref = top > -INFINITY ? top : 0.f, kb = ref * a.c2;
+    const bool fits = isfinite(kb);
+    float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            x[j][k] = exp_of(x[j][k] - ref, a.c2);
-            r.s += x[j][k];
+            x[j][k] = __builtin_amdgcn_exp2f(fits ? fmaf(x[j][k], a.c2, -kb) : (x[j][k] - ref) * a.c2);
+            sum += x[j][k];
         }
-    r = block_exp_sum<T>(r, a.c2, sh.red);
-    r.m = top;
+    // what rounding kb took off; 2^-kb is what a silent neuron's term is relative to, too
+    const float fix = fits ? __builtin_amdgcn_exp2f(fmaf(ref, -a.c2, kb)) : 1.f;
+    if (silent > 0)
+        sum += static_cast<float>(silent) *
+               __builtin_amdgcn_exp2f(fits ? fmaf(-a.t_cap, a.c2, -kb) : (-a.t_cap - ref) * a.c2);
+    sum = block_add<T>(sum, sh.red) * fix;
+    const ExpSum r{top, top > -INFINITY ? sum : 0.f};
     const RecordSums s = sh.sums;
     const RowFactors f(s, r, a.c2);
-    if (tid < kWave) put_loss(a, b, e, s, f);
-    if (!a.grad) return;
-    const float w = s.any ? -a.weight * a.inv * f.other : 0.f;
+    if (!a.grad) {
+        if (tid < kWave) put_loss(a, b, e, s, f);
+        return;
+    }
+    const float w = s.any ? -a.weight * a.inv * f.other * fix : 0.f;
     float *grad = a.grad + b * a.ld_g;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int i = (tid + T * j) * 4;
-        f32x4 g;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            g[k] = silent[(j * 4 + k) / 32] >> ((j * 4 + k) % 32) & 1 ? 0.f : x[j][k] * w;
+        const f32x4 g = x[j] * w;
         if (i + 4 <= n) {
             f32x4_any *o = reinterpret_cast<f32x4_any *>(grad + i);
             *o = a.accumulate ? *o + g : g;
@@ -248,6 +266,7 @@ __global__ __launch_bounds__(T) void distill_row_kernel(KdArgs a, const L *__res
                 if (i + k < n) grad[i + k] = a.accumulate ? grad[i + k] + g[k] : g[k];
         }
     }
+    if (tid < kWave) put_loss(a, b, e, s, f);
     __syncthreads();
     if (tid < kWave && s.any) put_named(a, b, e, first, s, f, sh.list, sh.logit, sh.twice != 0, 0, n);
 }
