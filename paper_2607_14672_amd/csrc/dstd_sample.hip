@@ -36,6 +36,8 @@ template <int T> struct RowShared {
     int count, seen;
 };
 
+__device__ __forceinline__ float larger(float y, float best) { return y > best ? y : best; }  // not NaN
+
 // What is kept of a row: all up to a place in its order.
 struct Border {
     u64 last;
@@ -205,19 +207,18 @@ __device__ int collect(RowShared<T> &sh, const E *row, int n, const ScoreMap &m,
     return sh.count;
 }
 
-// First index where the sum of weight(goodness, index) up to it exceeds share times
-// the whole sum (returned in *all), -1 where that is 0. The waves sum a part of
-// the row each; the part that holds the place is read again.
+// First index where the sum of weight(score, index) up to it exceeds share times the whole
+// sum (returned in *all), -1 where that is 0. The waves sum a part of the row each; the
+// part that holds the place is read again.
 template <int T, int kAhead, typename E, typename F>
-__device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, double share, u64 *all,
-                        F weight) {
+__device__ int by_index(RowShared<T> &sh, const E *row, int n, double share, u64 *all, F weight) {
     constexpr int waves = T / kWave, unit = kWave * RowVec<E>::n;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int part = (n + waves * unit - 1) / (waves * unit) * unit;
     const int lo = min(n, wave * part), hi = min(n, lo + part);
     u64 s = 0;
     row_each<kAhead>(row + lo, hi - lo, lane, kWave,
-                [&](int i, float x) { s += weight(goodness(x, m), lo + i); });
+                [&](int i, float x) { s += weight(x, lo + i); });
     u64 total;
     u64 before = block_before<T>(s, sh.red, &total);
     *all = total;
@@ -242,11 +243,11 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, const ScoreMap &m
         if (a + vn <= last) {
             const auto r = load_vec<E>(row + a);
 #pragma unroll
-            for (int k = 0; k < vn; ++k) w[k] = weight(goodness(widen1(static_cast<E>(r[k])), m), a + k);
+            for (int k = 0; k < vn; ++k) w[k] = weight(widen1(static_cast<E>(r[k])), a + k);
         } else {
 #pragma unroll
             for (int k = 0; k < vn; ++k)
-                w[k] = a + k < last ? weight(goodness(widen1(row[a + k]), m), a + k) : 0;
+                w[k] = a + k < last ? weight(widen1(row[a + k]), a + k) : 0;
         }
 #pragma unroll
         for (int k = 0; k < vn; ++k) mine += w[k];
@@ -284,7 +285,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                            float ymax, double span, W weight, u64 target_n, double share) {
     u32 lo = 0, hi = 0;   // keys of the bin
     int shift = -1;       // bins of 2^shift keys; -1: bins of the range of values
-    const double range = fmin(static_cast<double>(ymax) - static_cast<double>(ymin), span);
+    const double range = fmin(static_cast<double>(ymax) - static_cast<double>(ymin), span);  // ymin may be -inf
     const float per = static_cast<float>(kBins / range);
     u64 base = 0;
     double target = static_cast<double>(target_n);
@@ -361,8 +362,8 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                     // k entries of that key lie before it
                     u64 all_ties;
                     const u32 tie = lo;
-                    auto is_tie = [&](float y, int i) -> u64 { return key_of(y) == tie && kept.has(tie, i); };
-                    const int i = by_index<T, kAhead>(sh, row, n, m, (static_cast<double>(k) + 0.5) / count, &all_ties, is_tie);
+                    auto is_tie = [&](float x, int i) -> u64 { return key_of(goodness(x, m)) == tie && kept.has(tie, i); };
+                    const int i = by_index<T, 0>(sh, row, n, (static_cast<double>(k) + 0.5) / count, &all_ties, is_tie);
                     return Border{rank_of(lo, i)};
                 }
                 shift = 0;
@@ -421,12 +422,19 @@ __device__ Extremes row_extremes(RowShared<T> &sh, const E *row, int n, const Sc
     return Extremes{value_of(lo), value_of(hi), count};
 }
 
-// The K first entries of a row, K of them at least. This and other ways that rows in
-// earnest seldom take are not inlined: they would take registers from the loops of those.
-template <int T, typename E>
+// The K first entries of a row; the shortest prefix of what is kept with at least `share`
+// of its weight. These and other ways that not every row goes are not inlined: they would
+// take registers from the loops that all go through.
+template <int T, int kAhead, typename E>
 __device__ __attribute__((noinline)) Border pick_count(RowShared<T> &sh, const E *row, int n, ScoreMap m, Extremes ex,
                                                        int K) {
-    return by_order<T, 0>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
+    return by_order<T, kAhead>(sh, row, n, m, Border{0}, ex.ymin, ex.ymax, INFINITY, One{}, K, 0.0);
+}
+template <int T, int kAhead, typename E>
+__device__ __attribute__((noinline)) Border pick_mass(RowShared<T> &sh, const E *row, int n, ScoreMap m, Border kept,
+                                                      float ymin, Mass mass, double share) {
+    return by_order<T, kAhead>(sh, row, n, m, kept, ymin, static_cast<float>(mass.top),
+                               0.6931471805599453 * (mass.shift + 1) / mass.scale, mass, 0, share);
 }
 
 // What a draw goes by, and where it is written.
@@ -448,10 +456,29 @@ __device__ __forceinline__ double share_of(const DrawArgs &a, int64_t b) {
     return fmin(fmax(static_cast<double>(a.u[b]), 0.0), 1.0 - 0x1p-24);
 }
 
+// The draw among what is kept of a row.
+template <int T, int kAhead, typename E, typename G>
+__device__ __forceinline__ void draw_kept(RowShared<T> &sh, const E *row, int64_t b, int n, const Mass &mass,
+                                          const Border &kept, const DrawArgs &a, G good) {
+    u64 all;
+    int i;
+    if (kept.all() && a.dmax == INFINITY) {
+        i = by_index<T, kAhead>(sh, row, n, share_of(a, b), &all, [&](float x, int) { return mass.of(good(x)); });
+    } else {
+        const float at = kept.at();
+        const int upto = kept.upto();
+        i = by_index<T, kAhead>(sh, row, n, share_of(a, b), &all, [&](float x, int k) -> u64 {
+            const float y = good(x);
+            return (y > at || (y == at && k <= upto)) && mass.distance(y) <= a.dmax ? mass.of(y) : 0;
+        });
+    }
+    if (threadIdx.x == 0) put_draw(a, b, i, mass.distance(good(widen1(row[i]))), all);
+}
+
 // One class of a row by its definition, whatever the values.
 template <int T, int kAhead, typename E>
-__device__ __forceinline__ void sample_row(RowShared<T> &sh, const E *row, int64_t b, int n, const ScoreMap &m,
-                                           const DrawArgs &a) {
+__device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const E *row, int64_t b, int n, ScoreMap m,
+                                                         DrawArgs a) {
     const Extremes ex = row_extremes<T, kAhead>(sh, row, n, m);
     if (ex.count == 0) {
         if (threadIdx.x == 0) put_draw(a, b, -1, 0.0, 0);
@@ -459,38 +486,35 @@ __device__ __forceinline__ void sample_row(RowShared<T> &sh, const E *row, int64
     }
     const Mass mass{ex.ymax, a.scale, a.shift};
     Border kept{0};
-    if (a.top_k > 0 && a.top_k < ex.count)
-        kept = pick_count<T, E>(sh, row, n, m, ex, a.top_k);
-    if (a.top_p < 1.0)
-        kept = by_order<T, kAhead>(sh, row, n, m, kept, ex.ymin, ex.ymax,
-                                   0.6931471805599453 * (a.shift + 1) / a.scale, mass, 0, a.top_p);
-    u64 all;
-    const double share = share_of(a, b);
-    int i;
-    if (kept.all() && a.dmax == INFINITY)
-        i = by_index<T, kAhead>(sh, row, n, m, share, &all, [&](float y, int) { return mass.of(y); });
-    else {
-        const float at = kept.at();
-        const int upto = kept.upto();
-        i = by_index<T, kAhead>(sh, row, n, m, share, &all, [&](float y, int k) -> u64 {
-            return (y > at || (y == at && k <= upto)) && mass.distance(y) <= a.dmax ? mass.of(y) : 0;
-        });
-    }
-    if (threadIdx.x == 0) put_draw(a, b, i, mass.distance(goodness(widen1(row[i]), m)), all);
-}
-// The same for rows that a faster way does not take.
-template <int T, typename E>
-__device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const E *row, int64_t b, int n, ScoreMap m,
-                                                         DrawArgs a) {
-    sample_row<T, 0>(sh, row, b, n, m, a);
+    if (a.top_k > 0 && a.top_k < ex.count) kept = pick_count<T, kAhead, E>(sh, row, n, m, ex, a.top_k);
+    if (a.top_p < 1.0) kept = pick_mass<T, kAhead, E>(sh, row, n, m, kept, ex.ymin, mass, a.top_p);
+    draw_kept<T, kAhead>(sh, row, b, n, mass, kept, a, [&](float x) { return goodness(x, m); });
 }
 
-template <int T, typename E>
+// Rows whose largest entry is found without a look at those that do not count: -inf and
+// NaN weigh nothing as they are (min(NaN, .) is the other), +inf shows up as the largest.
+template <int T, bool kCaps, typename E>
 __global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
                                                                       ScoreMap m, DrawArgs a) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
-    sample_row<T, 1>(sh, x + b * ld, b, n, m, a);
+    const E *row = x + b * ld;
+    auto good = [&](float v) { return kCaps ? goodness(v, m) : flipped(v, m); };
+    float top = -INFINITY;
+    row_each<kRowAhead>(row, n, threadIdx.x, T, [&](int, float v) { top = larger(good(v), top); });
+    top = value_of(block_max<T>(key_of(top), sh.red));
+    if (top == INFINITY || (a.top_k > 0 && a.top_k < n)) {
+        sample_any_row<T, 1, E>(sh, row, b, n, m, a);
+        return;
+    }
+    if (!(top > -INFINITY)) {
+        if (threadIdx.x == 0) put_draw(a, b, -1, 0.0, 0);
+        return;
+    }
+    const Mass mass{top, a.scale, a.shift};
+    Border kept{0};
+    if (a.top_p < 1.0) kept = pick_mass<T, 1, E>(sh, row, n, m, kept, -INFINITY, mass, a.top_p);
+    draw_kept<T, 1>(sh, row, b, n, mass, kept, a, good);
 }
 
 // Candidates for the K first entries of a row's order: all that reach a bound which K
@@ -511,8 +535,6 @@ __device__ __forceinline__ float order16_value(int16_t k) {
     const u32 bits = static_cast<uint16_t>(k ^ ((k >> 15) & 0x7fff));
     return __uint_as_float(bits << 16);
 }
-
-__device__ __forceinline__ float larger(float y, float best) { return y > best ? y : best; }  // not NaN
 
 // The largest goodness of each group of a thread. Entries that do not count are not
 // looked for: a NaN changes nothing, and where +inf shows up (a NaN too, in 16 bits)
@@ -614,7 +636,7 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
 // over all entries behind a place in the row's order, relative to the largest of them.
 template <int T, typename E>
 __device__ __attribute__((noinline)) int pick_exactly(RowShared<T> &sh, const E *row, int n, ScoreMap m, int K) {
-    const Border kept = pick_count<T, E>(sh, row, n, m, row_extremes<T, 0>(sh, row, n, m), K);
+    const Border kept = pick_count<T, 0, E>(sh, row, n, m, row_extremes<T, 0>(sh, row, n, m), K);
     return collect<T, 0>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
 }
 template <int T, typename E>
@@ -825,8 +847,9 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_picked_kernel(int
 // ---------------------------------------------- rows of few distinct values --
 // bf16 scores of a magnitude in [2^-24, 2^8) take 2 * 4096 values: how often each occurs
 // says which are kept and what they weigh, with an exponential a value instead of one an
-// entry. Zeros are counted apart, and so is what is larger with a goodness below 0, which
-// weighs nothing (or the row is drawn from by its definition, as one with any other value).
+// entry. Zeros are counted apart; the few values nearer to 0 are listed one by one; what is
+// larger with a goodness below 0 has to weigh nothing. Other rows are drawn from by their
+// definition.
 constexpr int kMags = 4096, kFirstMag = 0x3380, kValues = 2 * kMags;
 using u16x2 = uint16_t __attribute__((ext_vector_type(2)));
 
@@ -837,6 +860,7 @@ __device__ __forceinline__ u32 slots_of(u32 bits, u16x2 *most) {
     return __builtin_bit_cast(u32, mag) | (bits >> 3 & 0x10001000u);
 }
 
+constexpr int kSmall = 16;
 template <int T> struct ValueShared {
     u64 red[T / kWave + 1];
     union {
@@ -846,11 +870,18 @@ template <int T> struct ValueShared {
     };
     u64 part[T / kWave];
     u32 ties[T / kWave];
-    u64 tie_weight, zero_weight;
+    u64 tie_weight;
     int tie_slot, tie_keep;
-    u32 zeros, below, odd;
+    u32 below, odd;
+    // zero and the values nearer to it than 2^-24, falling: places, entries, weights. They
+    // have the slots from kValues on.
+    u64 small[kSmall], small_weight[kSmall];
+    u32 small_count[kSmall];
+    int smalls;
+    u64 listed[kSmall];
+    u32 zeros;
 };
-constexpr int kZeroSlot = kValues, kNoSlot = -1;
+constexpr int kNoSlot = -1, kBelow = -2, kOdd = -3, kTiny = -4, kZero = -5;
 
 // The slot of one entry, whatever it is.
 struct OneSlot {
@@ -862,9 +893,9 @@ struct OneSlot {
         }
         const u32 mag = (bits & 0x7fff) - kFirstMag;
         if (mag < static_cast<u32>(kMags)) return static_cast<int>(mag | (bits >> 3 & 0x1000));
-        if ((bits & 0x7fff) == 0) return kZeroSlot;
-        // too large: below all (-2), or of a goodness above 0, or too small (-3)
-        return ((bits ^ flip) & 0x8000) && (bits & 0x7fff) > kFirstMag ? -2 : -3;
+        if ((bits & 0x7fff) == 0) return kZero;
+        if ((bits & 0x7fff) < kFirstMag) return kTiny;
+        return (bits ^ flip) & 0x8000 ? kBelow : kOdd;
     }
 };
 
@@ -877,13 +908,18 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
     const uint16_t *row = x + b * ld;
     const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
     for (int k = tid; k < kValues; k += T) sh.count[k] = 0;
-    if (tid == 0) sh.zeros = sh.below = sh.odd = 0;
+    if (tid == 0) sh.smalls = sh.zeros = sh.below = sh.odd = 0;
     __syncthreads();
-    auto count_one = [&](u32 bits) {
+    auto count_one = [&](u32 bits, int i) {
         const int slot = one(bits);
-        if (slot >= 0) atomicAdd(slot == kZeroSlot ? &sh.zeros : &sh.count[slot], 1u);
-        else if (slot == -2) sh.below = 1;
-        else if (slot == -3) sh.odd = 1;
+        if (slot >= 0) atomicAdd(&sh.count[slot], 1u);
+        else if (slot == kZero) atomicAdd(&sh.zeros, 1u);
+        else if (slot == kBelow) sh.below = 1;
+        else if (slot == kOdd) sh.odd = 1;
+        else if (slot == kTiny) {
+            const int at = atomicAdd(&sh.smalls, 1);
+            if (at < kSmall - 1) sh.listed[at] = rank_of(key_of(goodness(widen1(static_cast<uint16_t>(bits)), m)), i);
+        }
     };
     int done = vec_each<kRowAhead>(row, n, tid, T, [&](int, int i, RowVec<uint16_t>::type r) {
         const u32x4 w = __builtin_bit_cast(u32x4, r);
@@ -901,12 +937,12 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
 #pragma unroll 1
             for (int k = 0; k < 4; ++k) {
                 const u32 v = k == 0 ? w[0] : k == 1 ? w[1] : k == 2 ? w[2] : w[3];
-                count_one(v & 0xffff);
-                count_one(v >> 16);
+                count_one(v & 0xffff, i + 2 * k);
+                count_one(v >> 16, i + 2 * k + 1);
             }
         }
     });
-    if (done + tid < n) count_one(row[done + tid]);
+    if (done + tid < n) count_one(row[done + tid], done + tid);
     __syncthreads();
     // the values in falling order: place p of the first half is magnitude kMags - 1 - p
     // above 0, of the second p - kMags below 0; 0 is taken behind the first half's last
@@ -918,80 +954,103 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
         const u32 mag = (p < kMags ? kMags - 1 - p : p - kMags) + kFirstMag;
         return __uint_as_float(mag << 16 | (p < kMags ? 0u : 0x80000000u));
     };
-    const bool has_zero = tid == kMags / each - 1;
-    u32 count[each + 1];
+    const int tinies = sh.smalls;
+    const bool odd = sh.odd || tinies >= kSmall, below = sh.below;
+    const int smalls = odd ? 0 : tinies + (sh.zeros > 0 ? 1 : 0);
+    if (tid < smalls) {
+        const u64 zero = rank_of(key_of(0.f), 0);
+        const u64 mine = tid < tinies ? sh.listed[tid] : zero;
+        int at = sh.zeros > 0 && zero > mine;
+        for (int k = 0; k < tinies; ++k) at += sh.listed[k] > mine;
+        sh.small[at] = mine;
+        sh.small_count[at] = tid < tinies ? 1 : sh.zeros;
+    }
+    // the thread of the first half's last values has these behind its own
+    const bool has_small = smalls > 0 && tid == kMags / each - 1;
+    u32 count[each];
     u32 first = 2 * kValues, counted = 0;
-    count[each] = has_zero ? sh.zeros : 0;
-    if (count[each]) first = 2 * (tid * each + each) - 1;
+    if (has_small) {
+        first = 2 * (tid * each + each) - 1;
+        counted = tinies + sh.zeros;
+    }
 #pragma unroll
     for (int k = each - 1; k >= 0; --k) {
         count[k] = sh.count[slot_at(tid * each + k)];
         if (count[k]) first = 2 * (tid * each + k);
+        counted += count[k];
     }
-#pragma unroll
-    for (int k = 0; k <= each; ++k) counted += count[k];
-    const bool odd = sh.odd, below = sh.below;
     first = block_min<T>(first, sh.red);
     if (first == 2 * kValues && !odd && !below) {
         if (tid == 0) put_draw(a, b, -1, 0.0, 0);
         return;
     }
-    const Mass mass{first % 2 ? 0.f : value_at(static_cast<int>(first / 2)), a.scale, a.shift};
+    __syncthreads();
+    const Mass mass{first % 2 ? value_of(rank_key(sh.small[0])) : value_at(static_cast<int>(first / 2)), a.scale,
+                    a.shift};
     if (odd || (below && (first == 2 * kValues || mass.of(value_at(kValues - 1)) != 0))) {
         __syncthreads();
-        sample_any_row<T, uint16_t>(sh.row, row, b, n, m, a);
+        sample_any_row<T, 0, uint16_t>(sh.row, row, b, n, m, a);
         return;
     }
-    auto entry = [&](int k) { return k == each ? 0.f : value_at(tid * each + k); };
     // Values in turn, one at a time: nothing but the counts stays in registers, a weight
     // is formed again where it is needed again.
     u64 sum = 0;
     u32 counts;
     u32 before = block_before<T>(counted, sh.red, &counts);
     u32 partly = 0;  // bits of the values of which not all entries are kept
-#pragma unroll
-    for (int k = 0; k <= each; ++k) {
-        __builtin_amdgcn_sched_barrier(0);
-        u32 keep = count[k];
+    auto keep_first = [&](u32 have, float value, u32 bit) {
+        u32 keep = have;
         if (a.top_k > 0) keep = before >= static_cast<u32>(a.top_k) ? 0 : min(keep, a.top_k - before);
-        before += count[k];
-        if (keep < count[k]) partly |= 1u << k;
-        count[k] = keep;
-        if (keep) sum += static_cast<u64>(keep) * mass.of(entry(k));
+        before += have;
+        if (keep < have) partly |= bit;
+        if (keep) sum += static_cast<u64>(keep) * mass.of(value);
+        return keep;
+    };
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        count[k] = keep_first(count[k], value_at(tid * each + k), 1u << k);
     }
     __builtin_amdgcn_sched_barrier(0);
+    if (has_small)
+        for (int k = 0; k < smalls; ++k)
+            sh.small_count[k] = keep_first(sh.small_count[k], value_of(rank_key(sh.small[k])), 256u << k);
     u64 all;
     u64 at = block_before<T>(sum, sh.red, &all);
     // the counts are in registers: their place takes the weights
     if (tid == 0) {
-        sh.tie_slot = -1;
+        sh.tie_slot = kNoSlot;
         sh.tie_keep = 0;
-        sh.tie_weight = sh.zero_weight = 0;
+        sh.tie_weight = 0;
     }
     __syncthreads();
     const double target = a.top_p < 1.0 ? a.top_p * static_cast<double>(all) : INFINITY;
     u64 tie_at = 0, tie_w = 0;
     u32 tie_keeps = 0;
-    int tie = -1;  // the value of which some entries are kept
-#pragma unroll
-    for (int k = 0; k <= each; ++k) {
-        __builtin_amdgcn_sched_barrier(0);
-        u64 w = 0;
-        if (count[k] && static_cast<double>(at) < target && mass.distance(entry(k)) <= a.dmax) {
-            w = mass.of(entry(k));
-            const u64 next = at + count[k] * w;
-            if (static_cast<double>(next) >= target || (partly >> k & 1)) {
-                tie = k;
-                tie_at = at;
-                tie_w = w;
-                tie_keeps = count[k];
-            }
-            at = next;
+    int tie = kNoSlot;  // the value of which some entries are kept
+    auto weigh = [&](u32 have, float value, u32 bit, int slot) -> u64 {
+        if (!have || !(static_cast<double>(at) < target) || mass.distance(value) > a.dmax) return 0;
+        const u64 w = mass.of(value), next = at + have * w;
+        if (static_cast<double>(next) >= target || (partly & bit)) {
+            tie = slot;
+            tie_at = at;
+            tie_w = w;
+            tie_keeps = have;
         }
-        if (k < each) sh.weight[slot_at(tid * each + k)] = tie == k ? 0 : w;
-        else if (has_zero) sh.zero_weight = tie == k ? 0 : w;
+        at = next;
+        return tie == slot ? 0 : w;
+    };
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int slot = slot_at(tid * each + k);
+        sh.weight[slot] = weigh(count[k], value_at(tid * each + k), 1u << k, slot);
     }
-    if (tie >= 0 && tie_w) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (has_small)
+        for (int k = 0; k < smalls; ++k)
+            sh.small_weight[k] = weigh(sh.small_count[k], value_of(rank_key(sh.small[k])), 256u << k, kValues + k);
+    if (tie_w) {
         // the fewest of its entries that reach the target; all of it may be
         u64 keep = tie_keeps;
         if (static_cast<double>(tie_at + keep * tie_w) >= target) {
@@ -1000,7 +1059,7 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
             while (static_cast<double>(tie_at + c * tie_w) < target) ++c;
             keep = min(keep, c);
         }
-        sh.tie_slot = tie == each ? kZeroSlot : slot_at(tid * each + tie);
+        sh.tie_slot = tie;
         sh.tie_keep = static_cast<int>(keep);
         sh.tie_weight = tie_w;
     }
@@ -1014,11 +1073,22 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
     const int lo = min(n, wave * part), hi = min(n, lo + part);
     u64 s = 0;
     u32 ties = 0;
-    auto weigh_one = [&](u32 bits) -> u64 {
+    auto slot_of = [&](u32 bits, int i) {
         const int slot = one(bits);
-        return slot < 0 ? 0 : slot == kZeroSlot ? sh.zero_weight : sh.weight[slot];
+        if (slot != kZero && slot != kTiny) return slot;
+        for (int k = 0; k < smalls; ++k)
+            if (slot == kZero ? rank_key(sh.small[k]) == key_of(0.f)
+                              : rank_index(sh.small[k]) == i && rank_key(sh.small[k]) != key_of(0.f))
+                return kValues + k;
+        return kNoSlot;
     };
-    auto is_tie = [&](u32 bits) { return one(bits) == tie_slot && tie_slot >= 0; };
+    // the weight of an entry that is kept with all of its value; counts one of the others
+    auto weigh_one = [&](u32 bits, int i, u32 &tied) -> u64 {
+        const int slot = slot_of(bits, i);
+        if (slot < 0) return 0;
+        tied += slot == tie_slot;
+        return slot < kValues ? sh.weight[slot] : sh.small_weight[slot - kValues];
+    };
     done = lo + vec_each<kRowAhead>(row + lo, hi - lo, lane, kWave, [&](int, int i, RowVec<uint16_t>::type r) {
         const u32x4 v = __builtin_bit_cast(u32x4, r);
         u16x2 most = {0, 0};
@@ -1037,16 +1107,11 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
 #pragma unroll 1
             for (int k = 0; k < 8; ++k) {
                 const u32 q = k < 4 ? (k < 2 ? v[0] : v[1]) : (k < 6 ? v[2] : v[3]);
-                const u32 bits = k % 2 ? q >> 16 : q & 0xffff;
-                s += weigh_one(bits);
-                ties += is_tie(bits);
+                s += weigh_one(k % 2 ? q >> 16 : q & 0xffff, lo + i + k, ties);
             }
         }
     });
-    if (done + lane < hi) {
-        s += weigh_one(row[done + lane]);
-        ties += is_tie(row[done + lane]);
-    }
+    if (done + lane < hi) s += weigh_one(row[done + lane], done + lane, ties);
     s = block_add<kWave>(s, nullptr);
     const u32 tied = block_add<kWave>(ties, nullptr);
     if (lane == 0) {
@@ -1089,8 +1154,9 @@ __global__ __launch_bounds__(T, 8) void sample_values_kernel(int n, int64_t ld, 
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                each_w[k] = k < have ? weigh_one(row[p0 + k]) : 0;
-                if (k < have) tie_bits |= static_cast<u32>(is_tie(row[p0 + k])) << k;
+                u32 tied = 0;
+                each_w[k] = k < have ? weigh_one(row[p0 + k], p0 + k, tied) : 0;
+                tie_bits |= tied << k;
             }
         }
 #pragma unroll
@@ -1123,7 +1189,7 @@ bool cap_has_slot(float cap, u32 *bits) {
     memcpy(&f, &cap, 4);
     *bits = f >> 16;
     const u32 mag = (*bits & 0x7fff) - kFirstMag;
-    return (f & 0xffff) == 0 && ((*bits & 0x7fff) == 0 || mag < static_cast<u32>(kMags));
+    return (f & 0xffff) == 0 && mag < static_cast<u32>(kMags);
 }
 
 template <typename E>
@@ -1147,8 +1213,10 @@ hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
         hipLaunchKernelGGL((sample_picked_kernel<T, true, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a);      \
     else if (picked)                                                                                            \
         hipLaunchKernelGGL((sample_picked_kernel<T, false, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a);     \
+    else if (caps)                                                                                              \
+        hipLaunchKernelGGL((sample_kernel<T, true, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a);             \
     else                                                                                                        \
-        hipLaunchKernelGGL((sample_kernel<T, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a)
+        hipLaunchKernelGGL((sample_kernel<T, false, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m, a)
     if (n <= 512) SAMPLE(64);
     else if (n <= 4096) SAMPLE(256);
     else SAMPLE(1024);

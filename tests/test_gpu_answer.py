@@ -67,6 +67,12 @@ def _scores(kind, B, N, seed):
     elif kind == "lowest":  # masked by the lowest value of the type
         x[rng.random((B, N)) < 0.6] = -3.3895314e38
         x[0] = -3.3895314e38
+    elif kind == "tiny":  # a few values next to 0, others equal to it
+        x[:, rng.integers(0, N, max(1, N // 700))] *= 1e-9
+        x[:, rng.integers(0, N, max(1, N // 100))] = 0.0
+        x[1 % B] = np.where(rng.random(N) < 0.9, 0.0, 1e-20 * x[1 % B])
+        x[2 % B] = -np.abs(x[2 % B])
+        x[2 % B, N // 3] = -1e-10
     elif kind == "sorted":  # one thread's share holds many of the largest
         x = np.sort(x, axis=1)
     elif kind == "outlier":
@@ -75,7 +81,7 @@ def _scores(kind, B, N, seed):
     return x
 
 
-KINDS = ["plain", "masked", "ties", "equal", "zeros", "huge", "near", "sorted", "outlier", "signalling", "lowest"]
+KINDS = ["plain", "masked", "ties", "equal", "zeros", "huge", "near", "sorted", "outlier", "signalling", "lowest", "tiny"]
 SIZES = [1, 2, 63, 64, 65, 511, 512, 513, 1000, 4096, 4097, 20011]
 
 
