@@ -93,14 +93,18 @@ __device__ __forceinline__ int vec_each(const E *p, int n, int tid, int count, F
 }
 
 // f(index, score) for the first n elements of a row, as vec_each, or (kAhead 0) element by
-// element in a loop of few registers, for what rows in earnest do not reach.
-template <int kAhead, typename E, typename F>
+// element in a loop of few registers, for what rows in earnest do not reach. kTurns: so
+// many elements at a time (an f of many registers), 0: as the compiler mixes them.
+template <int kAhead, int kTurns = 0, typename E, typename F>
 __device__ __forceinline__ void row_each(const E *p, int n, int tid, int count, F f) {
     int done = 0;
     if constexpr (kAhead > 0)
         done = vec_each<kAhead>(p, n, tid, count, [&](int, int i, typename RowVec<E>::type r) {
 #pragma unroll
-            for (int k = 0; k < RowVec<E>::n; ++k) f(i + k, widen1(static_cast<E>(r[k])));
+            for (int k = 0; k < RowVec<E>::n; ++k) {
+                f(i + k, widen1(static_cast<E>(r[k])));
+                if (kTurns > 0 && k % (kTurns > 0 ? kTurns : 1) == kTurns - 1) __builtin_amdgcn_sched_barrier(0);
+            }
         });
 #pragma unroll 1
     for (int i = done + tid; i < n; i += count) f(i, widen1(p[i]));

@@ -20,10 +20,10 @@ namespace dstd {
 
 namespace {
 
-constexpr int kBins = 2048;  // of a histogram over a row
+template <int T> constexpr int kBins = T >= 1024 ? 2048 : T >= 256 ? 1024 : 512;  // of a histogram over a row
 // Candidates of a row that are held at once, and so the largest top_k that is
 // chosen from candidates.
-template <int T> constexpr int kList = T >= 1024 ? 2048 : 1024;
+template <int T> constexpr int kList = kBins<T>;
 constexpr int kMaxPicked = 1024;
 // groups of a thread's share of the row, a maximum each
 template <typename E> constexpr int kGroups = sizeof(E) == 2 ? 2 * kRowAhead : kRowAhead;
@@ -31,7 +31,7 @@ template <typename E> constexpr int kGroups = sizeof(E) == 2 ? 2 * kRowAhead : k
 template <int T> struct RowShared {
     u64 red[T / kWave + 1];
     u64 list[kList<T>];
-    u64 hist[kBins];
+    u64 hist[kBins<T>];
     u64 found[2];
     int count, seen;
 };
@@ -54,6 +54,8 @@ struct Border {
 struct Mass {
     double top, scale;  // the largest goodness; |scale|
     int shift;
+    // how far below the largest weights are 0
+    __device__ double span() const { return 0.6931471805599453 * (shift + 1) / scale; }
     __device__ double distance(float y) const { return (top - static_cast<double>(y)) * scale; }
     __device__ double distance(u32 key) const { return distance(value_of(key)); }
     // rint(e^-d 2^shift): d = n ln 2 + r, e^-r by its series to r^12 / 12! (|r| <= ln 2 / 2:
@@ -104,9 +106,9 @@ template <int T, typename F> __device__ void sort_list(RowShared<T> &sh, int n, 
         __syncthreads();
         return;
     }
-    constexpr int most = 256, share = kList<T> / T, per = kBins / T;
-    u32 *count = reinterpret_cast<u32 *>(sh.hist), *first = count + kBins;
-    for (int k = threadIdx.x; k < kBins; k += T) count[k] = 0;
+    constexpr int most = 256, share = kList<T> / T, per = kBins<T> / T;
+    u32 *count = reinterpret_cast<u32 *>(sh.hist), *first = count + kBins<T>;
+    for (int k = threadIdx.x; k < kBins<T>; k += T) count[k] = 0;
     __syncthreads();
     u64 v[share];
     u32 place[share];  // the bin, and how many were there before
@@ -182,10 +184,10 @@ template <int T> __device__ void sort_by_value(RowShared<T> &sh, int n) {
         }
         ymax = value_of(block_max<T>(hi, sh.red));
         lo = ~block_max<T>(lo, sh.red);
-        per = static_cast<float>(kBins / (static_cast<double>(ymax) - static_cast<double>(value_of(lo))));
+        per = static_cast<float>(kBins<T> / (static_cast<double>(ymax) - static_cast<double>(value_of(lo))));
     }
     sort_list<T>(sh, n, [&](u64 r) {
-        return static_cast<u32>(fminf((ymax - value_of(rank_key(r))) * per, kBins - 1.f));
+        return static_cast<u32>(fminf((ymax - value_of(rank_key(r))) * per, kBins<T> - 1.f));
     });
 }
 
@@ -217,7 +219,7 @@ __device__ int by_index(RowShared<T> &sh, const E *row, int n, double share, u64
     const int part = (n + waves * unit - 1) / (waves * unit) * unit;
     const int lo = min(n, wave * part), hi = min(n, lo + part);
     u64 s = 0;
-    row_each<kAhead>(row + lo, hi - lo, lane, kWave,
+    row_each<kAhead, 2>(row + lo, hi - lo, lane, kWave,
                 [&](int i, float x) { s += weight(x, lo + i); });
     u64 total;
     u64 before = block_before<T>(s, sh.red, &total);
@@ -286,29 +288,29 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
     u32 lo = 0, hi = 0;   // keys of the bin
     int shift = -1;       // bins of 2^shift keys; -1: bins of the range of values
     const double range = fmin(static_cast<double>(ymax) - static_cast<double>(ymin), span);  // ymin may be -inf
-    const float per = static_cast<float>(kBins / range);
+    const float per = static_cast<float>(kBins<T> / range);
     u64 base = 0;
     double target = static_cast<double>(target_n);
     for (;;) {
         auto bin_of = [&](u32 key) {
-            if (shift < 0) return static_cast<int>(fminf((ymax - value_of(key)) * per, kBins - 1.f));
+            if (shift < 0) return static_cast<int>(fminf((ymax - value_of(key)) * per, kBins<T> - 1.f));
             return static_cast<int>((hi - key) >> shift);
         };
         auto in_range = [&](u32 key, int i) { return kept.has(key, i) && (shift < 0 || (key >= lo && key <= hi)); };
         int bin = 0;
         if (shift >= 0 || n > kList<T>) {
             __syncthreads();
-            for (int k = threadIdx.x; k < kBins; k += T) sh.hist[k] = 0;
+            for (int k = threadIdx.x; k < kBins<T>; k += T) sh.hist[k] = 0;
             __syncthreads();
             auto *hist = reinterpret_cast<unsigned long long *>(sh.hist);
             if (shift < 0) {
                 const float at = kept.at();
                 const int upto = kept.upto();
-                row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
+                row_each<kAhead, 2>(row, n, threadIdx.x, T, [&](int i, float x) {
                     const float y = goodness(x, m);
                     if (!(y > at || (y == at && i <= upto))) return;
                     const u64 w = weight.of(y);
-                    if (w) atomicAdd(&hist[static_cast<int>(fminf((ymax - y) * per, kBins - 1.f))], w);
+                    if (w) atomicAdd(&hist[static_cast<int>(fminf((ymax - y) * per, kBins<T> - 1.f))], w);
                 });
             } else {
                 row_each<0>(row, n, threadIdx.x, T, [&](int i, float x) {
@@ -319,7 +321,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                 });
             }
             __syncthreads();
-            constexpr int per_thread = kBins / T;
+            constexpr int per_thread = kBins<T> / T;
             u64 mine = 0;
 #pragma unroll
             for (int k = 0; k < per_thread; ++k) mine += sh.hist[threadIdx.x * per_thread + k];
@@ -367,7 +369,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                     return Border{rank_of(lo, i)};
                 }
                 shift = 0;
-                while ((static_cast<u64>(hi - lo) >> shift) >= kBins) ++shift;
+                while ((static_cast<u64>(hi - lo) >> shift) >= kBins<T>) ++shift;
                 continue;
             }
         } else {
@@ -433,8 +435,7 @@ __device__ __attribute__((noinline)) Border pick_count(RowShared<T> &sh, const E
 template <int T, int kAhead, typename E>
 __device__ __attribute__((noinline)) Border pick_mass(RowShared<T> &sh, const E *row, int n, ScoreMap m, Border kept,
                                                       float ymin, Mass mass, double share) {
-    return by_order<T, kAhead>(sh, row, n, m, kept, ymin, static_cast<float>(mass.top),
-                               0.6931471805599453 * (mass.shift + 1) / mass.scale, mass, 0, share);
+    return by_order<T, kAhead>(sh, row, n, m, kept, ymin, static_cast<float>(mass.top), mass.span(), mass, 0, share);
 }
 
 // What a draw goes by, and where it is written.
@@ -494,7 +495,7 @@ __device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const
 // Rows whose largest entry is found without a look at those that do not count: -inf and
 // NaN weigh nothing as they are (min(NaN, .) is the other), +inf shows up as the largest.
 template <int T, bool kCaps, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
                                                                       ScoreMap m, DrawArgs a) {
     __shared__ RowShared<T> sh;
     const int64_t b = blockIdx.x;
@@ -504,7 +505,7 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_kernel(int n, int
     row_each<kRowAhead>(row, n, threadIdx.x, T, [&](int, float v) { top = larger(good(v), top); });
     top = value_of(block_max<T>(key_of(top), sh.red));
     if (top == INFINITY || (a.top_k > 0 && a.top_k < n)) {
-        sample_any_row<T, 1, E>(sh, row, b, n, m, a);
+        sample_any_row<T, kRowAhead, E>(sh, row, b, n, m, a);
         return;
     }
     if (!(top > -INFINITY)) {
@@ -513,8 +514,9 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_kernel(int n, int
     }
     const Mass mass{top, a.scale, a.shift};
     Border kept{0};
-    if (a.top_p < 1.0) kept = pick_mass<T, 1, E>(sh, row, n, m, kept, -INFINITY, mass, a.top_p);
-    draw_kept<T, 1>(sh, row, b, n, mass, kept, a, good);
+    if (a.top_p < 1.0)
+        kept = by_order<T, kRowAhead>(sh, row, n, m, kept, -INFINITY, top, mass.span(), mass, 0, a.top_p);
+    draw_kept<T, kRowAhead>(sh, row, b, n, mass, kept, a, good);
 }
 
 // Candidates for the K first entries of a row's order: all that reach a bound which K
@@ -590,22 +592,22 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
     if (hi == INFINITY || K > groups * T) return -FLT_MAX;
     if (!(hi > -INFINITY)) return INFINITY;  // nothing counts
     // bins of the range of the maxima
-    const float per = static_cast<float>(kBins / (static_cast<double>(hi) - static_cast<double>(lo)));
+    const float per = static_cast<float>(kBins<T> / (static_cast<double>(hi) - static_cast<double>(lo)));
     u32 *hist = reinterpret_cast<u32 *>(sh.hist);
-    for (int k = threadIdx.x; k < kBins; k += T) hist[k] = 0;
+    for (int k = threadIdx.x; k < kBins<T>; k += T) hist[k] = 0;
     if (threadIdx.x == 0) sh.count = -1;
     __syncthreads();
     int bin[groups];
 #pragma unroll
     for (int g = 0; g < groups; ++g) {
-        bin[g] = kBins;  // a group without an entry
+        bin[g] = kBins<T>;  // a group without an entry
         if (best[g] > -INFINITY) {
-            bin[g] = static_cast<int>(fminf((hi - best[g]) * per, kBins - 1.f));
+            bin[g] = static_cast<int>(fminf((hi - best[g]) * per, kBins<T> - 1.f));
             atomicAdd(&hist[bin[g]], 1u);
         }
     }
     __syncthreads();
-    constexpr int each = kBins / T;
+    constexpr int each = kBins<T> / T;
     u32 mine = 0;
 #pragma unroll
     for (int k = 0; k < each; ++k) mine += hist[threadIdx.x * each + k];
@@ -668,7 +670,7 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     const int bound16 = bound == 0.f ? -1 : order16(__float_as_uint(bound) >> 16, 0)[0];
     // vectors with a candidate, in the histogram's memory; they are looked through behind
     // the loop, all at once
-    constexpr int most = 2 * kBins, vn = RowVec<E>::n;
+    constexpr int most = 2 * kBins<T>, vn = RowVec<E>::n;
     u32 *seen = reinterpret_cast<u32 *>(sh.hist);
     __syncthreads();
     if (threadIdx.x == 0) sh.count = sh.seen = 0;
@@ -755,7 +757,7 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
 }
 
 template <int T, bool kCaps, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void top_logits_kernel(int n, int64_t ld, const E *__restrict__ x, ScoreMap m,
                                                        double scale, float c2, int K,
                                                        int32_t *__restrict__ idx, float *__restrict__ logit,
                                                        float *__restrict__ rest) {
@@ -777,7 +779,7 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void top_logits_kernel(int n,
 
 // One class from the top_k <= kMaxPicked first entries of each row.
 template <int T, bool kCaps, typename E>
-__global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_picked_kernel(int n, int64_t ld,
+__global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_picked_kernel(int n, int64_t ld,
                                                                              const E *__restrict__ x, ScoreMap m,
                                                                              DrawArgs a) {
     __shared__ RowShared<T> sh;
@@ -821,9 +823,9 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 1) void sample_picked_kernel(int
 #pragma unroll
     for (int k = 0; k < each; ++k)
         if (first + k < count) sh.list[first + k] = back[k];
-    const float per = static_cast<float>(kBins) / static_cast<float>(n);
+    const float per = static_cast<float>(kBins<T>) / static_cast<float>(n);
     sort_list<T>(sh, count, [&](u64 r) {
-        return static_cast<u32>(fminf(static_cast<float>(~static_cast<u32>(r >> 32)) * per, kBins - 1.f));
+        return static_cast<u32>(fminf(static_cast<float>(~static_cast<u32>(r >> 32)) * per, kBins<T> - 1.f));
     });
     mine = 0;
 #pragma unroll
