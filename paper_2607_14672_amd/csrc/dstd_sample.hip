@@ -59,12 +59,14 @@ struct Mass {
     __device__ double distance(float y) const { return (top - static_cast<double>(y)) * scale; }
     __device__ double distance(u32 key) const { return distance(value_of(key)); }
     // rint(e^-d 2^shift): d = n ln 2 + r, e^-r by its series to r^12 / 12! (|r| <= ln 2 / 2:
-    // 2^-52 relative). Adding 2^52 leaves the integer in the low bits.
+    // 2^-52 relative), n taken off its exponent. Adding 2^52 leaves the integer in the low
+    // bits. From d = 64 on (and for NaN) the result is 0.
     static __device__ __forceinline__ u64 fixed_exp(double d, int shift) {
+        d = fmin(d, 64.0);
         const double big = 0x1.8p52;
-        const double t = fma(fmin(d, 128.0), 1.4426950408889634, big);
+        const double t = fma(d, 1.4426950408889634, big);
         const double n = t - big;
-        const double r = fma(n, -0x1.abc9e3b39803fp-56, fma(n, -0x1.62e42fefa39efp-1, fmin(d, 128.0)));
+        const double r = fma(n, -0x1.abc9e3b39803fp-56, fma(n, -0x1.62e42fefa39efp-1, d));
         double p = 1.0 / 479001600;
         p = fma(p, -r, 1.0 / 39916800);
         p = fma(p, -r, 1.0 / 3628800);
@@ -78,7 +80,8 @@ struct Mass {
         p = fma(p, -r, 0.5);
         p = fma(p, -r, 1.0);
         p = fma(p, -r, 1.0);
-        const double v = ldexp(p, shift - static_cast<int>(__double2loint(t))) + 0x1p52;
+        const int up = (shift - __double2loint(t)) << 20;
+        const double v = __hiloint2double(__double2hiint(p) + up, __double2loint(p)) + 0x1p52;
         return __double_as_longlong(v) & 0xfffffffffffffull;
     }
     __device__ u64 of(float y) const { return fixed_exp(distance(y), shift); }
@@ -191,18 +194,18 @@ template <int T> __device__ void sort_by_value(RowShared<T> &sh, int n) {
     });
 }
 
-// Entries of a row that `want` (key, index) holds for, into the list, as many as
-// fit; returns how many there are.
+// Entries of a row that `want` (goodness, index) holds for, into the list, as many as fit;
+// returns how many there are.
 template <int T, int kAhead, typename E, typename F>
 __device__ int collect(RowShared<T> &sh, const E *row, int n, const ScoreMap &m, F want) {
     __syncthreads();
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     row_each<kAhead>(row, n, threadIdx.x, T, [&](int i, float x) {
-        const u32 key = key_of(goodness(x, m));
-        if (key > kAbsentKey && want(key, i)) {
+        const float y = goodness(x, m);
+        if (y > -INFINITY && want(y, i)) {
             const int at = atomicAdd(&sh.count, 1);
-            if (at < kList<T>) sh.list[at] = rank_of(key, i);
+            if (at < kList<T>) sh.list[at] = rank_of(key_of(y), i);
         }
     });
     __syncthreads();
@@ -341,9 +344,19 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
             __syncthreads();
             base = sh.found[0];
             bin = static_cast<int>(sh.found[1]);
-            const int count = collect<T, kAhead>(sh, row, n, m, [&](u32 key, int i) {
-                return in_range(key, i) && bin_of(key) == bin;
-            });
+            int count;
+            if (shift < 0) {
+                const float last = kept.at();
+                const int upto = kept.upto();
+                count = collect<T, kAhead>(sh, row, n, m, [&](float y, int i) {
+                    return static_cast<int>(fminf((ymax - y) * per, kBins<T> - 1.f)) == bin &&
+                           (y > last || (y == last && i <= upto));
+                });
+            } else {
+                count = collect<T, 0>(sh, row, n, m, [&](float y, int i) {
+                    return in_range(key_of(y), i) && bin_of(key_of(y)) == bin;
+                });
+            }
             if (count > kList<T>) {
                 u32 a = 0xffffffffu, b = 0;
                 row_each<0>(row, n, threadIdx.x, T, [&](int i, float x) {
@@ -373,7 +386,7 @@ __device__ Border by_order(RowShared<T> &sh, const E *row, int n, const ScoreMap
                 continue;
             }
         } else {
-            collect<T, kAhead>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+            collect<T, kAhead>(sh, row, n, m, [&](float y, int i) { return kept.has(key_of(y), i); });
         }
         // the list in order, and the sums of its weights
         const int count = sh.count;
@@ -639,7 +652,7 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
 template <int T, typename E>
 __device__ __attribute__((noinline)) int pick_exactly(RowShared<T> &sh, const E *row, int n, ScoreMap m, int K) {
     const Border kept = pick_count<T, 0, E>(sh, row, n, m, row_extremes<T, 0>(sh, row, n, m), K);
-    return collect<T, 0>(sh, row, n, m, [&](u32 key, int i) { return kept.has(key, i); });
+    return collect<T, 0>(sh, row, n, m, [&](float y, int i) { return kept.has(key_of(y), i); });
 }
 template <int T, typename E>
 __device__ __attribute__((noinline)) ExpSum sum_behind(const E *row, int n, ScoreMap m, u64 last, float c2) {
