@@ -63,9 +63,9 @@ template <typename E> __device__ __forceinline__ typename RowVec<E>::type load_v
     return *reinterpret_cast<const typename RowVec<E>::any *>(p);
 }
 
-// f(slot, first index, vector) for the whole vectors of the first n elements of a row, by
-// `count` threads, of which this is number `tid`: kAhead a thread on the way at once,
-// `slot` the number among these. Returns the index of the first element behind them.
+// f(first index, vector) for the whole vectors of the first n elements of a row, by `count`
+// threads, of which this is number `tid`: kAhead a thread on the way at once. Returns the
+// index of the first element behind them.
 constexpr int kRowAhead = 4;
 template <int kAhead, typename E, typename F>
 __device__ __forceinline__ int vec_each(const E *p, int n, int tid, int count, F f) {
@@ -78,7 +78,7 @@ __device__ __forceinline__ int vec_each(const E *p, int n, int tid, int count, F
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) r[a] = load_vec<E>(p + static_cast<int64_t>(v + a * count) * V::n);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) f(a, (v + a * count) * V::n, r[a]);
+        for (int a = 0; a < kAhead; ++a) f((v + a * count) * V::n, r[a]);
     }
     if (whole < nv) {
         typename V::type r[kAhead] = {};
@@ -87,7 +87,7 @@ __device__ __forceinline__ int vec_each(const E *p, int n, int tid, int count, F
             if (v + a * count < nv) r[a] = load_vec<E>(p + static_cast<int64_t>(v + a * count) * V::n);
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
-            if (v + a * count < nv) f(a, (v + a * count) * V::n, r[a]);
+            if (v + a * count < nv) f((v + a * count) * V::n, r[a]);
     }
     return nv * V::n;
 }
@@ -99,7 +99,7 @@ template <int kAhead, int kTurns = 0, typename E, typename F>
 __device__ __forceinline__ void row_each(const E *p, int n, int tid, int count, F f) {
     int done = 0;
     if constexpr (kAhead > 0)
-        done = vec_each<kAhead>(p, n, tid, count, [&](int, int i, typename RowVec<E>::type r) {
+        done = vec_each<kAhead>(p, n, tid, count, [&](int i, typename RowVec<E>::type r) {
 #pragma unroll
             for (int k = 0; k < RowVec<E>::n; ++k) {
                 f(i + k, widen1(static_cast<E>(r[k])));

@@ -1450,10 +1450,11 @@ dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_ou
     if ((st = check_top(K, N)) != DSTD_OK) return st;
     if (logit_dtype != DSTD_F32 && logit_dtype != DSTD_BF16)
         return fail(DSTD_ERR_PARAM, "unknown dtype %d", (int)logit_dtype);
-    if (!(isfinite(tau_soft) && tau_soft > 0.f && isfinite(1.f / tau_soft)))
+    if (!(isfinite(tau_soft) && tau_soft > 0.f && isfinite(1.4426950408889634f / tau_soft)))
         return fail(DSTD_ERR_PARAM, "tau_soft must be > 0, and 1 / tau_soft finite");
     if (!isfinite(t_cap)) return fail(DSTD_ERR_PARAM, "t_cap must be finite");
-    if (!(isfinite(weight) && weight >= 0.f)) return fail(DSTD_ERR_PARAM, "weight must be finite and >= 0");
+    if (!(weight >= 0.f && isfinite(weight * (1.f / tau_soft))))
+        return fail(DSTD_ERR_PARAM, "weight must be >= 0, and weight / tau_soft finite");
     if (accumulate != 0 && accumulate != 1) return fail(DSTD_ERR_PARAM, "accumulate must be 0 or 1");
     if (!loss || (B > 0 && (!t_out || !idx || !logit)))
         return fail(DSTD_ERR_NULL, "t_out, idx, logit and loss are required");

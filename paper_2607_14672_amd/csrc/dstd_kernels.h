@@ -115,6 +115,9 @@ struct SampleJob {
     float *logp;
 };
 hipError_t launch_sample(const SampleJob &j, hipStream_t st);
+// the same for 0 < top_k <= kMaxPicked
+constexpr int kMaxPicked = 1024;
+hipError_t launch_sample_picked(const SampleJob &j, hipStream_t st);
 
 // inv = 1 / tau_soft, c2 = log2(e) / tau_soft; part: distill_parts(N) for each row.
 constexpr int kKdMaxK = 256;

@@ -360,3 +360,188 @@ def test_empty_batches(op):
                                     torch.empty((0, 3), device="cuda"), t_cap=1.0)
         torch.cuda.synchronize()
         assert g.shape == (0, 9) and loss.tolist() == [0.0]
+
+
+# -------------------------------------------------- calls as programs make them --
+def _calls(torch, dstd, B=40, N=20011, seed=0):
+    """One call of each operator on inputs of its own, as (name, call) pairs; a call
+    returns its outputs."""
+    rng = np.random.default_rng(seed)
+    x = _put(torch, _scores("ties", B, N, seed), torch.bfloat16)
+    f = _put(torch, _scores("plain", B, N, seed + 1), torch.float32)
+    u = torch.from_numpy(rng.random(B).astype(np.float32)).cuda()
+    t = _times(B, N, seed)
+    idx, logit, rest = (torch.from_numpy(v).cuda() for v in _record(rng, t, 50, 0.1, 1.5, True, "f32", "twice"))
+    tv = torch.from_numpy(t).cuda()
+    return [("top", lambda: dstd.top_logits(x, 64)), ("top f32", lambda: dstd.top_logits(f, 200, scale=-2.0, cap=1.0)),
+            ("picked", lambda: dstd.sample(x, u, top_k=100, top_p=0.9)),
+            ("values", lambda: dstd.sample(x, u, top_p=0.9, min_p=0.01)),
+            ("f32", lambda: dstd.sample(f, u, top_p=0.9)), ("f32 all", lambda: dstd.sample(f, u)),
+            ("f32 count", lambda: dstd.sample(f, u, top_k=3000)),
+            ("distill", lambda: dstd.distill_grad(tv, idx, logit, rest, tau_soft=0.1, t_cap=1.5)),
+            ("distill rows", lambda: dstd.distill_grad(tv[:5], idx[:5], logit[:5], rest[:5], tau_soft=0.1, t_cap=1.5))]
+
+
+def _same(torch, a, b):
+    return all(torch.equal(p.view(torch.int32), q.view(torch.int32)) for p, q in zip(a, b))
+
+
+def test_repeated_calls_give_the_same_bits():
+    torch, dstd = _torch()
+    for name, call in _calls(torch, dstd):
+        print(f"again: {name}", flush=True)
+        first = [v.clone() for v in call()]
+        for _ in range(5):
+            assert _same(torch, first, call()), name
+
+
+def test_calls_on_another_stream_and_two_at_once():
+    torch, dstd = _torch()
+    calls = _calls(torch, dstd)
+    want = [[v.clone() for v in call()] for _, call in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for k, (_, call) in enumerate(calls + calls):
+        with torch.cuda.stream(streams[k % 2]):
+            got.append(call())
+    torch.cuda.synchronize()
+    for k, g in enumerate(got):
+        assert _same(torch, want[k % len(calls)], g), calls[k % len(calls)][0]
+
+
+def test_captured_calls_replay():
+    """Each call captured, replayed between eager work, on inputs that change."""
+    torch, dstd = _torch()
+    B, N = 33, 5003
+    x = torch.empty((B, N), dtype=torch.bfloat16, device="cuda")
+    t = torch.empty((B, N), device="cuda")
+    u = torch.empty(B, device="cuda")
+
+    def fill(seed):
+        x.copy_(torch.from_numpy(_scores("plain", B, N, seed)))
+        t.copy_(torch.from_numpy(_times(B, N, seed)))
+        u.copy_(torch.from_numpy(np.random.default_rng(seed).random(B).astype(np.float32)))
+
+    def step():
+        idx, logit, rest = dstd.top_logits(x, 30, scale=0.5)
+        g, loss = dstd.distill_grad(t, idx, logit, rest, tau_soft=0.1, t_cap=1.5)
+        g, loss2 = dstd.distill_grad(t, idx, logit, tau_soft=0.2, t_cap=1.5, grad=g, accumulate=True)
+        return (idx, logit, rest, g, loss, loss2) + dstd.sample(x, u, top_p=0.8) + dstd.sample(t, u, scale=-5.0, top_k=9)
+
+    fill(0)
+    step()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    outs = []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(step())
+    for seed in range(1, 5):
+        fill(seed)
+        want = [v.clone() for v in step()]
+        graphs[seed % 2].replay()
+        torch.zeros(1000, device="cuda").sum().item()
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for o in outs:
+            assert _same(torch, want, o), seed
+
+
+def test_rows_far_apart():
+    """Places beyond 2^32 elements."""
+    torch, dstd = _torch()
+    B, N, ld = 4200, 9, 1 << 20
+    xs = _scores("plain", B, N, 3)
+    flat = torch.empty(B * ld, dtype=torch.bfloat16, device="cuda")
+    x = flat.view(B, ld)[:, :N]
+    x.copy_(torch.from_numpy(xs))
+    small = x.contiguous()
+    for a, b in zip(dstd.top_logits(x, 3), dstd.top_logits(small, 3)):
+        assert torch.equal(a, b)
+    u = torch.rand(B, device="cuda")
+    for a, b in zip(dstd.sample(x, u), dstd.sample(small, u)):
+        assert torch.equal(a, b)
+    del flat, x
+    tf, gf = (torch.empty(B * ld, device="cuda") for _ in range(2))
+    t, g = tf.view(B, ld)[:, :N], gf.view(B, ld)[:, :N]
+    t.copy_(torch.from_numpy(_times(B, N, 4)))
+    idx, logit, rest = dstd.top_logits(small, 3)
+    got = dstd.distill_grad(t, idx, logit, rest, tau_soft=0.3, t_cap=1.5, grad=g)
+    want = dstd.distill_grad(t.contiguous(), idx, logit, rest, tau_soft=0.3, t_cap=1.5)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_views_are_read_as_they_are():
+    """Transposed, stepped and reversed-stride views give what their copies give."""
+    torch, dstd = _torch()
+    base = torch.from_numpy(_scores("plain", 300, 200, 6)).cuda()
+    u = torch.rand(200, device="cuda")
+    for v in (base.t(), base[::3], base[:, ::2], base[:, 7:50], base[5:6], base.expand(2, 300, 200)[1]):
+        c = v.contiguous()
+        assert all(torch.equal(a, b) for a, b in zip(dstd.top_logits(v, 5), dstd.top_logits(c, 5)))
+        k = u[:v.shape[0]] if v.shape[0] <= 200 else torch.rand(v.shape[0], device="cuda")
+        assert all(torch.equal(a, b) for a, b in zip(dstd.sample(v, k), dstd.sample(c, k)))
+    with pytest.raises(ValueError):
+        dstd.distill_grad(base, torch.zeros((300, 2), dtype=torch.int32, device="cuda"),
+                          torch.zeros((300, 2), device="cuda"), t_cap=1.0,
+                          grad=torch.zeros((200, 300), device="cuda").t())
+
+
+def test_outputs_of_the_caller():
+    torch, dstd = _torch()
+    x = torch.randn(20, 500, device="cuda")
+    i, l, r = torch.empty((20, 4), dtype=torch.int32, device="cuda"), torch.empty((20, 4), device="cuda"), torch.empty(20, device="cuda")
+    assert [a is b for a, b in zip(dstd.top_logits(x, 4, idx=i, logit=l, rest=r), (i, l, r))] == [True] * 3
+    c, p = torch.empty(20, dtype=torch.int32, device="cuda"), torch.empty(20, device="cuda")
+    assert [a is b for a, b in zip(dstd.sample(x, r.clamp(0, 0.5), choice=c, logp=p), (c, p))] == [True] * 2
+    with pytest.raises(dstd.DSTDError):  # the scores' own memory
+        dstd.sample(x, r, choice=x.view(torch.int32).view(-1)[:20])
+    with pytest.raises(dstd.DSTDError):
+        dstd.distill_grad(x, i, l, r, t_cap=1.0, grad=x)
+    with pytest.raises(TypeError):
+        dstd.sample(x, r, choice=c.long())
+    with pytest.raises(ValueError):
+        dstd.top_logits(x, 4, idx=i[:, :3])
+    with pytest.raises(ValueError):
+        dstd.distill_grad(x, i, l, r)  # no t_cap
+    with pytest.raises(ValueError):
+        dstd.distill_grad(x, i, l[:, :2], r, t_cap=1.0)
+    with pytest.raises(ValueError):
+        dstd.distill_grad(x, i, l, r, t_cap=1.0, accumulate=True)
+
+
+def test_a_student_learns_from_a_teacher():
+    """A run of all three: the teacher's record from its spike times, the student's layer
+    forward, its loss and gradients, an update, and a drawn answer. The weights' gradient
+    is the loss's difference along a direction."""
+    torch, dstd = _torch()
+    rng = np.random.default_rng(3)
+    B, N_in, N, M, tau, cap = 64, 96, 500, 16, 0.2, 1.6
+    p = dstd.make_params(1.0, 0.3, 1.0, M, 0.0, 1.0 / M)
+    t_in = torch.from_numpy(rng.random((B, N_in)).astype(np.float32)).cuda()
+    W_t, W_s = (torch.from_numpy((7.0 / N_in * (1 + 0.3 * math.sqrt(N_in) * rng.standard_normal((N, N_in))))
+                                 .astype(np.float32)).cuda() for _ in range(2))
+    idx, logit, rest = dstd.top_logits(dstd.forward(p, t_in, W_t)[0], 40, scale=-1.0 / tau, cap=cap)
+    u = torch.from_numpy(rng.random(B).astype(np.float32)).cuda()
+
+    def loss_of(W):
+        t, slope, q = dstd.forward(p, t_in, W)
+        return t, slope, q, dstd.distill_grad(t, idx, logit, rest, tau_soft=tau, t_cap=cap)
+
+    t, slope, q, (g, loss) = loss_of(W_s)
+    e_loss, e_grad, _ = ref.distill(t.cpu().numpy(), idx.cpu().numpy(), logit.cpu().numpy(), rest.cpu().numpy(),
+                                    float(np.float32(tau)), float(np.float32(cap)), 1.0 / B)
+    assert abs(float(loss[0]) - e_loss.sum()) <= 1e-4 * abs(e_loss.sum())
+    gW = torch.empty_like(W_s)
+    dstd.backward(p, t_in, W_s, t, slope, q, g, need_t_in=False, grad_W=gW)
+    tl = dstd.make_tensor_list([gW], weights=[W_s.clone()], m=[torch.zeros_like(W_s)], v=[torch.zeros_like(W_s)])
+    norm = dstd.adamw_step(tl, dstd.make_adamw(lr=1e-3, max_norm=1.0), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    choice, logp = dstd.sample(t, u, scale=-1.0 / tau, cap=cap, top_k=10)
+    w = ref.kept(t.cpu().numpy(), -1.0 / tau, cap, 10, 1.0, 0.0)
+    torch.cuda.synchronize()
+    assert math.isfinite(float(norm)) and float(norm) > 0
+    assert all(w[b, c] > 0 for b, c in enumerate(choice.tolist()))
+    # the layer's own gradient through its loss: only the outputs' part is checked here
+    assert np.allclose(g.cpu().numpy(), e_grad, rtol=1e-3, atol=1e-6 / B)
