@@ -317,6 +317,10 @@ typedef struct {
 dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float *logit,
                             float *rest, void *stream);
 
+/* Workspace bytes of dstd_distill_grad; 0 where it needs none (ws may then be
+   NULL), and for invalid arguments (the call then reports the error). */
+size_t dstd_distill_workspace_size(int64_t B, int64_t N, int64_t K);
+
 /*
  * Distillation from a teacher's top logits: the Kullback-Leibler divergence of
  * the softmax of a student's output spike times (logits -t/tau_soft, neurons
@@ -332,14 +336,14 @@ dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float
  *               named twice has both probabilities. A row without entries (a
  *               padded one) has no loss and no gradient.
  *  rest  [B]    logits of the rest; one that is not finite says p_rest = 0.
- *  weight       factor of loss and gradient, finite and >= 0 (1/B: batch mean).
+ *  weight       factor of loss and gradient, >= 0, weight / tau_soft finite (1/B:
+ *               batch mean).
  *  grad_t       out, B rows of N, ld_g apart: dL/dt, added to what is there
  *               with accumulate = 1 (another loss's gradient), written with 0;
  *               NULL: the loss alone.
  *  loss  [B + 1] out: loss[0] = L, loss[1 + b] = L_b, as in dstd_softmax_ce_grad.
  * 1 <= K <= min(N, DSTD_MAX_TOP); other sizes, and overlaps, as for dstd_scores.
  */
-size_t dstd_distill_workspace_size(int64_t B, int64_t N, int64_t K);
 dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_out, int64_t ld_t,
                               const int32_t *idx, const void *logit, dstd_dtype logit_dtype,
                               const float *rest, float tau_soft, float t_cap, float weight,

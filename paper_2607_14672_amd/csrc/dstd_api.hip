@@ -1436,7 +1436,7 @@ dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float
 
 size_t dstd_distill_workspace_size(int64_t B, int64_t N, int64_t K) {
     if (check_rows(B, N, N, "t_out") != DSTD_OK || check_top(K, N) != DSTD_OK) return 0;
-    return align_up(std::max<size_t>((size_t)(B * dstd::distill_parts(N)) * sizeof(float2), 1));
+    return align_up((size_t)(B * dstd::distill_parts(B, N)) * sizeof(float2));
 }
 
 dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_out, int64_t ld_t,
@@ -1466,7 +1466,7 @@ dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_ou
                             Place{rest, (size_t)B * 4, 4, false, "rest"},
                             Place{grad_t, rows_bytes(B, N, ld_g, 4), 4, true, "grad_t"},
                             Place{loss, (size_t)(B + 1) * 4, 4, true, "loss"},
-                            Place{ws, need, kAlign, true, "the workspace"}})) != DSTD_OK)
+                            Place{need ? ws : nullptr, need, kAlign, true, "the workspace"}})) != DSTD_OK)
         return st;
     dstd::KdArgs a{};
     a.N = (int)N;

@@ -119,7 +119,7 @@ hipError_t launch_sample(const SampleJob &j, hipStream_t st);
 constexpr int kMaxPicked = 1024;
 hipError_t launch_sample_picked(const SampleJob &j, hipStream_t st);
 
-// inv = 1 / tau_soft, c2 = log2(e) / tau_soft; part: distill_parts(N) for each row.
+// inv = 1 / tau_soft, c2 = log2(e) / tau_soft; part: distill_parts(B, N) for each row.
 constexpr int kKdMaxK = 256;
 struct KdArgs {
     int N, K;
@@ -134,9 +134,9 @@ struct KdArgs {
     float *loss;
     float2 *part;
 };
-// per row: a sum for each chunk of the classes, and three of its record
+// per row of several blocks: a sum for each chunk of the classes, and three of its record
 __host__ __device__ constexpr int64_t kd_row_parts(int64_t chunks) { return chunks + 3; }
-int64_t distill_parts(int64_t N);
+int64_t distill_parts(int64_t B, int64_t N);  // 0: a row is one block's
 hipError_t launch_distill(const KdArgs &a, int64_t B, const void *logit, bool bf16, hipStream_t st);
 
 // ------------------------------------------------------------------ conv --

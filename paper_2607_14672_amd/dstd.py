@@ -857,7 +857,8 @@ def top_logits(x, K: int, scale: float = 1.0, cap: Optional[float] = None, idx=N
     x = _rows(x, (torch.float32, torch.bfloat16), "x")
     dev, B = x.device, x.shape[0]
     idx = _out(torch, idx, (B, max(K, 0)), torch.int32, dev, "idx")
-    logit = _out(torch, logit, (B, max(K, 0)), torch.float32, dev, "logit")
+    logit = (torch.empty_like(idx, dtype=torch.float32) if logit is None else  # half an empty()'s host time
+             _given(logit, (B, max(K, 0)), torch.float32, dev, "logit"))
     rest = _out(torch, rest, (B,), torch.float32, dev, "rest")
     _on(torch, dev, "dstd_top_logits", dstd_top_logits, make_scores(x, scale, cap), K, idx.data_ptr(),
         logit.data_ptr(), rest.data_ptr())
@@ -894,11 +895,13 @@ def distill_grad(t_out, idx, logit, rest=None, tau_soft: float = 1.0, t_cap: Opt
     loss = _out(torch, loss, (B + 1,), torch.float32, dev, "loss")
     if weight is None:
         weight = 1.0 / max(B, 1)
-    ws = _ws_for(torch, ws, dstd_distill_workspace_size(B, N, K), dev)
+    need = dstd_distill_workspace_size(B, N, K)
+    if need > 0:
+        ws = _ws_for(torch, ws, need, dev)
     _on(torch, dev, "dstd_distill_grad", dstd_distill_grad, B, N, K, t_out.data_ptr(), _ld(t_out),
         idx.data_ptr(), logit.data_ptr(), DSTD_BF16 if bf16 else DSTD_F32, _ptr(rest), tau_soft, t_cap,
         weight, 1 if accumulate else 0, _ptr(grad), _ld(grad) if need_grad else 0, loss.data_ptr(),
-        ws.data_ptr(), ws.numel())
+        ws.data_ptr() if need > 0 else None, ws.numel() if need > 0 else 0)
     return grad, loss
 
 
@@ -913,8 +916,9 @@ def sample(x, u, scale: float = 1.0, cap: Optional[float] = None, top_k: int = 0
     x = _rows(x, (torch.float32, torch.bfloat16), "x")
     dev, B = x.device, x.shape[0]
     _given(u, (B,), torch.float32, dev, "u")
-    choice = _out(torch, choice, (B,), torch.int32, dev, "choice")
-    logp = _out(torch, logp, (B,), torch.float32, dev, "logp")
+    choice = (torch.empty_like(u, dtype=torch.int32) if choice is None else
+              _given(choice, (B,), torch.int32, dev, "choice"))
+    logp = torch.empty_like(u) if logp is None else _given(logp, (B,), torch.float32, dev, "logp")
     _on(torch, dev, "dstd_sample", dstd_sample, make_scores(x, scale, cap),
         dstd_sample_params(int(top_k), float(top_p), float(min_p)), u.data_ptr(), choice.data_ptr(),
         logp.data_ptr())

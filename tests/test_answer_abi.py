@@ -92,17 +92,19 @@ def _distill(B=4, N=100, K=5, t=X, ld_t=None, idx=IDX, logit=LOGIT, dtype=dstd.D
     (dict(cap=math.inf), PARAM), (dict(cap=math.nan), PARAM), (dict(weight=-1.0), PARAM),
     (dict(weight=math.inf), PARAM), (dict(weight=math.nan), PARAM), (dict(acc=2), PARAM),
     (dict(t=None), NULL), (dict(idx=None), NULL), (dict(logit=None), NULL), (dict(loss=None), NULL),
-    (dict(ws=None), NULL), (dict(ws=WSP + 8), WS), (dict(size=1), WS), (dict(t=X + 1), PARAM),
+    (dict(N=100000, ws=None), NULL), (dict(N=100000, ws=WSP + 8), WS),
+    (dict(N=100000, size=1), WS), (dict(t=X + 1), PARAM), (dict(weight=1e38, tau=1e-3), PARAM),
     (dict(grad=X), PARAM), (dict(grad=X + 4 * 399), PARAM), (dict(ld_t=1000, grad=X + 4 * 3000), PARAM),
     (dict(loss=GRAD + 4 * 399), PARAM), (dict(loss=REST + 8), PARAM), (dict(rest=GRAD), PARAM),
-    (dict(idx=GRAD), PARAM), (dict(ws=IDX), PARAM), (dict(logit=LOGIT + 2), PARAM),
+    (dict(idx=GRAD), PARAM), (dict(N=100000, ws=IDX), PARAM), (dict(logit=LOGIT + 2), PARAM),
 ])
 def test_distill_arguments(kw, status):
     assert _distill(**kw) == status, dstd.dstd_last_error()
 
 
 def test_workspace_sizes_grow_with_what_they_hold():
-    assert dstd.dstd_distill_workspace_size(0, 10, 1) > 0
+    assert dstd.dstd_distill_workspace_size(1, 10, 1) == 0  # none is needed
+    assert dstd.dstd_distill_workspace_size(1, 1 << 20, 1) >= 128 * 8
     assert dstd.dstd_distill_workspace_size(65535, (1 << 24) - 1, 256) > 65535 * 8
     for bad in ((-1, 10, 1), (1, 0, 1), (1, 10, 11), (1, 1000, 257)):
         assert dstd.dstd_distill_workspace_size(*bad) == 0
