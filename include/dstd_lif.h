@@ -335,7 +335,8 @@ size_t dstd_distill_workspace_size(int64_t B, int64_t N, int64_t K);
  *               [0, N), or whose logit is not finite, is none; a class that is
  *               named twice has both probabilities. A row without entries (a
  *               padded one) has no loss and no gradient.
- *  rest  [B]    logits of the rest; one that is not finite says p_rest = 0.
+ *  rest  [B]    logits of the rest; one that is not finite says p_rest = 0. (A
+ *               record that names all classes and a rest has the loss +inf.)
  *  weight       factor of loss and gradient, >= 0, weight / tau_soft finite (1/B:
  *               batch mean).
  *  grad_t       out, B rows of N, ld_g apart: dL/dt, added to what is there

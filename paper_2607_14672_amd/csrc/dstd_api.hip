@@ -398,7 +398,7 @@ const char *dstd_status_string(dstd_status s) {
 
 const char *dstd_last_error(void) { return g_err; }
 
-int32_t dstd_version(void) { return 101; }
+int32_t dstd_version(void) { return 102; }
 
 size_t dstd_lif_forward_workspace_size(const dstd_lif_params *p, int64_t B, int64_t N_in,
                                        int64_t N_out) {

@@ -51,8 +51,13 @@ __device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const
     draw_kept<T, kAhead>(sh, row, b, n, mass, kept, a, [&](float x) { return goodness(x, m); });
 }
 
-// One class of every row.
-// kCount, kMass: with top_k (more than kMaxPicked), with top_p.
+// One class of every row, a block each (threads as in dstd_top.hip): the largest score,
+// then what top_k and top_p keep, then the draw: two readings of the row, and two or three
+// more for each filter. Bound by its fp64 operations, some 30 an entry and reading of
+// weights: 300 x 50021 without filters 40 us (the reads alone would take 20), 105 with top_p.
+// kCount, kMass: with top_k (more than kMaxPicked), with top_p; a kernel for each, since what
+// one of them needs in registers would be taken from the others' loops (top_p's 105 us were
+// 238 in a kernel of both).
 template <int T, bool kCount, bool kMass, typename E>
 __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
                                                                       ScoreMap m, DrawArgs a) {
@@ -85,6 +90,12 @@ __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int
 // entry. Zeros are counted apart; the few values nearer to 0 are listed one by one; what is
 // larger with a goodness below 0 has to weigh nothing. Other rows are drawn from by their
 // definition.
+//
+// Two passes, 64 KB of LDS a block (two a CU): the counts (an LDS atomic an entry), then,
+// once the weights have taken the counts' place, their sums by parts of the row (a look-up
+// an entry). 64 x 131072 with top_p 0.95: 29 us, 8 for the counts, 9 for the values (their
+// exponentials twice, which is faster than held in registers: 38), 5 for the look-ups; an
+// exponential an entry took 546. 512 rows: 62 us.
 constexpr int kMags = 4096, kFirstMag = 0x3380, kValues = 2 * kMags;
 using u32x4 = u32 __attribute__((ext_vector_type(4)));
 using u16x2 = uint16_t __attribute__((ext_vector_type(2)));

@@ -473,6 +473,62 @@ def test_rows_far_apart():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("B,N,K", [(65535, 3, 2), (65535, 1, 1), (1, (1 << 24) - 1, 4)])
+def test_largest_sizes(B, N, K):
+    torch, dstd = _torch()
+    print(f"largest B={B} N={N}", flush=True)
+    t = _times(B, N, 1)
+    _check_top(torch, dstd, t, torch.float32, K, -4.0, 1.5)
+    _check_sample(torch, dstd, t, torch.float32, -4.0, 1.5, 0, 0.9, 0.0)
+    rng = np.random.default_rng(2)
+    idx = rng.integers(0, N, (B, K)).astype(np.int32)
+    logit = rng.standard_normal((B, K)).astype(np.float32)
+    rest = rng.standard_normal(B).astype(np.float32) if N > 3 else None
+    if B * N < 1 << 20:
+        t, idx, logit = t[-300:], idx[-300:], logit[-300:]
+        g, loss = dstd.distill_grad(*(torch.from_numpy(v).cuda() for v in (_times(B, N, 1), np.resize(idx, (B, K)),
+                                                                            np.resize(logit, (B, K)))),
+                                    tau_soft=0.25, t_cap=1.5, weight=1.0)
+        e_loss, e_grad, _ = ref.distill(t, np.resize(idx, (B, K))[-300:], np.resize(logit, (B, K))[-300:], None, 0.25,
+                                        1.5, 1.0)
+        torch.cuda.synchronize()
+        assert np.allclose(g[-300:].cpu().numpy(), e_grad, rtol=0, atol=1e-4)
+        assert np.allclose(loss[-300:].cpu().numpy(), e_loss, rtol=1e-4, atol=1e-5)
+    else:
+        _check_distill(torch, dstd, t, idx, logit, rest, 0.25, 1.5, 1.0, "f32")
+
+
+@pytest.mark.parametrize("scale", [1e38, -1e38, 1e-38, -1e-42, 1e-3])
+@pytest.mark.parametrize("N", [100, 3000, 20011])
+def test_scales_at_the_ends_of_fp32(scale, N):
+    """Logits beyond fp32 read inf; choices hold all the same."""
+    torch, dstd = _torch()
+    x = _scores("ties", 4, N, 5)
+    scale = float(np.float32(scale))
+    for dt in (torch.float32, torch.bfloat16):
+        v = _put(torch, x, dt)
+        idx, logit, rest = dstd.top_logits(v, 7, scale=scale)
+        e_idx, e_logit, _ = ref.top(x, 7, scale, None)
+        assert np.array_equal(idx.cpu().numpy(), e_idx)
+        with np.errstate(over="ignore"):
+            assert np.array_equal(logit.cpu().numpy(), e_logit.astype(np.float32))
+        assert not torch.isnan(rest).any()
+        _check_sample(torch, dstd, x, dt, scale, None, 0, 0.7, 0.0)
+        _check_sample(torch, dstd, x, dt, scale, None, 5, 1.0, 0.0)
+
+
+def test_record_that_names_all_classes():
+    """Without a rest nothing is left outside; with one the loss says so."""
+    torch, dstd = _torch()
+    t = torch.from_numpy(_times(3, 8, 3)).cuda()
+    idx = torch.arange(8, dtype=torch.int32, device="cuda").repeat(3, 1)
+    logit = torch.randn(3, 8, device="cuda")
+    g, loss = dstd.distill_grad(t, idx, logit, tau_soft=0.5, t_cap=1.5)
+    h, more = dstd.distill_grad(t, idx, logit, torch.zeros(3, device="cuda"), tau_soft=0.5, t_cap=1.5)
+    assert torch.isfinite(loss).all() and (loss[1:] >= 0).all()
+    assert (more == math.inf).all() and torch.isfinite(g).all() and torch.isfinite(h).all()
+
+
 def test_views_are_read_as_they_are():
     """Transposed, stepped and reversed-stride views give what their copies give."""
     torch, dstd = _torch()
