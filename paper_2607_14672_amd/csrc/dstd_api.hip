@@ -1503,7 +1503,7 @@ dstd_status dstd_sample(const dstd_scores *s, const dstd_sample_params *p, const
     int bits = 0;  // ceil(log2 N)
     while (((int64_t)1 << bits) < s->N) ++bits;
     j.shift = std::min(51, 62 - bits);
-    j.top_k = (int)std::min<int64_t>(p->top_k, s->N);
+    j.top_k = p->top_k < s->N ? (int)p->top_k : 0;
     j.top_p = p->top_p;
     j.min_p = p->min_p;
     j.u = u;

@@ -458,16 +458,23 @@ hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
     const ScoreMap m{j.in.cap, j.in.flip};
     const DrawArgs a = draw_args(j);
     const E *x = static_cast<const E *>(j.in.x);
+    const bool filters = (a.top_k > 0 && a.top_k < n) || a.top_p < 1.0;
+    // Counting values pays where a filter needs the order (bf16, top_p 0.9, counted and by
+    // definition: 512 x 2500 21 and 26 us, 64 x 5000 14 and 26), else on long rows only (2000
+    // x 15000 without filters 84 and 44).
     if constexpr (sizeof(E) == 2) {
         u32 cap;
-        if (n > 4096 && cap_has_slot(j.in.cap, &cap)) {
+        if (n > (filters ? 2048 : 16384) && cap_has_slot(j.in.cap, &cap)) {
             const OneSlot one{j.in.flip >> 16, cap};
             hipLaunchKernelGGL((sample_values_kernel<1024>), grid, dim3(1024), 0, st, n, j.in.ld, x, m, one, a);
             return hipGetLastError();
         }
     }
+    // Threads a row: small blocks overlap each other's steps, large ones take a long row
+    // sooner (fp32, 256 and 1024 threads: 2000 x 9000 34 and 44 us without filters, 78 and 114
+    // with top_p; 64 x 15000 with top_p 35 and 25).
     if (n <= 512) launch_sample_rows<64, E>(grid, st, n, j.in.ld, x, m, a);
-    else if (n <= 4096) launch_sample_rows<256, E>(grid, st, n, j.in.ld, x, m, a);
+    else if (n <= (filters ? 8192 : 16384)) launch_sample_rows<256, E>(grid, st, n, j.in.ld, x, m, a);
     else launch_sample_rows<1024, E>(grid, st, n, j.in.ld, x, m, a);
     return hipGetLastError();
 }

@@ -45,17 +45,16 @@ struct Mass {
     __device__ double span() const { return 0.6931471805599453 * (shift + 1) / scale; }
     __device__ double distance(float y) const { return (top - static_cast<double>(y)) * scale; }
     __device__ double distance(u32 key) const { return distance(value_of(key)); }
-    // rint(e^-d 2^shift): d = n ln 2 + r, e^-r by its series to r^12 / 12! (|r| <= ln 2 / 2:
-    // 2^-52 relative), n taken off its exponent. Adding 2^52 leaves the integer in the low
-    // bits. From d = 64 on (and for NaN) the result is 0.
+    // rint(e^-d 2^shift): d = n ln 2 + r, e^-r by its series to r^11 / 11! (|r| <= ln 2 / 2:
+    // 2^-47 relative at the ends; ln 2 is a double, 2^-55 n off), n taken off its exponent.
+    // Adding 2^52 leaves the integer in the low bits. From d = 64 on (and for NaN) it is 0.
     static __device__ __forceinline__ u64 fixed_exp(double d, int shift) {
         d = fmin(d, 64.0);
         const double big = 0x1.8p52;
         const double t = fma(d, 1.4426950408889634, big);
         const double n = t - big;
-        const double r = fma(n, -0x1.abc9e3b39803fp-56, fma(n, -0x1.62e42fefa39efp-1, d));
-        double p = 1.0 / 479001600;
-        p = fma(p, -r, 1.0 / 39916800);
+        const double r = fma(n, -0x1.62e42fefa39efp-1, d);
+        double p = 1.0 / 39916800;
         p = fma(p, -r, 1.0 / 3628800);
         p = fma(p, -r, 1.0 / 362880);
         p = fma(p, -r, 1.0 / 40320);

@@ -7,9 +7,9 @@
 // below, then what reaches the bound is listed and what does not is summed. The order is
 // that of the scores themselves, not of their products with the scale.
 //
-// A block a row: 64 threads up to 512 scores (which are all listed), 256 up to 4096 (with
-// K up to 256), 1024 beyond, two of those a CU (64 registers a thread: more loads on the
-// way from two blocks than from one of 128). Many long rows are bound by their two passes
+// A block a row: 64 threads up to 512 scores (which are all listed), 256 up to kShortRow
+// (with K up to 256), 1024 beyond, two of those a CU (64 registers a thread: more loads on
+// the way from two blocks than from one of 128). Many long rows are bound by their two passes
 // (512 x 131072 bf16: 53 us, 268 MB leave the L2; 6 TB/s would be 44), a few by the issue
 // rate of the CU that has one (131072 bf16: 21 us, 35000 operations, one a clock).
 #include "dstd_profile.h"
@@ -19,6 +19,9 @@ namespace dstd {
 
 namespace {
 
+// Small blocks overlap each other's steps (top 32 of 2000 x 15000 bf16: 31 us with 256
+// threads, 52 with 1024; 64 rows: 12.5 with either).
+constexpr int kShortRow = 16384;
 // groups of a thread's share of the row, a maximum each: by the place in a vector, so that
 // short rows have as many as long ones
 template <typename E> constexpr int kGroups = RowVec<E>::n;
@@ -378,7 +381,7 @@ template <int T, typename E> void launch_picked_t(const SampleJob &j, hipStream_
 }
 template <typename E> void launch_picked(const SampleJob &j, hipStream_t st) {
     if (j.in.N <= 512) launch_picked_t<64, E>(j, st);
-    else if (j.in.N <= 4096 && j.top_k <= 256) launch_picked_t<256, E>(j, st);
+    else if (j.in.N <= kShortRow && j.top_k <= 256) launch_picked_t<256, E>(j, st);
     else launch_picked_t<1024, E>(j, st);
 }
 
@@ -397,7 +400,7 @@ hipError_t launch_top_t(const TopJob &j, hipStream_t st) {
         hipLaunchKernelGGL((top_logits_kernel<T, false, E>), grid, dim3(T), 0, st, n, j.in.ld, x, m,            \
                            j.in.scale, c2, j.K, j.idx, j.logit, j.rest)
     if (n <= 512) TOP(64);
-    else if (n <= 4096) TOP(256);
+    else if (n <= kShortRow) TOP(256);
     else TOP(1024);
 #undef TOP
     return hipGetLastError();
