@@ -159,7 +159,7 @@ template <int T, int V> struct KdShared {
 };
 
 template <int T, int V, typename L>
-__global__ __launch_bounds__(T) void distill_row_kernel(KdArgs a, const L *__restrict__ logit) {
+__global__ __launch_bounds__(T, V >= 16 ? 4 : 1) void distill_row_kernel(KdArgs a, const L *__restrict__ logit) {
     __shared__ KdShared<T, V> sh;
     const int64_t b = blockIdx.x;
     const int tid = threadIdx.x, lane = tid % kWave, n = a.N;
@@ -414,10 +414,12 @@ template <typename L> void launch_t(const KdArgs &a, int64_t B, const L *logit, 
         launch_row<64, 4>(a, B, logit, st);
     } else if (n <= 4096) {
         launch_row<256, 4>(a, B, logit, st);
+    } else if (n <= 8192) {
+        launch_row<256, 8>(a, B, logit, st);
     } else if (n <= 16384) {
-        launch_row<512, 8>(a, B, logit, st);
+        launch_row<256, 16>(a, B, logit, st);
     } else if (n <= 32768) {
-        launch_row<1024, 8>(a, B, logit, st);
+        launch_row<512, 16>(a, B, logit, st);
     } else {
         launch_row<1024, 16>(a, B, logit, st);
     }
