@@ -128,7 +128,7 @@ struct KdArgs {
     const int32_t *idx;
     const float *rest;
     float inv, c2, t_cap, weight;
-    int accumulate;
+    int accumulate, alone;  // alone: there is one row
     float *grad;
     int64_t ld_g;
     float *loss;

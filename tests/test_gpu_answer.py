@@ -184,6 +184,10 @@ def _check_distill(torch, dstd, t, idx, logit, rest, tau, t_cap, weight, dtype, 
     ltol = weight * (4 * eps(N) + 16 * H * zmax + len(idx[0]) * H * zmax)
     assert np.all(np.abs(loss[1:] - e_loss) <= ltol), (loss[1:], e_loss, ltol)
     assert abs(loss[0] - loss[1:].astype(np.float64).sum()) <= H * (B + 8) * np.abs(loss[1:]).sum()
+    if B > 1:  # one row by itself
+        one = dstd.distill_grad(tv[1:2], iv[1:2], lv[1:2], None if rv is None else rv[1:2], tau_soft=tau, t_cap=t_cap,
+                                weight=weight, need_grad=False)[1].cpu().numpy()
+        assert one[0] == one[1] and abs(one[1] - e_loss[1]) <= ltol[1]
 
 
 def _times(B, N, seed, silent=0.2):
