@@ -414,10 +414,11 @@ def test_calls_on_another_stream_and_two_at_once():
         assert _same(torch, want[k % len(calls)], g), calls[k % len(calls)][0]
 
 
-def test_captured_calls_replay():
-    """Each call captured, replayed between eager work, on inputs that change."""
+@pytest.mark.parametrize("B,N", [(33, 5003), (3, 20011), (1, 70001)])
+def test_captured_calls_replay(B, N):
+    """Each call captured, replayed between eager work, on inputs that change; two graphs
+    side by side."""
     torch, dstd = _torch()
-    B, N = 33, 5003
     x = torch.empty((B, N), dtype=torch.bfloat16, device="cuda")
     t = torch.empty((B, N), device="cuda")
     u = torch.empty(B, device="cuda")
