@@ -236,9 +236,10 @@ __global__ __launch_bounds__(T, V >= 16 ? 4 : 1) void distill_row_kernel(KdArgs 
     }
     if (silent > 0) top = fmaxf(top, -a.t_cap);
     top = value_of(block_max<T>(key_of(top), sh.red));
-    // 2^(c2 y - kb); kb may leave fp32 where times are huge, then by the difference itself
+    // 2^(c2 y - kb), off by the rounding of kb, half a binary order at most up to 2^24 (from
+    // 2^31 on it may be more than fp32 holds); beyond by the difference itself
     const float ref = top > -INFINITY ? top : 0.f, kb = ref * a.c2;
-    const bool fits = isfinite(kb);
+    const bool fits = fabsf(kb) < 0x1p24f;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j)
