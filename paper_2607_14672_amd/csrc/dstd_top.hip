@@ -185,10 +185,11 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     __syncthreads();
     if (threadIdx.x == 0) sh.count = sh.seen = 0;
     __syncthreads();
-    // what is below the bound is summed relative to it, as 2^(c x - kb); NaN adds 0
+    // what is below the bound is summed relative to it, as 2^(c x - kb); NaN adds 0. The
+    // rounding of kb is half a binary order at most
     float kb = bound * c2, sum = 0.f;
     const float c = m.flip ? -c2 : c2;
-    const bool sums = bound > -FLT_MAX && isfinite(kb);
+    const bool sums = bound > -FLT_MAX && fabsf(kb) < 0x1p24f;
     if (!sums) kb = 0.f;
     auto term = [&](float x) {
         return __builtin_amdgcn_exp2f(fmaxf(fmaf(x, c, -kb), -1000.f));

@@ -1,0 +1,62 @@
+"""The rest of a softmax behind its top logits where the others lie far below them, or scores
+far from 0.
+
+Tolerance: a term of the sum takes a difference, the scale and their product with half a step
+(H) each, 3 H of its distance to the others' largest (ln N of them at the mean at most); exp2
+is two half steps off, again at each of the some 30 places where partial sums are joined, and
+a thread adds N over its block's threads (64 up to 512 scores, 256 up to 16384, 1024 beyond)
+one by one. The result is rounded once."""
+import math
+
+import numpy as np
+import pytest
+
+from tests import answer_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+H = 2.0 ** -24
+
+
+def eps(N):
+    T = 64 if N <= 512 else 256 if N <= 16384 else 1024
+    return H * (3 * math.log(N + 1) + 2 * 30 + 4 + math.ceil(N / T))
+
+
+def _torch():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2607_14672_amd import dstd
+    return torch, dstd
+
+
+def _check_rest(torch, dstd, x, dtype, K, scale, cap=None):
+    v = torch.from_numpy(x).to(dtype).cuda()
+    idx, logit, rest = (a.cpu().numpy() for a in dstd.top_logits(v, K, scale=scale, cap=cap))
+    e_idx, e_logit, e_rest = ref.top(v.float().cpu().numpy(), K, scale, cap)
+    assert np.array_equal(idx, e_idx)
+    f = np.isfinite(e_logit)
+    assert np.all(np.abs(logit[f] - e_logit[f]) <= H * np.abs(e_logit[f]))
+    bad = np.isfinite(rest) != np.isfinite(e_rest)
+    assert not bad.any(), (np.argwhere(bad)[:4].ravel(), rest[bad][:4], e_rest[bad][:4])
+    bad = np.isfinite(e_rest)
+    bad[bad] = np.abs(rest[bad] - e_rest[bad]) > eps(x.shape[1]) + H * np.abs(e_rest[bad])
+    assert not bad.any(), (np.argwhere(bad)[:4].ravel(), rest[bad][:4], e_rest[bad][:4])
+
+
+@pytest.mark.parametrize("N", [400, 2000, 20011])
+@pytest.mark.parametrize("power", [20, 24, 28, 34, 60])
+def test_scores_whose_logits_are_beyond_the_integers_of_fp32(N, power):
+    """One entry a row at the top, the others a step of fp32 below it, with logits just above
+    a power of two, where the product with log2(e) is rounded by up to a step of theirs."""
+    torch, dstd = _torch()
+    scale = 0.7
+    c2 = np.float32(scale * math.log2(math.e))
+    top = np.float32(2.0 ** power / float(c2))
+    x = np.empty((400, N), dtype=np.float32)
+    for b in range(x.shape[0]):
+        top = np.nextafter(top, np.float32(np.inf))
+        x[b] = np.nextafter(top, np.float32(0))
+        x[b, b * 7 % N] = top
+    _check_rest(torch, dstd, x, torch.float32, 1, scale)
+    _check_rest(torch, dstd, -x, torch.float32, 1, -scale)
