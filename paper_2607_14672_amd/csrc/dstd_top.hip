@@ -250,7 +250,9 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     }
     __syncthreads();
     int count = sh.count;
-    bool listed = bound == -FLT_MAX;  // the sum is that of the list's others alone
+    // Whether the others' sum is that of the list and of `sum`: the list holds all others,
+    // or one of them that reached the bound, beside which what is 0 in fp32 counts for nothing.
+    bool listed = bound == -FLT_MAX || (sums && count > K);
     if (count > kList<T>) {
         count = pick_exactly<T, E>(sh, row, n, m, K);
         sum = 0.f;
@@ -260,14 +262,16 @@ __device__ int candidates(RowShared<T> &sh, const E *row, int n, const ScoreMap 
     if (!kSum || count < K) return count;
     if (!sums) sum = 0.f;
     ExpSum s{-INFINITY, 0.f};
-    const bool some = __syncthreads_or(sum > 0.f);
+    // Else terms below 2^-126 are missing: 2^24 of them are 2^-26 of a sum of 2^-76
+    const bool some = __syncthreads_or(sum >= 0x1p-76f);
     if (some || listed) {
         // kb was rounded
         if (sum > 0.f) s = ExpSum{bound, sum * __builtin_amdgcn_exp2f(-fmaf(bound, c2, -kb))};
         for (int k = K + threadIdx.x; k < count; k += T)
             s = exp_join(s, ExpSum{value_of(rank_key(sh.list[k])), 1.f}, c2);
     } else {
-        // all others far below the bound (their sum there is 0), or no bound was found
+        // all others lie so far below the bound that terms are lost there, or their sum was
+        // not formed (logits beyond 2^24, more candidates than the list holds)
         s = sum_behind<T, E>(row, n, m, sh.list[K - 1], c2);
     }
     *others = block_exp_sum<T>(s, c2, sh.red);

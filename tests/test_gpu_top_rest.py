@@ -44,6 +44,46 @@ def _check_rest(torch, dstd, x, dtype, K, scale, cap=None):
     assert not bad.any(), (np.argwhere(bad)[:4].ravel(), rest[bad][:4], e_rest[bad][:4])
 
 
+# how far below the top the others lie: around where an fp32 exponential becomes 0 (87.3) and
+# where even its denormal numbers end (104)
+GAPS = [50.0, 80.0, 85.0, 86.5, 87.0, 87.25, 87.5, 90.0, 100.0, 103.5, 104.5, 200.0]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [400, 2000, 20011, 131072])
+def test_others_far_below_the_top(N, dtype):
+    """Row by row another gap: the top K, one entry at the gap, the others half a unit and
+    more behind it."""
+    torch, dstd = _torch()
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng = np.random.default_rng(N)
+    for K in (1, 7):
+        for behind in (0.5, 3.0):
+            x = np.empty((len(GAPS), N), dtype=np.float32)
+            for b, gap in enumerate(GAPS):
+                x[b] = -gap - behind - rng.integers(0, 3, N) * 0.5
+                at = rng.permutation(N)[:K + 1]
+                x[b, at[:K]] = 0.5 * rng.integers(0, 4, K)
+                x[b, at[K]] = -gap
+            print(f"N={N} {dtype} K={K} behind={behind}", flush=True)
+            _check_rest(torch, dstd, x, dt, K, 1.0)
+            _check_rest(torch, dstd, x * -0.125, dt, K, -8.0)
+
+
+@pytest.mark.parametrize("N", [2000, 20011])
+def test_spike_times_of_a_cold_softmax(N):
+    """Spike times with tau_soft = 0.01: a class fires early, the others up to 1.5 later."""
+    torch, dstd = _torch()
+    rng = np.random.default_rng(N)
+    for start in (0.8, 0.85, 0.9, 1.0, 1.1):
+        t = (start + 0.3 * rng.random((8, N))).astype(np.float32)
+        t[rng.random(t.shape) < 0.3] = np.inf
+        t[:, N // 2] = 0.0
+        t[:, N // 3] = 0.01
+        _check_rest(torch, dstd, t, torch.float32, 2, -100.0, 1.5)
+        _check_rest(torch, dstd, t, torch.float32, 2, -100.0)
+
+
 @pytest.mark.parametrize("N", [400, 2000, 20011])
 @pytest.mark.parametrize("power", [20, 24, 28, 34, 60])
 def test_scores_whose_logits_are_beyond_the_integers_of_fp32(N, power):
