@@ -311,7 +311,8 @@ typedef struct {
  *  idx   [B][K] out: their classes; -1 where a row has fewer entries.
  *  logit [B][K] out: their logits, rounded to fp32; -inf there.
  *  rest  [B]    out: ln of the sum of e^z over all others, -inf without any; or
- *               NULL to skip.
+ *               NULL to skip. With it scale log2(e) has to be finite in fp32, too
+ *               (|scale| <= 2.35e38).
  * 1 <= K <= min(N, DSTD_MAX_TOP). Rows are ordered by their scores, exactly.
  */
 dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float *logit,

@@ -1425,6 +1425,9 @@ dstd_status dstd_top_logits(const dstd_scores *s, int64_t K, int32_t *idx, float
     dstd_status st = check_scores(s);
     if (st != DSTD_OK) return st;
     if ((st = check_top(K, s->N)) != DSTD_OK) return st;
+    // the sum's exponents are formed in base 2
+    if (rest && !isfinite((float)(s->scale * 1.4426950408889634)))
+        return fail(DSTD_ERR_PARAM, "scale * log2(e) must be finite in fp32 where rest is wanted (scale %g)", s->scale);
     if (s->B > 0 && (!s->x || !idx || !logit)) return fail(DSTD_ERR_NULL, "x, idx and logit are required");
     const size_t bk = (size_t)(s->B * K) * 4;
     if ((st = check_places({scores_place(s), Place{idx, bk, 4, true, "idx"}, Place{logit, bk, 4, true, "logit"},

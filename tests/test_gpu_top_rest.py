@@ -100,3 +100,42 @@ def test_scores_whose_logits_are_beyond_the_integers_of_fp32(N, power):
         x[b, b * 7 % N] = top
     _check_rest(torch, dstd, x, torch.float32, 1, scale)
     _check_rest(torch, dstd, -x, torch.float32, 1, -scale)
+
+
+@pytest.mark.parametrize("scale", [2.3e38, -2.3e38])
+@pytest.mark.parametrize("N", [400, 2000, 20011])
+def test_rest_at_the_largest_scales(N, scale):
+    """Scores of a few steps of 2^-128, whose logits are 0.7 apart."""
+    torch, dstd = _torch()
+    scale = float(np.float32(scale))
+    x = (np.random.default_rng(N).integers(-30, 30, (6, N)) * 2.0 ** -128).astype(np.float32)
+    x[0] = 0.0
+    for dt in (torch.float32, torch.bfloat16):
+        _check_rest(torch, dstd, x, dt, 1, scale)
+        _check_rest(torch, dstd, x, dt, 9, scale)
+
+
+def test_scales_beyond_those_of_rest():
+    """Top logits without a rest, and sampling, take every scale that is finite in fp32."""
+    torch, dstd = _torch()
+    scale = float(np.float32(3.3e38))
+    x = (np.random.default_rng(1).integers(-30, 30, (50, 3001)) * 2.0 ** -129).astype(np.float32)
+    v = torch.from_numpy(x).cuda()
+    with pytest.raises(dstd.DSTDError, match="log2"):
+        dstd.top_logits(v, 4, scale=scale)
+    idx = torch.empty((50, 4), dtype=torch.int32, device="cuda")
+    logit = torch.empty((50, 4), device="cuda")
+    st = dstd.dstd_top_logits(dstd.make_scores(v, scale), 4, idx.data_ptr(), logit.data_ptr(), None,
+                              torch.cuda.current_stream().cuda_stream)
+    assert st == dstd.DSTD_OK
+    e_idx, e_logit, _ = ref.top(x, 4, scale, None)
+    torch.cuda.synchronize()
+    assert np.array_equal(idx.cpu().numpy(), e_idx)
+    assert np.all(np.abs(logit.cpu().numpy() - e_logit) <= H * np.abs(e_logit))
+    c, logp = dstd.sample(v, torch.full((50,), 0.3, device="cuda"), scale=scale, top_p=0.9)
+    w = ref.kept(x, scale, None, 0, 0.9, 0.0)
+    cum = np.cumsum(w, axis=1)
+    for b, k in enumerate(c.tolist()):
+        # 3001 weights to 2^-51 each, and the reference's own sums
+        below, goal = (cum[b, k - 1] if k else 0.0), float(np.float32(0.3)) * cum[b, -1]
+        assert w[b, k] > 0 and below <= goal + 1e-10 and cum[b, k] > goal - 1e-10
