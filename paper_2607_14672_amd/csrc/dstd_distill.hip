@@ -107,17 +107,18 @@ struct RowFactors {
 // The loss of a row, by one wave.
 template <typename L>
 __device__ void put_loss(const KdArgs &a, int64_t b, const Entries<L> &e, const RecordSums &s, const RowFactors &f) {
-    // ln p_k = l_k - ln sum, ln q_k = (y_k - z.m) / tau - ln z.s
-    const float logp0 = s.p.m + logf(s.p.s), lz = logf(f.z.s);
+    // ln p_k = (l_k - p.m) - ln p.s, ln q_k = (y_k - z.m) / tau - ln z.s: a logarithm added
+    // to a large maximum would lose its digits
+    const float lp = logf(s.p.s), lz = logf(f.z.s);
     float term = 0.f;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         if (e.at[j] < 0) continue;
         const float p = exp_of(e.l[j] - s.p.m, kLog2e) / s.p.s;
-        if (p > 0.f) term += p * (e.l[j] - logp0 - ((e.y[j] - f.z.m) * a.inv - lz));
+        if (p > 0.f) term += p * (e.l[j] - s.p.m - lp - ((e.y[j] - f.z.m) * a.inv - lz));
     }
     if (threadIdx.x % kWave == 0 && f.pr > 0.f)
-        term += f.pr * (s.rest - logp0 - ((f.r.m - f.z.m) * a.inv + logf(f.r.s) - lz));
+        term += f.pr * (s.rest - s.p.m - lp - ((f.r.m - f.z.m) * a.inv + logf(f.r.s) - lz));
     term = block_add<kWave>(term, nullptr);
     if (threadIdx.x % kWave == 0) {
         const float loss = s.any ? term * a.weight : 0.f;

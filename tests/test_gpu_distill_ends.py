@@ -134,3 +134,32 @@ def test_times_far_from_zero(B, N):
             assert np.isfinite(loss).all() and np.abs(e_loss).max() < FMAX
             bad = np.abs(loss[1:] - e_loss) > ltol
             assert not bad.any(), (np.argwhere(bad)[:3], loss[1:][bad][:3], e_loss[bad][:3], ltol[bad][:3])
+
+
+@pytest.mark.parametrize("B,N,K", [(8, 10, 3), (8, 4096, 32), (8, 20000, 200), (40, 20000, 200), (1, 70000, 64)])
+@pytest.mark.parametrize("size", [1e4, 1e6, 1e8])
+def test_records_of_large_logits(B, N, K, size):
+    """A teacher whose logits are large and near each other: only their differences count,
+    which fp32 holds exactly here."""
+    torch, dstd = _torch()
+    rng = np.random.default_rng(N)
+    tau, t_cap = 0.125, 1.5
+    t, _ = _far_rows(B, N, K, tau, t_cap, rng)
+    t = np.where(np.isfinite(t) & (np.abs(t) <= 1), t, np.inf).astype(np.float32)
+    t[:, 0] = 0.25
+    idx = np.stack([rng.permutation(N)[:K] for _ in range(B)]).astype(np.int32)
+    step = float(np.spacing(np.float32(size)))
+    apart = max(step, 0.25)  # of fp32 around it, or a quarter
+    for sign in (1.0, -1.0):
+        logit = (sign * size + apart * rng.integers(-4, 5, (B, K))).astype(np.float32)
+        rest = (sign * size + apart * rng.integers(-4, 5, B)).astype(np.float32)
+        dev = [torch.from_numpy(v).cuda() for v in (t, idx, logit, rest)]
+        for r in (rest, None):
+            g, loss = dstd.distill_grad(dev[0], dev[1], dev[2], None if r is None else dev[3], tau_soft=tau,
+                                        t_cap=t_cap, weight=1.0)
+            torch.cuda.synchronize()
+            g, loss = g.cpu().numpy().astype(np.float64), loss.cpu().numpy().astype(np.float64)
+            e_loss, ltol, e_grad, gtol = reference(t, idx, logit, r, tau, t_cap, 1.0)
+            assert np.all(np.abs(g - e_grad) <= gtol)
+            bad = np.abs(loss[1:] - e_loss) > ltol
+            assert not bad.any(), (np.argwhere(bad)[:3], loss[1:][bad][:3], e_loss[bad][:3], ltol[bad][:3])
