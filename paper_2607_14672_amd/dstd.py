@@ -771,8 +771,8 @@ def _whole_rows(x):
     return (x.shape[1] <= 1 or x.stride(1) == 1) and (x.shape[0] <= 1 or x.stride(0) >= x.shape[1])
 
 
-def _rows(x, dtypes, what):
-    """A matrix on the GPU, copied only if its rows do not lie whole in memory."""
+def _matrix(x, dtypes, what):
+    """A matrix on the GPU, checked."""
     if not isinstance(x, _torch().Tensor):
         raise TypeError(f"{what} must be a tensor, got {type(x).__name__}")
     if x.dtype not in dtypes:
@@ -781,6 +781,12 @@ def _rows(x, dtypes, what):
         raise ValueError(f"{what} must live on the GPU")
     if x.dim() != 2:
         raise ValueError(f"{what} must have two dimensions, got {x.dim()}")
+    return x
+
+
+def _rows(x, dtypes, what):
+    """A matrix on the GPU, copied only if its rows do not lie whole in memory."""
+    _matrix(x, dtypes, what)
     return x if x.is_contiguous() or _whole_rows(x) else x.contiguous()
 
 
@@ -840,7 +846,17 @@ def _on(torch, dev, name, fn, *args):
 def make_scores(x, scale: float = 1.0, cap: Optional[float] = None) -> dstd_scores:
     """Rows of scores x [B, N], f32 or bf16, as top_logits and sample read them: logits
     scale * x. Entries that are not finite count as `cap`, or are left out (None).
-    It holds x's address, so x has to stay while it is used."""
+    It holds x's address, so x has to stay while it is used, and its rows have to lie
+    whole in memory."""
+    torch = _torch()
+    _matrix(x, (torch.float32, torch.bfloat16), "x")
+    if not (x.is_contiguous() or _whole_rows(x)):
+        raise ValueError("the rows of x must lie whole in memory, one behind the other")
+    return _scores(x, scale, cap)
+
+
+def _scores(x, scale, cap):
+    """The scores of a matrix that `_rows` gave."""
     B, N = x.shape
     return dstd_scores(x.data_ptr(), B, N, _ld(x), DSTD_F32 if x.dtype == _torch().float32 else DSTD_BF16,
                        math.nan if cap is None else cap, scale)
@@ -860,7 +876,7 @@ def top_logits(x, K: int, scale: float = 1.0, cap: Optional[float] = None, idx=N
     logit = (torch.empty_like(idx, dtype=torch.float32) if logit is None else  # half an empty()'s host time
              _given(logit, (B, max(K, 0)), torch.float32, dev, "logit"))
     rest = _out(torch, rest, (B,), torch.float32, dev, "rest")
-    _on(torch, dev, "dstd_top_logits", dstd_top_logits, make_scores(x, scale, cap), K, idx.data_ptr(),
+    _on(torch, dev, "dstd_top_logits", dstd_top_logits, _scores(x, scale, cap), K, idx.data_ptr(),
         logit.data_ptr(), rest.data_ptr())
     return idx, logit, rest
 
@@ -919,7 +935,7 @@ def sample(x, u, scale: float = 1.0, cap: Optional[float] = None, top_k: int = 0
     choice = (torch.empty_like(u, dtype=torch.int32) if choice is None else
               _given(choice, (B,), torch.int32, dev, "choice"))
     logp = torch.empty_like(u) if logp is None else _given(logp, (B,), torch.float32, dev, "logp")
-    _on(torch, dev, "dstd_sample", dstd_sample, make_scores(x, scale, cap),
+    _on(torch, dev, "dstd_sample", dstd_sample, _scores(x, scale, cap),
         dstd_sample_params(int(top_k), float(top_p), float(min_p)), u.data_ptr(), choice.data_ptr(),
         logp.data_ptr())
     return choice, logp
