@@ -439,14 +439,21 @@ bool cap_has_slot(float cap, u32 *bits) {
     return (f & 0xffff) == 0 && mag < static_cast<u32>(kMags);
 }
 
-template <int T, typename E>
+// kMost: the longest rows that T threads take.
+template <int T, int kMost, typename E>
 void launch_sample_rows(dim3 grid, hipStream_t st, int n, int64_t ld, const E *x, ScoreMap m, DrawArgs a) {
-    const bool count = a.top_k > 0 && a.top_k < n, mass = a.top_p < 1.0;
+    const bool mass = a.top_p < 1.0;
 #define SAMPLE(kCount, kMass) \
     hipLaunchKernelGGL((sample_kernel<T, kCount, kMass, E>), grid, dim3(T), 0, st, n, ld, x, m, a)
-    if (count && mass) SAMPLE(true, true);
-    else if (count) SAMPLE(true, false);
-    else if (mass) SAMPLE(false, true);
+    // a top_k that comes here is more than kMaxPicked, and less than n
+    if constexpr (kMost > kMaxPicked) {
+        if (a.top_k > 0) {
+            if (mass) SAMPLE(true, true);
+            else SAMPLE(true, false);
+            return;
+        }
+    }
+    if (mass) SAMPLE(false, true);
     else SAMPLE(false, false);
 #undef SAMPLE
 }
@@ -473,9 +480,9 @@ hipError_t launch_sample_t(const SampleJob &j, hipStream_t st) {
     // Threads a row: small blocks overlap each other's steps, large ones take a long row
     // sooner (fp32, 256 and 1024 threads: 2000 x 9000 34 and 44 us without filters, 78 and 114
     // with top_p; 64 x 15000 with top_p 35 and 25).
-    if (n <= 512) launch_sample_rows<64, E>(grid, st, n, j.in.ld, x, m, a);
-    else if (n <= (filters ? 8192 : 16384)) launch_sample_rows<256, E>(grid, st, n, j.in.ld, x, m, a);
-    else launch_sample_rows<1024, E>(grid, st, n, j.in.ld, x, m, a);
+    if (n <= 512) launch_sample_rows<64, 512, E>(grid, st, n, j.in.ld, x, m, a);
+    else if (n <= (filters ? 8192 : 16384)) launch_sample_rows<256, 16384, E>(grid, st, n, j.in.ld, x, m, a);
+    else launch_sample_rows<1024, 1 << 24, E>(grid, st, n, j.in.ld, x, m, a);
     return hipGetLastError();
 }
 
