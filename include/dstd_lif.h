@@ -360,8 +360,10 @@ dstd_status dstd_distill_grad(int64_t B, int64_t N, int64_t K, const float *t_ou
  *   (1: all), equal scores by index in both,
  *   of these, those with w_i >= min_p (0: all);
  * the choice is the first class, by index, where the sum of the kept w up to it
- * exceeds u times the sum of all kept. Weights are held to 2^-s of the largest,
- * s = min(51, 62 - ceil(log2 N)), and their sums are exact.
+ * exceeds u times the sum of all kept. Weights are rounded to multiples of 2^-s
+ * of the largest, s = min(51, 62 - ceil(log2 N)), and their sums are exact: what a
+ * sum is off by, N 2^-(s+1) of the largest weight, is a step of u (2^-24) at
+ * N = 2^19 and 2^-15 at 2^24, and a class below 2^-(s+1) of the largest is not drawn.
  *  u      [B]     fp32 in [0, 1); others are drawn in to it, NaN counts as 0.
  *  choice [B] out int32; -1 for a row without entries.
  *  logp   [B] out: ln of the choice's probability among the kept, -inf for a row

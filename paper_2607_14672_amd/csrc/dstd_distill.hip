@@ -283,8 +283,8 @@ __global__ __launch_bounds__(T, V >= 16 ? 4 : 1) void distill_row_kernel(KdArgs 
 }
 
 // ---------------------------------------------------- several blocks a row --
-// For rows that no block's registers hold, and for few rows: 1 x 131072 takes 17 us
-// (the host's three launches), 256 x 131072 95 us (268 MB of them read twice).
+// For rows that no block's registers hold, and for few rows: 1 x 131072 takes 15 us
+// (the host's two launches), 256 x 131072 91 us (its 134 MB read twice, and written).
 constexpr int kKdThreads = 256;
 constexpr int kKdChunk = 8192;  // classes of a block
 

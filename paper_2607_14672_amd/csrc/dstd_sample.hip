@@ -54,10 +54,15 @@ __device__ __attribute__((noinline)) void sample_any_row(RowShared<T> &sh, const
 // One class of every row, a block each (threads as in dstd_top.hip): the largest score,
 // then what top_k and top_p keep, then the draw: two readings of the row, and two or three
 // more for each filter. Bound by its fp64 operations, some 30 an entry and reading of
-// weights: 300 x 50021 without filters 40 us (the reads alone would take 20), 105 with top_p.
+// weights: 300 x 50021 without filters 39 us (the reads alone would take 20), 95 with top_p.
 // kCount, kMass: with top_k (more than kMaxPicked), with top_p; a kernel for each, since what
-// one of them needs in registers would be taken from the others' loops (top_p's 105 us were
-// 238 in a kernel of both).
+// one of them needs in registers would be taken from the others' loops (with top_p 238 us in
+// a kernel of both).
+// Two blocks of 1024 threads a CU leave 64 registers a thread, and some of a row's are kept in
+// scratch memory: fp32 9 (no filter), 22 (top_p), 12 (top_k), 98 (both), bf16 94 to 135. Against
+// one block of 128, 300 x 50021 fp32: 39 and 41 us, 95 and 105, 83 and 97, 159 and 151; 1000 rows 85
+// and 96, with top_p 199 and 231. bf16 rows, here only where the cap is no value that is counted
+// below, would gain: 50 and 43 us, 125 and 109, 222 and 102, 318 and 186.
 template <int T, bool kCount, bool kMass, typename E>
 __global__ __launch_bounds__(T, T >= 1024 ? 8 : 4) void sample_kernel(int n, int64_t ld, const E *__restrict__ x,
                                                                       ScoreMap m, DrawArgs a) {

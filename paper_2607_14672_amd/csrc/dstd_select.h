@@ -35,9 +35,11 @@ struct Border {
     __device__ int upto() const { return all() ? -1 : rank_index(last); }
 };
 
-// Weights of the exponentials in 64-bit integers, the largest 2^shift (shift <= 51):
-// their sums do not depend on the order, and what is lost of a weight, 2^-(shift+1) of
-// the largest, is below what sums in 64-bit floats lose over long rows.
+// Weights of the exponentials in 64-bit integers, the largest 2^shift (shift <= 51): their
+// sums do not depend on the order. A weight is off by half a unit, 2^-(shift+1) of the
+// largest, and 0 below that; the sum of a row by up to N times as much, 2^-29 of the largest
+// at 131072 entries, 2^-24 (a step of a random number) at 2^19, 2^-15 at 2^24, where 64-bit
+// floats would lose 2^-29 at most.
 struct Mass {
     double top, scale;  // the largest goodness; |scale|
     int shift;

@@ -142,7 +142,13 @@ __device__ float candidate_bound(RowShared<T> &sh, const E *row, int n, const Sc
 }
 
 // The K first entries into the list where the candidates are too many for it; and the sum
-// over all entries behind a place in the row's order, relative to the largest of them.
+// over all entries behind a place in the row's order, relative to the largest of them. Some
+// eight and one passes entry by entry, for rows where many entries equal the K-th (fewer than
+// K neurons fired, and the silent ones count as a cap) or no bound is found (bf16 rows with
+// a NaN, rows with an entry of +inf goodness that does not count): 256 x 4096 spike times of which
+// 0.5 % fired, K = 32, 37 us instead of 11, 512 x 65536 without any 463 instead of 48, 512 x 131072
+// bf16 all equal 841 and with a NaN a row 400 instead of 56. The sum alone (logits beyond 2^24): 512 x
+// 65536 fp32 76 us instead of 47.
 template <int T, typename E>
 __device__ __attribute__((noinline)) int pick_exactly(RowShared<T> &sh, const E *row, int n, ScoreMap m, int K) {
     const Border kept = pick_count<T, 0, E>(sh, row, n, m, row_extremes<T, 0>(sh, row, n, m), K);
