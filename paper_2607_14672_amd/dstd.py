@@ -868,7 +868,7 @@ def top_logits(x, K: int, scale: float = 1.0, cap: Optional[float] = None, idx=N
     for spike times scale = -1 / tau_soft), falling, equal ones by index. Entries that are
     not finite count as `cap`, or are left out (None). Returns (idx [B, K] int32, logit
     [B, K] f32, rest [B] f32): classes, logits, and the log of the sum of all others'
-    exponentials; -1 and -inf where there is none."""
+    exponentials; -1 and -inf where there is none. |scale| up to 2.35e38."""
     torch = _torch()
     x = _rows(x, (torch.float32, torch.bfloat16), "x")
     dev, B = x.device, x.shape[0]
